@@ -1,4 +1,4 @@
-"""ctypes binding of libmte (include/mte.h): argument marshalling only.
+"""ctypes binding of libmte (include/mte.h, mte_vision.h, mte_cond.h): argument marshalling only.
 
 Every function keeps the C name and returns what the C call returns, except
 that a negative status raises MteError. Device buffers are passed as integer
@@ -20,6 +20,8 @@ MTE_MROPE_SECTIONS, MTE_MROPE_INTERLEAVED = 0, 1
 MTE_WEIGHTS_DTYPE, MTE_WEIGHTS_E4M3 = 0, 1
 STATUS = {0: "MTE_OK", -1: "MTE_E_INVALID", -2: "MTE_E_CAPACITY", -3: "MTE_E_HIP",
           -4: "MTE_E_OOM", -5: "MTE_E_UNSUPPORTED"}
+MTE_ACT_NONE, MTE_ACT_SILU = 0, 1
+MTE_KV8_BLOCK = 32
 KERNEL_CLASSES = {"qkv_gemm": 0, "attention": 1, "o_gemm": 2, "gate_up_gemm": 3, "down_gemm": 4}
 
 
@@ -78,6 +80,18 @@ class mte_vision_weights(C.Structure):
                 ("merge_b1", C.c_void_p), ("merge_w2", C.c_void_p), ("merge_b2", C.c_void_p)]
 
 
+class mte_attn_shape(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("scale", C.c_float),
+                ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+                ("v_row", C.c_int64), ("v_head", C.c_int64), ("o_row", C.c_int64), ("o_head", C.c_int64)]
+
+
+class mte_kv8(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("scales", C.c_void_p),
+                ("n_blocks", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2606_05981_amd.build`")
 lib = C.CDLL(LIB_PATH)
@@ -109,6 +123,21 @@ _sig = {
     "mte_vision_encode": (C.c_int, [_P, _P, C.c_int32, C.c_int32, C.c_int32, _P, _P]),
     "mte_vision_encode_strided": (C.c_int, [_P, _P, C.c_int32, C.c_int32, C.c_int32, _P, C.c_int32, _P]),
     "mte_vision_destroy": (None, [_P]),
+    "mte_cross_attention": (C.c_int, [C.POINTER(mte_attn_shape), _P, _P, _P, _P, C.POINTER(C.c_int32), C.c_int32,
+                                      C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_int32), _P, _P, C.c_int64, _P]),
+    "mte_cross_attention_workspace": (C.c_int64, [C.POINTER(mte_attn_shape), C.POINTER(C.c_int32), C.c_int32,
+                                                  C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_int32)]),
+    "mte_kv8_append": (C.c_int, [C.POINTER(mte_kv8), _P, C.c_int32, C.c_int64, _P, _P, C.c_int64, C.c_int64, _P,
+                                 C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_int32), C.c_int32, _P]),
+    "mte_kv8_read": (C.c_int, [C.POINTER(mte_kv8), _P, C.c_int32, C.c_int64, _P, C.POINTER(C.c_int32), C.c_int32,
+                               _P, _P, C.c_int32, _P]),
+    "mte_kv8_attention": (C.c_int, [C.POINTER(mte_attn_shape), C.POINTER(mte_kv8), _P, C.c_int32, C.c_int64, _P, _P,
+                                    C.POINTER(C.c_int32), C.c_int32, C.c_int32, _P, _P, C.c_int64, _P]),
+    "mte_kv8_attention_workspace": (C.c_int64, [C.POINTER(mte_attn_shape), C.POINTER(C.c_int32), C.c_int32,
+                                                C.c_int32]),
+    "mte_group_norm": (C.c_int, [_P, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P,
+                                 C.c_float, C.c_int32, C.c_int32, _P, C.c_int64, C.c_int64, _P, C.c_int64, _P]),
+    "mte_group_norm_workspace": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(lib, _name)
@@ -277,3 +306,57 @@ def mte_vision_encode_strided(enc: int, pixels: int, n_images: int, height: int,
     return _check(lib.mte_vision_encode_strided(enc, pixels, n_images, height, width, out, image_stride, stream),
                   "mte_vision_encode_strided")
 
+
+def make_attn_shape(n_q_heads, n_kv_heads, head_dim, dtype, scale, q=(0, 0), k=(0, 0), v=(0, 0),
+                    out=(0, 0)) -> mte_attn_shape:
+    """q, k, v, out: (row, head) strides in elements."""
+    return mte_attn_shape(n_q_heads, n_kv_heads, head_dim, dtype, scale, *q, *k, *v, *out)
+
+
+def mte_cross_attention_workspace(shape: mte_attn_shape, q_lens, n_q: int, kv_lens, n_kv: int, kv_index) -> int:
+    """q_lens, kv_lens, kv_index (or None): int32 arrays as _i32 makes them, as in every call below."""
+    return _check(lib.mte_cross_attention_workspace(C.byref(shape), q_lens, n_q, kv_lens, n_kv, kv_index),
+                  "mte_cross_attention_workspace")
+
+
+def mte_cross_attention(shape: mte_attn_shape, q: int, k: int, v: int, key_mask: Optional[int], q_lens, n_q: int,
+                        kv_lens, n_kv: int, kv_index, out: int, workspace: Optional[int], workspace_bytes: int,
+                        stream: int) -> int:
+    return _check(lib.mte_cross_attention(C.byref(shape), q, k, v, key_mask, q_lens, n_q, kv_lens, n_kv, kv_index,
+                                          out, workspace, workspace_bytes, stream), "mte_cross_attention")
+
+
+def mte_kv8_append(cache: mte_kv8, table: int, table_width: int, table_row: int, kv_lens: int, k: int, k_row: int,
+                   k_head: int, v: int, v_row: int, v_head: int, dtype: int, new_lens, n: int, stream: int) -> int:
+    return _check(lib.mte_kv8_append(C.byref(cache), table, table_width, table_row, kv_lens, k, k_row, k_head, v,
+                                     v_row, v_head, dtype, new_lens, n, stream), "mte_kv8_append")
+
+
+def mte_kv8_read(cache: mte_kv8, table: int, table_width: int, table_row: int, kv_lens: int, counts, n: int, k: int,
+                 v: int, dtype: int, stream: int) -> int:
+    return _check(lib.mte_kv8_read(C.byref(cache), table, table_width, table_row, kv_lens, counts, n, k, v, dtype,
+                                   stream), "mte_kv8_read")
+
+
+def mte_kv8_attention_workspace(shape: mte_attn_shape, q_lens, n: int, table_width: int) -> int:
+    return _check(lib.mte_kv8_attention_workspace(C.byref(shape), q_lens, n, table_width),
+                  "mte_kv8_attention_workspace")
+
+
+def mte_kv8_attention(shape: mte_attn_shape, cache: mte_kv8, table: int, table_width: int, table_row: int,
+                      kv_lens: int, q: int, q_lens, n: int, causal: int, out: int, workspace: Optional[int],
+                      workspace_bytes: int, stream: int) -> int:
+    return _check(lib.mte_kv8_attention(C.byref(shape), C.byref(cache), table, table_width, table_row, kv_lens, q,
+                                        q_lens, n, causal, out, workspace, workspace_bytes, stream),
+                  "mte_kv8_attention")
+
+
+def mte_group_norm_workspace(n: int, pixels: int, channels: int, groups: int, dtype: int) -> int:
+    return _check(lib.mte_group_norm_workspace(n, pixels, channels, groups, dtype), "mte_group_norm_workspace")
+
+
+def mte_group_norm(x: int, x_row: int, x_image: int, n: int, pixels: int, channels: int, groups: int,
+                   gamma: Optional[int], beta: Optional[int], eps: float, act: int, dtype: int, y: int, y_row: int,
+                   y_image: int, workspace: Optional[int], workspace_bytes: int, stream: int) -> int:
+    return _check(lib.mte_group_norm(x, x_row, x_image, n, pixels, channels, groups, gamma, beta, eps, act, dtype, y,
+                                     y_row, y_image, workspace, workspace_bytes, stream), "mte_group_norm")

@@ -20,7 +20,7 @@ OUT = os.path.join(HERE, "libmte.so")
 PROBE_OUT = os.path.join(HERE, "libmte_probe.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["gemm.hip", "gemm_f8.hip", "attention.hip", "norm_rope.hip", "vision_kernels.hip",
-           "api.cpp", "vision.cpp"]
+           "cond_attention.hip", "kv8.hip", "group_norm.hip", "api.cpp", "vision.cpp", "cond.cpp"]
 PROBE_SOURCES = ["probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

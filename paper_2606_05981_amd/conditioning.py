@@ -1,0 +1,302 @@
+"""Torch-facing wrappers of include/mte_cond.h: the operators with which a denoiser's layers
+read the encoder's conditioning (cross attention, an 8-bit key/value cache, group norm).
+
+Tensors in, tensors out, as in ``encoder``: PyTorch provides memory and streams, every step
+runs in libmte's HIP kernels, nothing falls back. Workspaces are taken from torch's
+allocator call by call, on the stream the call runs on, so calls on several streams and
+captured graphs share none. A call given a `stream` other than the current one orders
+nothing by itself: the caller makes that stream wait for the inputs, and the current
+one for the results.
+"""
+from __future__ import annotations
+
+import math
+from typing import NamedTuple, Optional, Sequence
+
+import torch
+
+from . import binding as B
+
+_DTYPE = {torch.float32: B.MTE_F32, torch.bfloat16: B.MTE_BF16}
+_ACT = {None: B.MTE_ACT_NONE, "none": B.MTE_ACT_NONE, "silu": B.MTE_ACT_SILU}
+
+
+def _on(device: torch.device, stream: Optional[torch.cuda.Stream], used, fn):
+    """fn(stream handle) with `device` and the stream current; `used` tensors (None allowed) and
+    the results stay allocated until a stream other than their own is done with them."""
+    if stream is None:
+        if device.index == torch.cuda.current_device():
+            return fn(torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(device):
+            return fn(torch.cuda.current_stream().cuda_stream)
+    if stream.device != device:
+        raise ValueError(f"stream: expected one of {device}, got one of {stream.device}")
+    with torch.cuda.device(device):
+        cur = torch.cuda.current_stream()
+        if cur == stream:
+            return fn(stream.cuda_stream)
+        with torch.cuda.stream(stream):
+            res = fn(stream.cuda_stream)
+        for t in used:
+            if t is not None:
+                t.record_stream(stream)
+        for t in res if isinstance(res, tuple) else (res,):
+            if t is not None:
+                t.record_stream(cur)
+        return res
+
+
+def _rows(name: str, t, dtype: torch.dtype, heads: int, d: int, device: torch.device):
+    """Checks a [rows, heads, d] tensor and returns its (row, head) strides."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name}: expected a [tokens, heads, head_dim] tensor")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError(f"{name}: expected shape (*, {heads}, {d}), got {tuple(t.shape)}")
+    row, head, one = t.stride()
+    if t.shape[0] <= 1:
+        row = 0
+    if heads == 1:
+        head = 0
+    if one != 1 or row % 8 or head % 8 or t.data_ptr() % 16:
+        raise ValueError(f"{name}: expected contiguous heads at 16-byte aligned addresses, strides multiples of 8 "
+                         f"elements; got strides {t.stride()}")
+    return row, head
+
+
+def _out_rows(out, q, row_head_of):
+    """Checks a caller's out like q, and that its rows and heads do not overlap."""
+    row, head = row_head_of
+    d, n, heads = q.shape[2], q.shape[0], q.shape[1]
+    if out.shape[0] != n:
+        raise ValueError(f"out: expected {n} rows, got {out.shape[0]}")
+    row, head = (row if n > 1 else None), (head if heads > 1 else None)
+    small, big, count = (row, head, n) if row is not None and head is not None and row < head else (head, row, heads)
+    if (small is not None and small < d) or (big is not None and big < (d if small is None else small * (count - 1) + d)):
+        raise ValueError("out: rows or heads overlap")
+
+
+def _query(q):
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not q.is_cuda or q.dtype not in _DTYPE:
+        raise ValueError("q: expected a [tokens, heads, head_dim] bf16 or fp32 tensor on the GPU")
+    return q.shape[1], q.shape[2], q.dtype, q.device
+
+
+def _lens(name: str, lens: Sequence[int], rows: Optional[int]):
+    n = len(lens)
+    if rows is not None and sum(lens) != rows:
+        raise ValueError(f"{name}: expected lengths that sum to {rows}, got {sum(lens)}")
+    return (B.C.c_int32 * n)(*lens), n
+
+
+def _space(nbytes: int, device: torch.device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: Sequence[int], kv_lens: Sequence[int],
+                    kv_index: Optional[Sequence[int]] = None, key_mask: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """mte_cross_attention: packed queries q [Tq, Hq, d] attend to packed conditioning tokens k, v
+    [Tk, Hkv, d] of another length -> [Tq, Hq, d].
+
+    q_lens / kv_lens: rows of each query / key sequence (0 allowed); kv_index: the key sequence
+    of each query sequence (default: its own), so that one frame's conditioning can serve all
+    ([0] * len(q_lens), as with TECache's batch_one); key_mask: uint8 or bool [Tk], 0 hides a
+    token from every query; scale: default 1 / sqrt(d). A query that sees no token gets
+    zeros. q, k, v (bf16 or fp32) may be strided over tokens and heads."""
+    hq, d, dtype, dev = _query(q)
+    hkv = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
+    sq = _rows("q", q, dtype, hq, d, dev)
+    sk, sv = _rows("k", k, dtype, hkv, d, dev), _rows("v", v, dtype, hkv, d, dev)
+    if v.shape[0] != k.shape[0]:
+        raise ValueError(f"v: expected {k.shape[0]} rows, got {v.shape[0]}")
+    ql, n_q = _lens("q_lens", q_lens, q.shape[0])
+    kl, n_kv = _lens("kv_lens", kv_lens, k.shape[0])
+    if kv_index is not None and len(kv_index) != n_q:
+        raise ValueError(f"kv_index: expected {n_q} entries, got {len(kv_index)}")
+    idx = None if kv_index is None else (B.C.c_int32 * n_q)(*kv_index)
+    if key_mask is not None:
+        if not isinstance(key_mask, torch.Tensor) or key_mask.dtype not in (torch.uint8, torch.bool) or \
+                key_mask.device != dev or tuple(key_mask.shape) != (k.shape[0],) or not key_mask.is_contiguous():
+            raise ValueError(f"key_mask: expected a contiguous uint8 or bool tensor of {k.shape[0]} values on {dev}")
+    so = None
+    if out is not None:
+        so = _rows("out", out, dtype, hq, d, dev)
+        _out_rows(out, q, so)
+    sc = 1.0 / math.sqrt(d) if scale is None else float(scale)
+
+    def call(st):
+        o = torch.empty((q.shape[0], hq, d), dtype=dtype, device=dev) if out is None else out
+        shape = B.mte_attn_shape(hq, hkv, d, _DTYPE[dtype], sc, *sq, *sk, *sv, *((hq * d, d) if so is None else so))
+        need = B.mte_cross_attention_workspace(shape, ql, n_q, kl, n_kv, idx)
+        ws = _space(need, dev)
+        B.mte_cross_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                              None if key_mask is None else key_mask.data_ptr(), ql, n_q, kl, n_kv, idx, o.data_ptr(),
+                              None if ws is None else ws.data_ptr(), need, st)
+        return o
+    return _on(dev, stream, (q, k, v, key_mask, out), call)
+
+
+class KV8Cache(NamedTuple):
+    """A key/value cache in 8 bits (mte_kv8): blocks of 32 tokens of all kv heads, e4m3 codes with one
+    power of two for each block, head and tensor. A sequence is a row of block numbers in a
+    table and a length, both on the device and the caller's; any triple of such tensors
+    serves as a cache."""
+    k_codes: torch.Tensor    # uint8 [blocks, Hkv, d / 16, 32, 16]
+    v_codes: torch.Tensor    # uint8 [blocks, Hkv, d, 32]
+    scales: torch.Tensor     # float32 [blocks, Hkv, 2]
+
+
+def kv8_cache(n_blocks: int, n_kv_heads: int, head_dim: int, device="cuda") -> KV8Cache:
+    """An empty cache of n_blocks * 32 tokens (head_dim 64 or 128)."""
+    if n_blocks <= 0 or n_kv_heads <= 0 or head_dim not in (64, 128):
+        raise ValueError("expected n_blocks > 0, n_kv_heads > 0 and head_dim 64 or 128")
+    return KV8Cache(torch.zeros((n_blocks, n_kv_heads, head_dim // 16, 32, 16), dtype=torch.uint8, device=device),
+                    torch.zeros((n_blocks, n_kv_heads, head_dim, 32), dtype=torch.uint8, device=device),
+                    torch.full((n_blocks, n_kv_heads, 2), 2.0 ** -126, dtype=torch.float32, device=device))
+
+
+def _cache(cache, table, kv_lens, n: int, dev: torch.device):
+    """Checks a cache with the table and lengths of n sequences -> (mte_kv8, width, table row)."""
+    kc, vc, sc = cache
+    for name, t, dt in (("k_codes", kc, torch.uint8), ("v_codes", vc, torch.uint8), ("scales", sc, torch.float32)):
+        if not isinstance(t, torch.Tensor) or t.dtype != dt or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"cache {name}: expected a contiguous {dt} tensor on {dev}")
+    if vc.dim() != 4:
+        raise ValueError("cache v_codes: expected [blocks, heads, head_dim, 32]")
+    nb, h, d, _ = vc.shape
+    if tuple(vc.shape) != (nb, h, d, 32) or tuple(kc.shape) != (nb, h, d // 16, 32, 16) or \
+            tuple(sc.shape) != (nb, h, 2):
+        raise ValueError(f"cache: shapes {tuple(kc.shape)}, {tuple(vc.shape)}, {tuple(sc.shape)} do not fit together")
+    if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.device != dev or \
+            table.dim() != 2 or table.shape[0] != n or table.shape[1] == 0 or \
+            (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError(f"table: expected an int32 [{n}, blocks] tensor on {dev} with contiguous rows")
+    if not isinstance(kv_lens, torch.Tensor) or kv_lens.dtype != torch.int32 or kv_lens.device != dev or \
+            tuple(kv_lens.shape) != (n,) or not kv_lens.is_contiguous():
+        raise ValueError(f"kv_lens: expected a contiguous int32 tensor of {n} lengths on {dev}")
+    return B.mte_kv8(kc.data_ptr(), vc.data_ptr(), sc.data_ptr(), nb, h, d), table.shape[1], table.stride(0)
+
+
+def kv8_append(cache, table: torch.Tensor, kv_lens: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+               new_lens: Sequence[int], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mte_kv8_append: rows k, v [sum(new_lens), Hkv, d] become the newest new_lens[i] tokens of each
+    sequence, whose lengths afterwards are kv_lens (int32, device); table int32 [n, blocks], device."""
+    n = len(new_lens)
+    if not isinstance(k, torch.Tensor) or k.dim() != 3 or not k.is_cuda or k.dtype not in _DTYPE:
+        raise ValueError("k: expected a [tokens, heads, head_dim] bf16 or fp32 tensor on the GPU")
+    dev = k.device
+    c, width, row = _cache(cache, table, kv_lens, n, dev)
+    sk = _rows("k", k, k.dtype, c.n_kv_heads, c.head_dim, dev)
+    sv = _rows("v", v, k.dtype, c.n_kv_heads, c.head_dim, dev)
+    lens, _ = _lens("new_lens", new_lens, k.shape[0])
+    if v.shape[0] != k.shape[0]:
+        raise ValueError(f"v: expected {k.shape[0]} rows, got {v.shape[0]}")
+    _on(dev, stream, (*cache, table, kv_lens, k, v),
+        lambda st: B.mte_kv8_append(c, table.data_ptr(), width, row, kv_lens.data_ptr(), k.data_ptr(), *sk,
+                                    v.data_ptr(), *sv, _DTYPE[k.dtype], lens, n, st) and None)
+
+
+def kv8_read(cache, table: torch.Tensor, kv_lens: torch.Tensor, counts: Sequence[int],
+             dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None):
+    """mte_kv8_read: the newest counts[i] tokens of each sequence -> (k, v), each
+    [sum(counts), Hkv, d] of `dtype` (bf16 or fp32, both exact)."""
+    if dtype not in _DTYPE:
+        raise ValueError("dtype: expected torch.bfloat16 or torch.float32")
+    dev = cache[0].device
+    c, width, row = _cache(cache, table, kv_lens, len(counts), dev)
+    lens, n = _lens("counts", counts, None)
+    total = sum(counts)
+    if n and min(counts) < 0:
+        raise ValueError("counts: expected lengths of 0 or more")
+
+    def call(st):
+        k = torch.empty((total, c.n_kv_heads, c.head_dim), dtype=dtype, device=dev)
+        v = torch.empty_like(k)
+        B.mte_kv8_read(c, table.data_ptr(), width, row, kv_lens.data_ptr(), lens, n, k.data_ptr(), v.data_ptr(),
+                       _DTYPE[dtype], st)
+        return k, v
+    return _on(dev, stream, (*cache, table, kv_lens), call)
+
+
+def kv8_attention(q: torch.Tensor, cache, table: torch.Tensor, kv_lens: torch.Tensor, q_lens: Sequence[int],
+                  causal: bool = False, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """mte_kv8_attention: packed queries q [Tq, Hq, d] attend to their sequence's cached tokens ->
+    [Tq, Hq, d]. causal: query u of q_lens[i] sees the tokens up to kv_lens[i] - q_lens[i] + u
+    (append its own token first). The work is split for sequences as long as the table is wide:
+    a narrower view table[:, :m] serves shorter ones better."""
+    hq, d, dtype, dev = _query(q)
+    c, width, row = _cache(cache, table, kv_lens, len(q_lens), dev)
+    sq = _rows("q", q, dtype, hq, c.head_dim, dev)
+    lens, n = _lens("q_lens", q_lens, q.shape[0])
+    so = None
+    if out is not None:
+        so = _rows("out", out, dtype, hq, d, dev)
+        _out_rows(out, q, so)
+    sc = 1.0 / math.sqrt(d) if scale is None else float(scale)
+
+    def call(st):
+        o = torch.empty((q.shape[0], hq, d), dtype=dtype, device=dev) if out is None else out
+        shape = B.mte_attn_shape(hq, c.n_kv_heads, d, _DTYPE[dtype], sc, *sq, 0, 0, 0, 0,
+                                 *((hq * d, d) if so is None else so))
+        need = B.mte_kv8_attention_workspace(shape, lens, n, width)
+        ws = _space(need, dev)
+        B.mte_kv8_attention(shape, c, table.data_ptr(), width, row, kv_lens.data_ptr(), q.data_ptr(), lens, n,
+                            1 if causal else 0, o.data_ptr(), None if ws is None else ws.data_ptr(), need, st)
+        return o
+    return _on(dev, stream, (q, *cache, table, kv_lens, out), call)
+
+
+def _pixels(name: str, t: torch.Tensor):
+    """(image stride, row stride, pixels) of a channels-last [N, P, C] or [N, H, W, C] tensor."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: expected contiguous channels (the last dimension), got strides {t.stride()}")
+    if t.dim() == 3:
+        row, px = t.stride(1), t.shape[1]
+    else:
+        h, w = t.shape[1], t.shape[2]
+        if h > 1 and w > 1 and t.stride(1) != w * t.stride(2):
+            raise ValueError(f"{name}: expected pixels at one stride, got strides {t.stride()}")
+        row, px = t.stride(2) if w > 1 else t.stride(1), h * w
+    return t.stride(0) if t.shape[0] > 1 else 0, row if px > 1 else 0, px
+
+
+def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None,
+               beta: Optional[torch.Tensor] = None, eps: float = 1e-5, act: Optional[str] = None,
+               out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """mte_group_norm: act(group norm of x), x channels last [N, P, C] or [N, H, W, C] (bf16 or fp32; a
+    channels_last NCHW tensor is x.permute(0, 2, 3, 1)), channels contiguous, pixels at one stride
+    (a slice of a wider buffer's channels is fine). gamma, beta: [C] of x's dtype; act: None or
+    "silu". out: like x, or x itself."""
+    if not isinstance(x, torch.Tensor) or x.dim() not in (3, 4) or not x.is_cuda or x.dtype not in _DTYPE:
+        raise ValueError("x: expected a [N, P, C] or [N, H, W, C] bf16 or fp32 tensor on the GPU")
+    if act not in _ACT:
+        raise ValueError(f"act: expected None or 'silu', got {act!r}")
+    dev, dtype, C = x.device, x.dtype, x.shape[-1]
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        if t is not None and (t.dtype != dtype or t.device != dev or tuple(t.shape) != (C,) or not t.is_contiguous()):
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {C} values on {dev}")
+    xi, xr, px = _pixels("x", x)
+    n = x.shape[0]
+    if out is not None:
+        if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != dtype or out.device != dev:
+            raise ValueError(f"out: expected a {dtype} tensor of shape {tuple(x.shape)} on {dev}")
+        oi, orow, _ = _pixels("out", out)
+        if (px > 1 and orow < C) or (n > 1 and oi < (px - 1) * orow + C):
+            raise ValueError("out: pixels or images overlap")
+
+    def call(st):
+        y = torch.empty(x.shape, dtype=dtype, device=dev) if out is None else out
+        yi, yr, _ = _pixels("out", y)
+        need = B.mte_group_norm_workspace(n, px, C, groups, _DTYPE[dtype])
+        ws = _space(need, dev)
+        B.mte_group_norm(x.data_ptr(), xr, xi, n, px, C, groups, None if gamma is None else gamma.data_ptr(),
+                         None if beta is None else beta.data_ptr(), eps, _ACT[act], _DTYPE[dtype], y.data_ptr(), yr, yi,
+                         None if ws is None else ws.data_ptr(), need, st)
+        return y
+    return _on(dev, stream, (x, gamma, beta, out), call)
