@@ -70,7 +70,9 @@ AttnProblem problem(const mte_attn_shape &s, const int32_t *q_lens, int32_t n) {
   p.c.n_split = 1;
   p.c.ws_rows = 0;
   p.c.ws_ml = 0;
+  p.c.big = 0;
   p.dtype = s.dtype;
+  p.near_rows = s.k_row < (1 << 24) && s.v_row < (1 << 24);
   p.q_lens = q_lens;
   p.n = n;
   return p;

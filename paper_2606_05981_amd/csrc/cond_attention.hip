@@ -48,6 +48,20 @@ __device__ __forceinline__ int find_seq(const CondSeq *seq, int n, int tile) {
   return lo;
 }
 
+// The workgroup's tile and kv head, heads next to each other: the workgroups that run together then read
+// and write whole rows of q and out between them (head-major order: 4 to 10% slower).
+struct Unit { int tile, g; };
+__device__ __forceinline__ Unit unit_of(int hkv) {
+  const int flat = blockIdx.x;
+  Unit u;
+  u.tile = flat / hkv;
+  u.g = flat - u.tile * hkv;
+  return u;
+}
+
+// Least key tiles of a split of k_cross_stream.
+constexpr int kStreamLeast = 8;
+
 // Key tiles [lo, hi) of split `split` of n_split over nt key tiles; used: the splits
 // that have any (at least 1). A split takes at least `least` tiles.
 struct Span { int lo, hi, used; };
@@ -61,6 +75,12 @@ __device__ __forceinline__ Span split_span(int nt, int n_split, int split, int l
 }
 
 // Running softmax of one row per lane (both halves of the wave hold the same row).
+// m is a reference, not quite the maximum: it moves only when some row of the wave has a
+// score more than kSlack above it, so that O and l are rescaled in the first step and hardly
+// ever after (with random scores every step raises some row's maximum a little, and the 64
+// multiplications of a rescaled O of 128 were a fifth of the step's vector work).
+// Probabilities are then at most 2^kSlack, and relative precision is what it was.
+constexpr float kSlack = 8.f;
 template <int ND> struct Rows {
   f32x16 o[ND];
   float m, l;      // m in log2 units; l over this lane's keys only
@@ -78,23 +98,52 @@ template <int ND> struct Rows {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[n][r] *= f;
   }
-  // takes the maximum mb of new scores (log2 units), returns what to subtract from them
+  // Takes the maximum mb (log2 units) of this lane's new scores and returns what to subtract from them.
   __device__ __forceinline__ float raise(float mb) {
-    const float m_new = fmaxf(m, mb);
-    const float ref = m_new == -INFINITY ? 0.f : m_new;   // nothing seen yet: exp2(-inf - 0) = 0
-    const float alpha = __builtin_amdgcn_exp2f(m - ref);
-    l *= alpha;
-    if (__any(alpha != 1.f)) scale(alpha);
+    if (over(mb)) lift(mb);
+    return ref();
+  }
+  __device__ __forceinline__ bool over(float mb) const { return __any(mb > m + kSlack); }   // wave-uniform
+  __device__ __forceinline__ float ref() const { return m == -INFINITY ? 0.f : m; }   // nothing seen yet: exp2(-inf - 0) = 0
+  __device__ __forceinline__ void lift(float mb) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
+    const float m_new = fmaxf(m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
+    if (__any(m != -INFINITY)) {                        // else O and l are still zero
+      const float alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.f : m_new));
+      l *= alpha;
+      scale(alpha);
+    }
     m = m_new;
-    return ref;
   }
 };
 
-// Keeps the scores of keys whose bit in `word` (bit = key of the 32) is set.
-__device__ __forceinline__ void mask_scores(f32x16 &s, uint32_t word, int lane) {
-  const uint32_t w = word >> (4 * (lane >> 5));
+// Keeps the scores of keys whose bit in `word` (wave-uniform; bit = key of the 32) is set: the lane
+// masks of the two halves are scalar work, one select a score.
+__device__ __forceinline__ void mask_word(f32x16 &s, uint32_t word) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) s[r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? s[r] : -INFINITY;
+  for (int r = 0; r < 16; ++r) {
+    const int k = 8 * (r >> 2) + (r & 3);
+    const uint32_t lo = (uint32_t)((int32_t)(word << (31 - k)) >> 31);
+    const uint32_t hi = (uint32_t)((int32_t)(word << (27 - k)) >> 31);
+    s[r] = __builtin_amdgcn_inverse_ballot_w64((uint64_t)hi << 32 | lo) ? s[r] : -INFINITY;
+  }
+}
+// Keeps the scores of this lane's keys below `n` (of the 32).
+__device__ __forceinline__ void mask_below(f32x16 &s, int n, int lane) {
+  const int left = n - 4 * (lane >> 5);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
+}
+__device__ __forceinline__ float max16(const f32x16 &s, float mb) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) mb = fmaxf(mb, s[i]);
+  return mb;
+}
+
+// Memory that is constant while a kernel runs, read at wave-uniform addresses: scalar loads.
+template <typename T> __device__ __forceinline__ T uniform_at(const T *p, int64_t i) {
+  typedef const T __attribute__((address_space(4))) * ptr;
+  return ((ptr)(uintptr_t)p)[i];
 }
 
 // Joins the KW waves' states of the same 32 rows through LDS into wave 0's.
@@ -133,6 +182,25 @@ __device__ __forceinline__ void join_waves(Rows<ND> &st, float *red, int kw, int
   st.m = mx;
 }
 
+// 8 consecutive d (16 p + 8 h .. of a 32-wide block) of this lane's row as bf16.
+__device__ __forceinline__ u32x4 out_chunk(const f32x16 &o, int p, float inv) {
+  bf16x4 lo, hi;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    lo[e] = (bf16)(o[8 * p + e] * inv);
+    hi[e] = (bf16)(o[8 * p + 4 + e] * inv);
+  }
+  u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    // the upper 32 lanes' x and the lower 32 lanes' y trade places
+    const auto r = __builtin_amdgcn_permlane32_swap(x[w], y[w], false, false);
+    x[w] = r[0];
+    y[w] = r[1];
+  }
+  return u32x4{x[0], x[1], y[0], y[1]};
+}
+
 // Writes a wave's finished rows (lane: row `tok`, head `head`; vscale: factor of O that
 // the probabilities did not carry) or, split, their partial state.
 template <typename T, int ND>
@@ -155,22 +223,9 @@ __device__ __forceinline__ void store_rows(const AttnCommon &a, Rows<ND> &st, fl
     } else {
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        bf16x4 lo, hi;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          lo[e] = (bf16)(st.o[n][8 * p + e] * inv);
-          hi[e] = (bf16)(st.o[n][8 * p + 4 + e] * inv);
-        }
-        u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          // the upper 32 lanes' x and the lower 32 lanes' y trade places: 8 consecutive d a lane
-          const auto r = __builtin_amdgcn_permlane32_swap(x[w], y[w], false, false);
-          x[w] = r[0];
-          y[w] = r[1];
-        }
         const int c = 32 * n + 16 * p + 8 * h;
-        if (live && c < a.d) *(u32x4 *)(row + c) = u32x4{x[0], x[1], y[0], y[1]};
+        const u32x4 x = out_chunk(st.o[n], p, inv);
+        if (live && c < a.d) *(u32x4 *)(row + c) = x;
       }
     }
   }
@@ -208,6 +263,82 @@ __device__ __forceinline__ void store_part(const AttnCommon &a, Rows<ND> &st, fl
 // writes nor the operand reads meet in a bank; values as rows, chunks xored so that the
 // transposing reads (bf16: 4 keys x 16 d per 16 lanes) and the fp32 reads (one d column
 // a lane) do not either.
+// Probabilities of 32 keys, p = 2^(sc s - ref), as the operand of the value product: bf16 (the values'
+// type: their range is bf16's; each term off by at most 2^-8 of itself) or fp32.
+template <typename T> struct Probs;
+template <> struct Probs<bf16> { bf16x8 f[2]; };
+template <> struct Probs<float> { float p[16]; };
+__device__ __forceinline__ void set_probs(Probs<bf16> &o, const float *p) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o.f[e >> 3][e & 7] = (bf16)p[e];
+}
+__device__ __forceinline__ void set_probs(Probs<float> &o, const float *p) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o.p[e] = p[e];
+}
+template <typename T>
+__device__ __forceinline__ Probs<T> probs_of(const f32x16 &s, float sc, float ref, float &l) {
+  float p[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -ref));
+    l += p[i];
+  }
+  Probs<T> o;
+  set_probs(o, p);
+  return o;
+}
+
+// O += V^T P^T for the 32 keys of subtile `sub`. Values as rows in LDS at sv, chunks xored.
+template <int NCH, bool B16> __device__ __forceinline__ int value_chunk(int row, int c) {
+  if constexpr (!B16) return c ^ (8 * ((row >> 2) & 1));
+  else if constexpr (NCH == 16) return c ^ (4 * (row & 3));
+  else return c ^ (4 * ((row >> 1) & 1));
+}
+template <typename T, int DP>
+__device__ __forceinline__ void add_values(f32x16 (&o)[DP / 32], const Probs<T> &p, const char *sv, int sub, int lane) {
+  constexpr int NCH = DP * sizeof(T) / 16, ND = DP / 32;
+  const int h = lane >> 5, lrow = lane & 31;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const int row = sub * 32 + 16 * f + 4 * h + ((lane & 15) >> 2);
+#pragma unroll
+      for (int n = 0; n < ND; ++n) {
+        const int c = 4 * n + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        const char *va = sv + (row * NCH + value_chunk<NCH, true>(row, c)) * 16 + (lane & 1) * 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)va);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(va + 8 * NCH * 16));
+        mfma32(o[n], __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), p.f[f]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = sub * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
+      const float *vr = (const float *)sv + row * DP;
+#pragma unroll
+      for (int n = 0; n < ND; ++n)
+        o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[32 * (n ^ h) + lrow], p.p[i], o[n], 0, 0, 0);
+    }
+  }
+}
+
+// S^T = K Q^T of subtile `sub`: keys as operand chunks in LDS at sk.
+template <typename T, int DP>
+__device__ __forceinline__ void key_scores(f32x16 &s, const u32x4 *sk,
+                                           const typename QFrag<T>::type (&qf)[DP * sizeof(T) / 32], int sub, int lane) {
+  constexpr int NCH = DP * sizeof(T) / 16;
+  const int lrow = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < NCH / 2; ++kk) {
+    const int c = 2 * kk + h;
+    mfma32(s, __builtin_bit_cast(typename QFrag<T>::type, sk[(sub * NCH + c) * 32 + (lrow ^ (c & 7))]), qf[kk]);
+  }
+}
+
 template <typename T, int DP, int RW>
 __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
   constexpr bool B16 = sizeof(T) == 2;
@@ -227,7 +358,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
   const int rw = wave % RW, kw = wave / RW;
-  const int tile = blockIdx.x, g = blockIdx.y, split = blockIdx.z;
+  const Unit un = unit_of(a.hkv);
+  const int tile = un.tile, g = un.g, split = blockIdx.y;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int klen = sq.k_len, rows = sq.q_len * a.rep;
   const int r0 = (tile - sq.tile0) * 32 * RW + rw * 32;   // first row of the wave
@@ -269,11 +401,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
     for (int t = 0; t < STEP; ++t) {
       const int idx = tid + (t0 + t) * kThreads, row = idx / NCH, c = idx % NCH;
       sk[((row >> 5) * NCH + c) * 32 + ((row & 31) ^ (c & 7))] = kx[t];
-      int vc;
-      if constexpr (!B16) vc = c ^ (8 * ((row >> 2) & 1));
-      else if constexpr (NCH == 16) vc = c ^ (4 * (row & 3));
-      else vc = c ^ (4 * ((row >> 1) & 1));
-      *(u32x4 *)(sv + (row * NCH + vc) * 16) = vx[t];
+      *(u32x4 *)(sv + (row * NCH + value_chunk<NCH, B16>(row, c)) * 16) = vx[t];
     }
   };
   auto lmask = [&]() {
@@ -305,62 +433,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
     float mb = -INFINITY;
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
-      const int sub = kw * NS + u;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        const int c = 2 * kk + h;
-        mfma32(s[u], __builtin_bit_cast(frag_t, sk[(sub * NCH + c) * 32 + (lrow ^ (c & 7))]), qf[kk]);
-      }
-      const uint32_t word = __builtin_amdgcn_readfirstlane(sm[sub]);
-      if (word != 0xFFFFFFFFu) mask_scores(s[u], word, lane);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mb = fmaxf(mb, s[u][i]);
+      key_scores<T, DP>(s[u], sk, qf, kw * NS + u, lane);
+      const uint32_t word = __builtin_amdgcn_readfirstlane(sm[kw * NS + u]);
+      if (word != 0xFFFFFFFFu) mask_word(s[u], word);
+      mb = max16(s[u], mb);
     }
-    mb = warp_max_xor(mb, 32) * a.sc;
-    const float ref = st.raise(mb);
+    const float ref = st.raise(mb * a.sc);
 #pragma unroll
-    for (int u = 0; u < NS; ++u) {
-      const int sub = kw * NS + u;
-      float p[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], a.sc, -ref));
-        st.l += p[i];
-      }
-      if constexpr (B16) {
-        // P in bf16, the values' type (their range is bf16's): each term off by at most 2^-8 of itself
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          bf16x8 pf;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pf[e] = (bf16)p[8 * f + e];
-          const int i = lane & 15;
-          const int row = sub * 32 + 16 * f + 4 * h + (i >> 2);
-#pragma unroll
-          for (int n = 0; n < ND; ++n) {
-            const int c = 4 * n + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            const int vc = NCH == 16 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
-            const char *va = sv + (row * NCH + vc) * 16 + (lane & 1) * 8;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)va);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(va + 8 * NCH * 16));
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const s16x8 w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            mfma32(st.o[n], __builtin_bit_cast(bf16x8, w), pf);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int row = sub * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-          const float *vr = (const float *)sv + row * DP;
-#pragma unroll
-          for (int n = 0; n < ND; ++n)
-            st.o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[32 * (n ^ h) + lrow], p[i], st.o[n], 0, 0, 0);
-        }
-      }
-    }
+    for (int u = 0; u < NS; ++u)
+      add_values<T, DP>(st.o, probs_of<T>(s[u], a.sc, ref, st.l), sv, kw * NS + u, lane);
   };
 
   for (int kt = span.lo; kt < span.hi; ++kt) {
@@ -391,49 +472,298 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
   else store_part<ND>(a, st, 1.f, live, tile, g, split, rw * 32 + lrow, lane);
 }
 
+// Lane j: which keys of the 32-key tile t0 + j count (a bit each), for up to 64 tiles.
+__device__ __forceinline__ uint32_t tile_words(const uint8_t *mask, int klen, int t0, int lane) {
+  if (!mask) {
+    const int n = klen - (t0 + lane) * 32;
+    return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+  }
+  uint32_t words = 0;
+  const int nk = min((klen + 31) / 32 - t0, 64);
+  for (int j0 = 0; j0 < nk; j0 += 16) {              // 512 keys a round, their bytes in flight together
+    bool see[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int key = (t0 + j0 + 2 * i) * 32 + lane;
+      see[i] = mask[min(key, klen - 1)] != 0 && key < klen;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint64_t b = __ballot(see[i]);
+      if (lane == j0 + 2 * i) words = (uint32_t)b;
+      if (lane == j0 + 2 * i + 1) words = (uint32_t)(b >> 32);
+    }
+  }
+  return words;
+}
+
+// One row tile over n steps of 32 keys, two at a time.
+//   scores(i, s): raw scores;  mask(i, s);  factor(i): what turns them into log2 units;
+//   probs(i, s, ref): their operand;  values(i, p): O += V^T P^T.
+template <int ND, typename P, typename SC, typename MA, typename FA, typename PR, typename VA>
+__device__ __forceinline__ void attend_steps(Rows<ND> &st, int n, SC scores, MA mask, FA factor, PR probs, VA values) {
+  int i = 0;
+  for (; i + 2 <= n; i += 2) {
+    f32x16 s0, s1;
+    scores(i, s0);
+    scores(i + 1, s1);
+    mask(i, s0);
+    mask(i + 1, s1);
+    const float ref = st.raise(fmaxf(max16(s0, -INFINITY) * factor(i), max16(s1, -INFINITY) * factor(i + 1)));
+    const P p0 = probs(i, s0, ref), p1 = probs(i + 1, s1, ref);
+    values(i, p0);
+    values(i + 1, p1);
+  }
+  if (i < n) {
+    f32x16 s0;
+    scores(i, s0);
+    mask(i, s0);
+    const float ref = st.raise(max16(s0, -INFINITY) * factor(i));
+    values(i, probs(i, s0, ref));
+  }
+}
+
+constexpr int kBox = 4096;          // a wave's LDS for it
+// A store that leaves nothing in L2 (written out: as a branch of two stores of one value the
+// compiler makes one plain store of it).
+__device__ __forceinline__ void store_past_caches(u32x4 *p, const u32x4 &x) {
+  asm volatile("global_store_dwordx4 %0, %1, off nt" ::"v"(p), "v"(x) : "memory");
+}
+// Rows of a tile between memory and the lanes that own them, 128 bytes of a row at a time: a load or
+// store takes 8 whole lines (8 lanes each), and 4 KB of LDS of the wave's own turn them (chunks
+// xored with the row: neither side meets in a bank). Straight from the owning lanes an access
+// would take 32 bytes of 32 rows: on 65536 rows of 10 heads of 64, copied, 40 us against 31.5.
+// The rows of the tile: r0 .. of `rows`, token r / rep and head g rep + r % rep.
+struct TileRows {
+  int64_t tok0;        // token of row r0, absolute
+  int rem0, left;      // r0 % rep, rows that exist
+  float inv;           // 1 / rep
+  __device__ __forceinline__ TileRows(const AttnCommon &a, const CondSeq &sq, int r0, int rows) {
+    const int t = r0 / a.rep;
+    tok0 = sq.q0 + t;
+    rem0 = r0 - t * a.rep;
+    left = rows - r0;
+    inv = 1.f / (float)a.rep;
+  }
+  // token offset of row r0 + i and its head within the group (small numbers: exact in fp32)
+  __device__ __forceinline__ int split(int i, int rep, int &head) const {
+    const int x = rem0 + i, t = (int)(((float)x + 0.5f) * inv);
+    head = x - t * rep;
+    return t;
+  }
+};
+template <typename T, int DP> struct QTile {
+  static constexpr int PARTS = DP * sizeof(T) / 128, E = 16 / sizeof(T);
+  u32x4 x[PARTS * 4];
+  __device__ __forceinline__ void load(const AttnCommon &a, const TileRows &t, int g, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * i + (lane >> 3);
+      int head;
+      const int tok = t.split(r, a.rep, head);
+      const T *row = (const T *)a.q + (t.tok0 + tok) * a.q_row + (int64_t)(g * a.rep + head) * a.q_head;
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) {
+        const int c = (8 * j + (lane & 7)) * E;
+        x[4 * j + i] = u32x4{0, 0, 0, 0};
+        if (r < t.left && c < a.d) x[4 * j + i] = *(const u32x4 *)(row + c);
+      }
+    }
+  }
+  // part j into the wave's 4 KB; then chunk c (of 8) of this lane's row
+  __device__ __forceinline__ void spread(u32x4 *box, int j, int lane) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) box[64 * i + (lane & 56) + ((lane & 7) ^ (lane >> 3))] = x[4 * j + i];
+  }
+  static __device__ __forceinline__ u32x4 chunk(const u32x4 *box, int c, int lane) {
+    const int r = lane & 31;
+    return box[r * 8 + (c ^ (r & 7))];
+  }
+};
+template <typename T, int ND>
+__device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, float vscale, const TileRows &t, int g,
+                                           u32x4 *box, int lane) {
+  constexpr int E = 16 / sizeof(T), PARTS = ND * 32 * sizeof(T) / 128;
+  const float l = st.l + __shfl_xor(st.l, 32, kWave);
+  const float inv = l > 0.f ? vscale / l : 0.f;
+  const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int j = 0; j < PARTS; ++j) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        box[r * 8 + ((2 * b + h) ^ (r & 7))] =
+            __builtin_bit_cast(u32x4, f32x4{st.o[j][4 * b] * inv, st.o[j][4 * b + 1] * inv, st.o[j][4 * b + 2] * inv,
+                                            st.o[j][4 * b + 3] * inv});
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) box[r * 8 + ((2 * q + h) ^ (r & 7))] = out_chunk(st.o[2 * j + (q >> 1)], q & 1, inv);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 x = box[64 * i + (lane & 56) + ((lane & 7) ^ (lane >> 3))];
+      const int row = 8 * i + (lane >> 3), c = (8 * j + (lane & 7)) * E;
+      int head;
+      const int tok = t.split(row, a.rep, head);
+      u32x4 *to = (u32x4 *)((T *)a.out + (t.tok0 + tok) * a.o_row + (int64_t)(g * a.rep + head) * a.o_head + c);
+      if (row < t.left && c < a.d) {
+        if (a.big) store_past_caches(to, x);
+        else *to = x;
+      }
+    }
+  }
+}
+
+// Many rows, keys streamed: four waves of 32 rows over a ring of 32-key tiles that the LDS-direct
+// copies (dma16) fill two tiles ahead, one barrier a tile. No registers and no vector work for
+// the staging, so that three waves fit a SIMD (head_dim 128), and workgroups in different phases
+// share a compute unit: rows come and go while others compute.
+// Tiles: keys [32][NCH chunks], values the same, chunk c of row r at c ^ key_swz / value_chunk: whole
+// rows for the copies, free of bank conflicts for the operand reads. Rows past the end repeat the
+// last one; their scores are masked, and value rows that must not count (past the end, masked)
+// are overwritten with zeros by the wave that copied them.
+// The ring's idle slots turn the rows (QTile): before the first barrier the last ones, after the
+// last barrier those that the last tile does not use.
+template <int NCH> __device__ __forceinline__ int key_swz(int r, int c) { return c ^ (r & (NCH - 1)); }
+template <int DP> struct Stream {
+  static constexpr int NCH = DP / 8, TILE = 32 * NCH;     // chunks a row; 16-byte chunks of a tile's keys
+  static constexpr int NB = DP == 64 ? 4 : 3;             // two slots for the first tiles, and the waves' kBox
+  static constexpr int COPIES = TILE / 64 / 4;            // 1 KB copies of keys (and of values) a wave and tile
+  static constexpr int BYTES = NB * 2 * TILE * 16;
+  static_assert((NB - 2) * 2 * TILE * 16 >= 4 * kBox, "room to turn the rows");
+};
+template <int DP>
+__global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(CrossArgs a) {
+  typedef Stream<DP> S;
+  constexpr int NCH = S::NCH, NK = NCH / 2, ND = DP / 32, CP = S::COPIES;
+  extern __shared__ u32x4 lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lrow = lane & 31, h = lane >> 5;
+  const Unit un = unit_of(a.hkv);
+  const int tile = un.tile, g = un.g, split = blockIdx.y;
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
+  const int klen = sq.k_len, nk = (klen + 31) >> 5;
+  const int rows = sq.q_len * a.rep, r0 = (tile - sq.tile0) * 128 + wave * 32;
+  const Span span = split_span(nk, a.n_split, split, kStreamLeast);
+  if (split >= span.used) return;                   // the whole workgroup
+
+  const bf16 *kg = (const bf16 *)a.k + (int64_t)sq.k0 * a.k_row + (int64_t)g * a.k_head;
+  const bf16 *vg = (const bf16 *)a.v + (int64_t)sq.k0 * a.v_row + (int64_t)g * a.v_head;
+  const uint8_t *mg = a.mask ? a.mask + sq.k0 : nullptr;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  // copy i of this wave: rows RPC (wave CP + i) .. of the tile
+  constexpr int RPC = 64 / NCH;
+  auto copy_tile = [&](int t) {
+    const bf16 *kb = kg + (int64_t)t * 32 * a.k_row, *vb = vg + (int64_t)t * 32 * a.v_row;
+    const uint32_t to = lds0 + (uint32_t)(((t - span.lo) % S::NB) * 2 * S::TILE + wave * CP * 64) * 16;
+#pragma unroll
+    for (int i = 0; i < CP; ++i) {
+      const int r = RPC * (wave * CP + i) + lane / NCH, p = lane % NCH;
+      const int row = min(r, klen - 1 - t * 32);
+      const int kc = key_swz<NCH>(r, p) * 8, vc = value_chunk<NCH, true>(r, p) * 8;
+      dma16(kb, (uint32_t)(row * (int)a.k_row + (kc < a.d ? kc : 0)) * 2u, to + i * 1024);
+      dma16(vb, (uint32_t)(row * (int)a.v_row + (vc < a.d ? vc : 0)) * 2u, to + (S::TILE + i * 64) * 16);
+    }
+  };
+  const TileRows rw(a, sq, r0, rows);
+  QTile<bf16, DP> qt;
+  if (r0 < rows) qt.load(a, rw, g, lane);
+  const int t0 = span.lo, t1 = span.hi;
+  uint32_t words = tile_words(mg, klen, t0, lane);
+  if (t0 < t1) copy_tile(t0);
+  if (t0 + 1 < t1) copy_tile(t0 + 1);
+  u32x4 *box = lds + (S::NB * 2 * S::TILE - 4 * (kBox / 16)) + wave * (kBox / 16);
+  bf16x8 qf[NK];
+  if (r0 < rows) {
+#pragma unroll
+    for (int j = 0; j < qt.PARTS; ++j) {
+      qt.spread(box, j, lane);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) qf[4 * j + kk] = __builtin_bit_cast(bf16x8, qt.chunk(box, 2 * kk + h, lane));
+    }
+  }
+  Rows<ND> st;
+  st.init();
+  for (int t = t0; t < t1; ++t) {
+    const u32x4 *sk = lds + ((t - t0) % S::NB) * 2 * S::TILE, *sv = sk + S::TILE;
+    if (t > t0 && (t - t0) % 64 == 0) words = tile_words(mg, klen, t, lane);
+    const uint32_t word = (uint32_t)__builtin_amdgcn_readlane((int)words, (t - t0) % 64);
+    if (t + 1 < t1) wait_vm<2 * CP>();              // this tile's copies: the next one's are younger
+    else wait_vm<0>();
+    if (word != 0xFFFFFFFFu) {
+#pragma unroll
+      for (int i = 0; i < CP; ++i) {
+        const int r = RPC * (wave * CP + i) + lane / NCH;
+        if (!((word >> r) & 1)) ((u32x4 *)sv)[(wave * CP + i) * 64 + lane] = u32x4{0, 0, 0, 0};
+      }
+    }
+    __syncthreads();                                // the tile is whole, and the one before it read
+    if (t + 2 < t1) copy_tile(t + 2);
+    if (r0 < rows) {                                // wave-uniform
+      f32x16 s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk)
+        mfma32(s, __builtin_bit_cast(bf16x8, sk[lrow * NCH + key_swz<NCH>(lrow, 2 * kk + h)]), qf[kk]);
+      if (word != 0xFFFFFFFFu) mask_word(s, word);
+      const float ref = st.raise(max16(s, -INFINITY) * a.sc);
+      add_values<bf16, DP>(st.o, probs_of<bf16>(s, a.sc, ref, st.l), (const char *)sv, 0, lane);
+    }
+  }
+  if (r0 >= rows) return;
+  if (span.used > 1) {
+    store_part<ND>(a, st, 1.f, r0 + lrow < rows, tile, g, split, wave * 32 + lrow, lane);
+    return;
+  }
+  // all slots but the last tile's and the one before hold nothing that is still read
+  constexpr int ROOM = S::NB * 2 * S::TILE;
+  int mine = (t1 - t0) % S::NB * 2 * S::TILE + wave * (kBox / 16);
+  if (mine >= ROOM) mine -= ROOM;
+  store_tile<bf16, ND>(a, st, 1.f, rw, g, lds + mine, lane);
+}
+
 // ---- keys and values as e4m3 codes --------------------------------------------------------------
 //
 // Codes widen exactly: keys to bf16 (the queries' type: their range is bf16's), values to
-// fp16, and the probabilities, at most 2^8 here (an offset in the exponent that
+// fp16, and the probabilities, at most 2^15 here (an offset in the exponent that
 // keeps small ones out of fp16's subnormals), to fp16. fp32 queries are three bf16
 // terms (24 bits) and fp32 probabilities two fp16 terms (22 bits), so that the products
 // keep fp32's precision on the 16-bit matrix cores.
 // Block scales: the key scale multiplies the scores; the value scale, relative to the
 // largest one so far (`vref`, a power of two, wave-uniform), multiplies the
 // probabilities, and O is in units of vref.
-constexpr float kPOff = 8.f;
+constexpr float kPOff = 15.f - kSlack;
 
 template <typename T, int NK> struct QCodes {      // query operands: NQ bf16 terms
   static constexpr int NQ = sizeof(T) == 4 ? 3 : 1;
   bf16x8 f[NQ][NK];
-  // MFMA 2 j + u takes d = 32 j + 16 h + 8 u .. + 7 (the order of the key codes)
+  // MFMA kk = 2 j + u takes d = 32 j + 16 h + 8 u .. + 7 (the order of the key codes)
+  static __device__ __forceinline__ int d_of(int kk, int h) { return 32 * (kk >> 1) + 16 * h + 8 * (kk & 1); }
+  __device__ __forceinline__ void set(int kk, const u32x4 &x) { f[0][kk] = __builtin_bit_cast(bf16x8, x); }
+  __device__ __forceinline__ void set(int kk, const u32x4 &x0, const u32x4 &x1) {   // 8 floats
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = __uint_as_float(e < 4 ? x0[e & 3] : x1[e & 3]);
+      const bf16 a = (bf16)x;
+      const float ra = x - (float)a;
+      const bf16 b = (bf16)ra;
+      f[0][kk][e] = a;
+      f[1][kk][e] = b;
+      f[2][kk][e] = (bf16)(ra - (float)b);
+    }
+  }
   __device__ __forceinline__ void load(const T *row, bool live, int h) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
-      const int c = 32 * (kk >> 1) + 16 * h + 8 * (kk & 1);
-      if constexpr (sizeof(T) == 2) {
-        u32x4 x{0, 0, 0, 0};
-        if (live) x = *(const u32x4 *)(row + c);
-        f[0][kk] = __builtin_bit_cast(bf16x8, x);
-      } else {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if (live) {
-          const f32x4 x0 = *(const f32x4 *)(row + c), x1 = *(const f32x4 *)(row + c + 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { x[e] = x0[e]; x[4 + e] = x1[e]; }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bf16 a = (bf16)x[e];
-          const float ra = x[e] - (float)a;
-          const bf16 b = (bf16)ra;
-          f[0][kk][e] = a;
-          f[1][kk][e] = b;
-          f[2][kk][e] = (bf16)(ra - (float)b);
-        }
+      const int c = d_of(kk, h);
+      u32x4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
+      if (live) {
+        x = *(const u32x4 *)(row + c);
+        if constexpr (sizeof(T) == 4) y = *(const u32x4 *)(row + c + 4);
       }
+      if constexpr (sizeof(T) == 4) set(kk, x, y);
+      else set(kk, x);
     }
   }
 };
@@ -463,60 +793,115 @@ __device__ __forceinline__ u32x4 keep_tokens(u32x4 x, int left, int h) {
   return x;
 }
 
-// Softmax of one block's scores s (raw, masked) with key factor ksc, and O += V^T P^T.
-// vf(n, f): value operand of d block n, keys 16 f ..
-template <typename T, int ND, typename VF>
-__device__ __forceinline__ void kv8_update(Rows<ND> &st, float &vref, float &vinv, const f32x16 &s, float ksc,
-                                           float vsc, VF vf) {
-  float mb = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) mb = fmaxf(mb, s[i]);
-  mb = warp_max_xor(mb, 32) * ksc;
-  const float ref = st.raise(mb) - kPOff;
-  if (vsc > vref) {                                 // wave-uniform
-    st.scale(vref / vsc);                           // 0 at the first block, where O is 0
-    vref = vsc;
-    vinv = 1.f / vsc;
+// 1 KB of codes (a lane's 16) widened into a block's operand fragments in LDS: piece `sub` of the keys
+// (sub < NL) or values.
+template <int NL>
+__device__ __forceinline__ void widen_to(u32x4 *block, int sub, const u32x4 &x, int lane) {
+  u32x4 *to = block + 2 * sub * 64 + lane;
+  if (sub < NL) {
+    to[0] = __builtin_bit_cast(u32x4, widen_bf16(x[0], x[1]));
+    to[64] = __builtin_bit_cast(u32x4, widen_bf16(x[2], x[3]));
+  } else {
+    to[0] = __builtin_bit_cast(u32x4, widen_f16(x[0], x[1]));
+    to[64] = __builtin_bit_cast(u32x4, widen_f16(x[2], x[3]));
   }
-  const float ratio = vsc * vinv;
+}
+
+// Raw scores of one block from its key fragments in LDS (fr: this lane's).
+template <typename T, int NK>
+__device__ __forceinline__ void kv8_scores(f32x16 &s, const QCodes<T, NK> &q, const u32x4 *fr) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < NK; ++kk) {
+    const bf16x8 kf = __builtin_bit_cast(bf16x8, fr[kk * 64]);
+#pragma unroll
+    for (int t = QCodes<T, NK>::NQ - 1; t >= 0; --t) mfma32(s, kf, q.f[t][kk]);   // small terms first
+  }
+}
+
+// Probabilities of one block, p = 2^(ksc s - ref), as fp16 (fp32 calls: two terms), times `ratio`: the
+// block's value scale over vref, a power of two at most 1.
+template <typename T> struct CodeProbs { f16x8 f[2], lo[sizeof(T) == 4 ? 2 : 1]; };
+template <typename T>
+__device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, float ref, float ratio, float &l) {
   float p[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], ksc, -ref));
-    st.l += p[i];
-    p[i] *= ratio;
+    l += p[i];
   }
+  CodeProbs<T> o;
 #pragma unroll
   for (int f = 0; f < 2; ++f) {
-    f16x8 hi, lo;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      hi[e] = (f16)p[8 * f + e];
-      if constexpr (sizeof(T) == 4) lo[e] = (f16)(p[8 * f + e] - (float)hi[e]);
+      if constexpr (sizeof(T) == 4) {
+        const float x = p[8 * f + e] * ratio;
+        o.f[f][e] = (f16)x;
+        o.lo[f][e] = (f16)(x - (float)o.f[f][e]);
+      } else {
+        o.f[f][e] = (f16)p[8 * f + e];
+      }
     }
+    if constexpr (sizeof(T) == 2) {
+      const f16 rt = (f16)ratio;
+      o.f[f] *= f16x8{rt, rt, rt, rt, rt, rt, rt, rt};
+    }
+  }
+  return o;
+}
+// O += V^T P^T; vf(n, f): value operand of d block n, keys 16 f ..
+template <typename T, int ND, typename VF>
+__device__ __forceinline__ void code_values(f32x16 (&o)[ND], const CodeProbs<T> &p, VF vf) {
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
 #pragma unroll
     for (int n = 0; n < ND; ++n) {
       const f16x8 v = vf(n, f);
-      mfma32(st.o[n], v, hi);
-      if constexpr (sizeof(T) == 4) mfma32(st.o[n], v, lo);
+      mfma32(o[n], v, p.f[f]);
+      if constexpr (sizeof(T) == 4) mfma32(o[n], v, p.lo[f]);
     }
-  }
 }
 
-// What the rows of a tile see of a sequence.
-struct Seen { int kv, tile_hi, row_hi; };           // length; keys of the tile's last row, of this lane's row
-__device__ __forceinline__ Seen seen_of(const Kv8AttnArgs &a, const CondSeq &sq, int last_tok, int tok) {
+// The largest value scale so far: O is in its units.
+struct VRef {
+  float top = 0.f, inv = 0.f;
+  template <int ND> __device__ __forceinline__ float ratio(Rows<ND> &st, float vsc) {
+    if (vsc > top) {                                // wave-uniform
+      st.scale(top / vsc);                          // 0 at the first block, where O is 0
+      top = vsc;
+      inv = 1.f / vsc;
+    }
+    return vsc * inv;
+  }
+};
+
+// What the rows of a tile see of a sequence: its length; the keys of the tile's first and last row,
+// and of this lane's row.
+struct Seen { int kv, tile_lo, tile_hi, row_hi; };
+__device__ __forceinline__ Seen seen_of(const Kv8AttnArgs &a, const CondSeq &sq, int first_tok, int last_tok, int tok) {
   Seen v;
-  v.kv = min(max(a.c.kv_lens[sq.k0], 0), a.c.width * 32);
-  v.tile_hi = a.causal ? min(max(v.kv - sq.q_len + last_tok + 1, 0), v.kv) : v.kv;
-  v.row_hi = a.causal ? min(max(v.kv - sq.q_len + tok + 1, 0), v.kv) : v.kv;
+  v.kv = min(max(uniform_at(a.c.kv_lens, sq.k0), 0), a.c.width * 32);
+  const int before = v.kv - sq.q_len + 1;           // keys of token 0, causal
+  v.tile_lo = a.causal ? min(max(before + first_tok, 0), v.kv) : v.kv;
+  v.tile_hi = a.causal ? min(max(before + last_tok, 0), v.kv) : v.kv;
+  v.row_hi = a.causal ? min(max(before + tok, 0), v.kv) : v.kv;
   return v;
 }
 
-// Bits of the block's keys below `hi` (key 0 of the block at `at`).
-__device__ __forceinline__ uint32_t bits_below(int hi, int at) {
-  const int n = hi - at;
-  return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+// What scores of a block's key codes are multiplied by; never 0, so that a masked score stays -inf.
+__device__ __forceinline__ float key_factor(float ks, float sc) { return fmaxf(ks * sc, 0x1p-126f); }
+
+// A block of the pool, or none: its number times heads + g, and its scales (vs < 0: none).
+struct BlockRef { int64_t at; float ks, vs; };
+__device__ __forceinline__ BlockRef block_ref(const Kv8View &c, int id, int g) {
+  const bool ok = id >= 0 && id < c.n_blocks;
+  BlockRef b;
+  b.at = (int64_t)(ok ? id : 0) * c.hkv + g;
+  b.ks = uniform_at(c.scales, b.at * 2);
+  b.vs = ok ? uniform_at(c.scales, b.at * 2 + 1) : -1.f;
+  return b;
 }
 
 // Least blocks of a split: below that a partial result costs more than its keys.
@@ -531,42 +916,42 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
   extern __shared__ u32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
-  const int tile = blockIdx.x, g = blockIdx.y, split = blockIdx.z;
+  const Unit un = unit_of(a.hkv);
+  const int tile = un.tile, g = un.g, split = blockIdx.y;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int rows = sq.q_len * a.rep, r0 = (tile - sq.tile0) * 32, r = r0 + lrow;
   const bool live = r < rows;
   const int qi = live ? r / a.rep : 0;
   const int head = g * a.rep + (live ? r % a.rep : 0);
-  const Seen seen = seen_of(a, sq, (min(r0 + 32, rows) - 1) / a.rep, qi);
+  const Seen seen = seen_of(a, sq, r0 / a.rep, (min(r0 + 32, rows) - 1) / a.rep, qi);
   const Span span = split_span((seen.tile_hi + 31) >> 5, a.n_split, split, kRowsLeast);
   if (split >= span.used) return;
 
   const int32_t *tab = a.c.table + (int64_t)sq.k0 * a.c.table_row;
-  struct Block { u32x4 k[NL], v[NL]; float ks, vs; };
-  auto load = [&](int b, Block &x) {
-    const int id = __builtin_amdgcn_readfirstlane(tab[b]);
-    const bool ok = id >= 0 && id < a.c.n_blocks;
-    const int64_t at = (int64_t)(ok ? id : 0) * a.c.hkv + g;
-    const u32x4 *kp = (const u32x4 *)(a.c.k_codes + at * (32 * D)) + lane;
-    const u32x4 *vp = (const u32x4 *)(a.c.v_codes + at * (32 * D)) + lrow * 2 + h;
+  auto id_at = [&](int b) { return b < span.hi ? uniform_at(tab, b) : -1; };
+  struct Block { u32x4 k[NL], v[NL]; BlockRef ref; };
+  auto load = [&](int id, Block &x) {
+    x.ref = block_ref(a.c, id, g);
+    const u32x4 *kp = (const u32x4 *)(a.c.k_codes + x.ref.at * (32 * D)) + lane;
+    const u32x4 *vp = (const u32x4 *)(a.c.v_codes + x.ref.at * (32 * D)) + lrow * 2 + h;
 #pragma unroll
     for (int i = 0; i < NL; ++i) x.k[i] = kp[64 * i];
 #pragma unroll
     for (int i = 0; i < NL; ++i) x.v[i] = vp[64 * i];
-    x.ks = a.c.scales[at * 2];
-    x.vs = ok ? a.c.scales[at * 2 + 1] : -1.f;      // a block that is none
   };
   QCodes<T, NK> q;
   Rows<ND> st;
   st.init();
-  float vref = 0.f, vinv = 0.f;
+  VRef vr;
   Block cur, nxt;
   const int b0 = span.lo + wave;
-  if (b0 < span.hi) load(b0, cur);
+  int id = id_at(b0 + 4);
+  if (b0 < span.hi) load(id_at(b0), cur);
   q.load((const T *)a.q + (int64_t)(sq.q0 + qi) * a.q_row + (int64_t)head * a.q_head, live, h);
   for (int b = b0; b < span.hi; b += 4) {
-    if (b + 4 < span.hi) load(b + 4, nxt);
-    if (cur.vs > 0.f) {
+    if (b + 4 < span.hi) load(id, nxt);
+    id = id_at(b + 8);
+    if (cur.ref.vs > 0.f) {
       f32x16 s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
@@ -576,26 +961,28 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
 #pragma unroll
         for (int t = q.NQ - 1; t >= 0; --t) mfma32(s, kf, q.f[t][kk]);   // small terms first
       }
-      const int at = b * 32;
-      if (at + 32 > seen.kv || a.causal) {          // wave-uniform
-        mask_scores(s, bits_below(seen.row_hi, at), lane);
-        const int left = seen.kv - at;
+      const int left = seen.kv - b * 32;
+      if (left < 32 || b * 32 + 32 > seen.tile_lo) {  // wave-uniform
+        mask_below(s, seen.row_hi - b * 32, lane);
         if (left < 32) {
 #pragma unroll
           for (int i = 0; i < NL; ++i) cur.v[i] = keep_tokens(cur.v[i], left, h);
         }
       }
-      kv8_update<T, ND>(st, vref, vinv, s, cur.ks * a.sc, cur.vs,
-                        [&](int n, int f) { return widen_f16(cur.v[n][2 * f], cur.v[n][2 * f + 1]); });
+      const float ksc = key_factor(cur.ref.ks, a.sc);
+      const float ref = st.raise(max16(s, -INFINITY) * ksc) - kPOff;
+      const float ratio = vr.ratio(st, cur.ref.vs);
+      code_values<T, ND>(st.o, code_probs<T>(s, ksc, ref, ratio, st.l),
+                         [&](int n, int f) { return widen_f16(cur.v[n][2 * f], cur.v[n][2 * f + 1]); });
     }
     cur = nxt;
   }
   // the waves' O in one unit before they are joined
   float *red = (float *)lds;
-  if (lane == 0) red[wave] = vref;
+  if (lane == 0) red[wave] = vr.top;
   __syncthreads();
   const float top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  if (top > 0.f) st.scale(vref / top);
+  if (top > 0.f) st.scale(vr.top / top);
   __syncthreads();
   join_waves<ND, 4>(st, red, wave, lane);
   if (wave > 0) return;
@@ -616,41 +1003,31 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
   extern __shared__ u32x4 lds[];                    // [block][NK key + 2 ND value fragments][64 lanes]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
-  const int tile = blockIdx.x, g = blockIdx.y, split = blockIdx.z;
+  const Unit un = unit_of(a.hkv);
+  const int tile = un.tile, g = un.g, split = blockIdx.y;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int rows = sq.q_len * a.rep, t0 = (tile - sq.tile0) * 128, r0 = t0 + wave * 32, r = r0 + lrow;
   const bool live = r < rows;
   const int qi = live ? r / a.rep : 0;
   const int head = g * a.rep + (live ? r % a.rep : 0);
-  const Seen seen = seen_of(a, sq, (min(t0 + 128, rows) - 1) / a.rep, qi);
+  const Seen seen = seen_of(a, sq, min(r0, rows - 1) / a.rep, (min(t0 + 128, rows) - 1) / a.rep, qi);
   const Span span = split_span((seen.tile_hi + 31) >> 5, a.n_split, split, kTilesLeast);
   if (split >= span.used) return;
-  const int wave_hi = !a.causal ? seen.kv
-                                : min(max(seen.kv - sq.q_len + (min(r0 + 32, rows) - 1) / a.rep + 1, 0), seen.kv);
-  const int wave_lo = !a.causal ? seen.kv : min(max(seen.kv - sq.q_len + min(r0, rows - 1) / a.rep + 1, 0), seen.kv);
 
   const int32_t *tab = a.c.table + (int64_t)sq.k0 * a.c.table_row;
-  auto block_at = [&](int b, bool &ok) {
-    const int id = b < span.hi ? __builtin_amdgcn_readfirstlane(tab[b]) : -1;
-    ok = id >= 0 && id < a.c.n_blocks;
-    return (int64_t)(ok ? id : 0) * a.c.hkv + g;
-  };
+  auto id_at = [&](int b) { return b < span.hi ? uniform_at(tab, b) : -1; };
   u32x4 x[PPW];
-  auto gload = [&](int b) {
+  auto gload = [&](int b, const BlockRef (&ref)[2]) {
 #pragma unroll
     for (int i = 0; i < PPW; ++i) {
       const int p = wave * PPW + i, blk = p / (2 * NL), sub = p % (2 * NL);
-      bool ok;
-      const int64_t at = block_at(b + blk, ok);
-      x[i] = u32x4{0, 0, 0, 0};
-      if (ok) {
-        if (sub < NL) {
-          x[i] = ((const u32x4 *)(a.c.k_codes + at * (32 * D)))[64 * sub + lane];
-        } else {
-          x[i] = ((const u32x4 *)(a.c.v_codes + at * (32 * D)))[64 * (sub - NL) + lrow * 2 + h];
-          const int left = seen.kv - (b + blk) * 32;
-          if (left < 32) x[i] = keep_tokens(x[i], left, h);
-        }
+      const BlockRef &r = ref[blk];
+      if (sub < NL) {
+        x[i] = ((const u32x4 *)(a.c.k_codes + r.at * (32 * D)))[64 * sub + lane];
+      } else {
+        x[i] = ((const u32x4 *)(a.c.v_codes + r.at * (32 * D)))[64 * (sub - NL) + lrow * 2 + h];
+        const int left = seen.kv - (b + blk) * 32;
+        if (left < 32) x[i] = keep_tokens(x[i], left, h);
       }
     }
   };
@@ -658,55 +1035,175 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
 #pragma unroll
     for (int i = 0; i < PPW; ++i) {
       const int p = wave * PPW + i, blk = p / (2 * NL), sub = p % (2 * NL);
-      u32x4 *to = lds + (blk * 4 * NL + 2 * sub) * 64 + lane;
-      if (sub < NL) {
-        to[0] = __builtin_bit_cast(u32x4, widen_bf16(x[i][0], x[i][1]));
-        to[64] = __builtin_bit_cast(u32x4, widen_bf16(x[i][2], x[i][3]));
-      } else {
-        to[0] = __builtin_bit_cast(u32x4, widen_f16(x[i][0], x[i][1]));
-        to[64] = __builtin_bit_cast(u32x4, widen_f16(x[i][2], x[i][3]));
-      }
+      widen_to<NL>(lds + blk * 4 * NL * 64, sub, x[i], lane);
     }
   };
-  if (span.lo < span.hi) gload(span.lo);
+  BlockRef cur[2], nxt[2];
+  int id[2] = {id_at(span.lo + 2), id_at(span.lo + 3)};
+  if (span.lo < span.hi) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) cur[u] = block_ref(a.c, id_at(span.lo + u), g);
+    gload(span.lo, cur);
+  }
   QCodes<T, NK> q;
   q.load((const T *)a.q + (int64_t)(sq.q0 + qi) * a.q_row + (int64_t)head * a.q_head, live, h);
   Rows<ND> st;
   st.init();
-  float vref = 0.f, vinv = 0.f;
+  VRef vr;
   for (int b = span.lo; b < span.hi; b += 2) {
     __syncthreads();
     lstore();
     __syncthreads();
-    if (b + 2 < span.hi) gload(b + 2);
-    if (r0 >= rows) continue;                       // wave-uniform: it still loads and meets the barriers
+    if (b + 2 < span.hi) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int at = (b + u) * 32;
-      bool ok;
-      const int64_t blk = block_at(b + u, ok);
-      if (!ok || at >= wave_hi) continue;
-      const u32x4 *fr = lds + u * 4 * NL * 64 + lane;
-      f32x16 s;
+      for (int u = 0; u < 2; ++u) nxt[u] = block_ref(a.c, id[u], g);
+      gload(b + 2, nxt);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, fr[kk * 64]);
-#pragma unroll
-        for (int t = q.NQ - 1; t >= 0; --t) mfma32(s, kf, q.f[t][kk]);
-      }
-      if (at + 32 > wave_lo) mask_scores(s, bits_below(seen.row_hi, at), lane);
-      kv8_update<T, ND>(st, vref, vinv, s, a.c.scales[blk * 2] * a.sc, a.c.scales[blk * 2 + 1], [&](int n, int f) {
-        return __builtin_bit_cast(f16x8, fr[(NK + 2 * n + f) * 64]);
-      });
+      for (int u = 0; u < 2; ++u) id[u] = id_at(b + 4 + u);
     }
+    if (r0 < rows) {                                // wave-uniform: others still load and meet the barriers
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (cur[u].vs > 0.f) {
+          const u32x4 *fr = lds + u * 4 * NL * 64 + lane;
+          f32x16 s;
+          kv8_scores<T, NK>(s, q, fr);
+          if ((b + u) * 32 + 32 > seen.tile_lo) mask_below(s, seen.row_hi - (b + u) * 32, lane);
+          const float ksc = key_factor(cur[u].ks, a.sc);
+          const float ref = st.raise(max16(s, -INFINITY) * ksc) - kPOff;
+          const float ratio = vr.ratio(st, cur[u].vs);
+          code_values<T, ND>(st.o, code_probs<T>(s, ksc, ref, ratio, st.l),
+                             [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(NK + 2 * n + f) * 64]); });
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) cur[u] = nxt[u];
   }
   if (r0 >= rows) return;
   if (span.used == 1)
-    store_rows<T, ND>(a, st, vref, live, sq.q0 + qi, head, lane);
+    store_rows<T, ND>(a, st, vr.top, live, sq.q0 + qi, head, lane);
   else
-    store_part<ND>(a, st, vref, live, tile, g, split, wave * 32 + lrow, lane);
+    store_part<ND>(a, st, vr.top, live, tile, g, split, wave * 32 + lrow, lane);
+}
+
+// Many rows over a cache that fits LDS whole once widened: the counterpart of k_cross_res. Lane j holds
+// block j's scales and how many of its tokens count (none: no such block).
+template <typename T, int D, int NW, bool BOX>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void k_kv8_res(Kv8AttnArgs a, int chunk) {
+  constexpr int ND = D / 32, NK = D / 16, NL = D / 32, NF = D / 8;
+  extern __shared__ u32x4 lds[];                    // [block][NK key + 2 ND value fragments][64 lanes]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lrow = lane & 31, h = lane >> 5;
+  const Unit un = unit_of(a.hkv);
+  const int tile = un.tile, g = un.g;
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
+  const int first = (tile - sq.tile0) * chunk;
+  const int rows = min(sq.q_len * a.rep, first + chunk);
+  const Seen all = seen_of(a, sq, 0, (rows - 1) / a.rep, 0);
+  const int nk = (all.tile_hi + 31) >> 5;
+  const int32_t *tab = a.c.table + (int64_t)sq.k0 * a.c.table_row;
+  u32x4 *box = lds + wave * (kBox / 16);
+  u32x4 *codes = lds + (BOX ? NW * (kBox / 16) : 0);
+
+  struct Own { QCodes<T, NK> f; int64_t tok; int head; bool live; };
+  auto load_own = [&](int r0, Own &q) {
+    const int r = r0 + lrow;
+    q.live = r < rows;
+    const int t = q.live ? r / a.rep : 0;
+    q.tok = sq.q0 + t;
+    q.head = g * a.rep + (q.live ? r - t * a.rep : 0);
+    q.f.load((const T *)a.q + q.tok * a.q_row + (int64_t)q.head * a.q_head, q.live, h);
+  };
+  Own q, qn;
+  QTile<T, D> qt;
+  int r0 = first + wave * 32;
+  if (r0 < rows) {
+    if constexpr (BOX) qt.load(a, TileRows(a, sq, r0, rows), g, lane);
+    else load_own(r0, q);
+  }
+
+  float ks = 1.f, vs = 0.f;
+  int count = 0;
+  if (lane < nk) {
+    const int id = tab[lane];
+    if (id >= 0 && id < a.c.n_blocks) {
+      const int64_t at = (int64_t)id * a.c.hkv + g;
+      ks = key_factor(a.c.scales[at * 2], a.sc);
+      vs = a.c.scales[at * 2 + 1];
+      count = min(all.kv - lane * 32, 32);
+    }
+  }
+  float vref = vs;
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) vref = warp_max_xor(vref, m);
+  const float ratio = vs > 0.f ? vs / vref : 0.f;
+  for (int j = wave; j < nk; j += NW) {
+    const int id = uniform_at(tab, j);
+    const bool ok = id >= 0 && id < a.c.n_blocks;
+    const int64_t at = (int64_t)(ok ? id : 0) * a.c.hkv + g;
+    const int left = ok ? all.kv - j * 32 : 0;
+    u32x4 x[2 * NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      x[i] = ((const u32x4 *)(a.c.k_codes + at * (32 * D)))[64 * i + lane];
+      x[NL + i] = ((const u32x4 *)(a.c.v_codes + at * (32 * D)))[64 * i + lrow * 2 + h];
+    }
+    if (left < 32) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) x[NL + i] = keep_tokens(x[NL + i], left, h);
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * NL; ++i) widen_to<NL>(codes + j * NF * 64, i, x[i], lane);
+  }
+  __syncthreads();
+  for (; r0 < rows; r0 += NW * 32) {                // wave-uniform
+    const bool more = r0 + NW * 32 < rows;
+    const int r = min(r0 + lrow, rows - 1);
+    if constexpr (BOX) {
+#pragma unroll
+      for (int j = 0; j < qt.PARTS; ++j) {
+        qt.spread(box, j, lane);
+        if constexpr (sizeof(T) == 4) {             // a part of 32 floats: two steps of 16
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            q.f.set(2 * j + u, qt.chunk(box, 4 * h + 2 * u, lane), qt.chunk(box, 4 * h + 2 * u + 1, lane));
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) q.f.set(4 * j + u, qt.chunk(box, 4 * (u >> 1) + 2 * h + (u & 1), lane));
+        }
+      }
+      if (more) qt.load(a, TileRows(a, sq, r0 + NW * 32, rows), g, lane);
+    } else if (sizeof(T) == 2 && more) {
+      load_own(r0 + NW * 32, qn);
+    }
+    const Seen seen = seen_of(a, sq, r0 / a.rep, (min(r0 + 32, rows) - 1) / a.rep, r / a.rep);
+    Rows<ND> st;
+    st.init();
+    auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+    attend_steps<ND, CodeProbs<T>>(
+        st, (seen.tile_hi + 31) >> 5,
+        [&](int i, f32x16 &s) { kv8_scores<T, NK>(s, q.f, codes + i * NF * 64 + lane); },
+        [&](int i, f32x16 &s) {
+          const int n = __builtin_amdgcn_readlane(count, i), at = i * 32;
+          if (n < 32 || at + 32 > seen.tile_lo) mask_below(s, min(seen.row_hi - at, n), lane);
+        },
+        [&](int i) { return lane_of(ks, i); },
+        [&](int i, const f32x16 &s, float ref) {
+          return code_probs<T>(s, lane_of(ks, i), ref - kPOff, lane_of(ratio, i), st.l);
+        },
+        [&](int i, const CodeProbs<T> &p) {
+          const u32x4 *fr = codes + (i * NF + NK) * 64 + lane;
+          code_values<T, ND>(st.o, p, [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(2 * n + f) * 64]); });
+        });
+    if constexpr (BOX) {
+      store_tile<T, ND>(a, st, vref, TileRows(a, sq, r0, rows), g, box, lane);
+    } else {
+      store_rows<T, ND>(a, st, vref, q.live, q.tok, q.head, lane);
+      if (sizeof(T) == 2) q = qn;
+      else if (more) load_own(r0 + NW * 32, q);
+    }
+  }
 }
 
 // ---- joining splits -----------------------------------------------------------------------------
@@ -717,7 +1214,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
 template <typename T, int DP, typename A, typename SPAN>
 __device__ __forceinline__ void join_body(const A &a, int TR, SPAN used_of) {
   constexpr int LPR = DP / 4;
-  const int tile = blockIdx.x, g = blockIdx.y;
+  const Unit un = unit_of(a.hkv);
+  const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int rows = sq.q_len * a.rep, r0 = (tile - sq.tile0) * TR;
   const int used = used_of(sq, (min(r0 + TR, rows) - 1) / a.rep);
@@ -752,16 +1250,16 @@ __device__ __forceinline__ void join_body(const A &a, int TR, SPAN used_of) {
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void k_cross_join(CrossArgs a, int TR, int KT) {
+__global__ __launch_bounds__(kThreads) void k_cross_join(CrossArgs a, int TR, int KT, int least) {
   join_body<T, DP>(a, TR, [&](const CondSeq &sq, int) {
-    return split_span((sq.k_len + KT - 1) / KT, a.n_split, 0, 1).used;
+    return split_span((sq.k_len + KT - 1) / KT, a.n_split, 0, least).used;
   });
 }
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads) void k_kv8_join(Kv8AttnArgs a, int TR, int least) {
   join_body<T, DP>(a, TR, [&](const CondSeq &sq, int last_tok) {
-    return split_span((seen_of(a, sq, last_tok, 0).tile_hi + 31) >> 5, a.n_split, 0, least).used;
+    return split_span((seen_of(a, sq, 0, last_tok, 0).tile_hi + 31) >> 5, a.n_split, 0, least).used;
   });
 }
 
@@ -771,7 +1269,11 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // How a class of query sequences is launched: TR rows a tile, the same number of splits for all.
 struct Plan {
-  int TR = 0, n_split = 1, ws_rows = 0;
+  enum { FEW, COPIES, STREAM, RESIDENT } kind = FEW;
+  int TR = 0, KT = 0, n_split = 1, ws_rows = 0;
+  int least = 0;                                    // key tiles of a split
+  int nw = 4, lds = 0;                              // RESIDENT: waves, LDS bytes,
+  bool box = false;                                 // and whether they hold kBox a wave
   int64_t tiles = 0;                                // of the launch (of kCondSeqs sequences) with the most
   int64_t floats(int hkv, int dp) const {
     return n_split > 1 ? tiles * hkv * n_split * (int64_t)ws_rows * (dp + 2) : 0;
@@ -786,40 +1288,84 @@ constexpr int kFill = 512;
 
 }  // namespace
 
-// Rows mode by the longest query sequence: up to 32 rows the four waves of a workgroup share
-// them and split the keys.
-static Plan cross_plan(const AttnProblem &p, const int32_t *kv_lens, const int32_t *kv_index, int &rw, int &KT) {
-  Plan pl;
-  int64_t most = 0;
-  int kmax = 0;
+// Row tiles of 32 and the most rows of one query sequence among those that `take` accepts.
+template <typename TAKE>
+static void count_rows(const AttnProblem &p, int64_t &tiles, int64_t &most, TAKE take) {
+  tiles = most = 0;
   for (int i = 0; i < p.n; ++i) {
-    most = std::max<int64_t>(most, (int64_t)p.q_lens[i] * p.c.rep);
-    if (p.q_lens[i] > 0) kmax = std::max(kmax, kv_lens[kv_index ? kv_index[i] : i]);
+    const int64_t rows = (int64_t)p.q_lens[i] * p.c.rep;
+    if (rows == 0 || !take(i)) continue;
+    tiles += ceil_div(rows, 32);
+    most = std::max(most, rows);
   }
-  rw = most <= 32 ? 1 : 4;
-  KT = rw == 1 ? 128 : p.dtype == MTE_BF16 ? 64 : 32;
-  pl.TR = 32 * rw;
-  pl.ws_rows = (int)std::min<int64_t>(pl.TR, most);
-  int64_t all = 0;
-  for (int i = 0, in = 0, at = 0; i < p.n; ++i) {
-    if (p.q_lens[i] == 0) continue;
-    const int t = ceil_div((int64_t)p.q_lens[i] * p.c.rep, pl.TR);
+}
+
+// Tiles of TR rows: of the launch (of kCondSeqs sequences) with the most, and of all.
+template <typename TAKE>
+static int64_t fill_tiles(const AttnProblem &p, Plan &pl, TAKE take) {
+  int64_t all = 0, at = 0;
+  int in = 0;
+  pl.tiles = 0;
+  for (int i = 0; i < p.n; ++i) {
+    const int64_t rows = (int64_t)p.q_lens[i] * p.c.rep;
+    if (rows == 0 || !take(i)) continue;
+    const int t = ceil_div(rows, pl.TR);
     all += t;
     at += t;
-    pl.tiles = std::max<int64_t>(pl.tiles, at);
+    pl.tiles = std::max(pl.tiles, at);
     if (++in == kCondSeqs) in = at = 0;
   }
-  if (all == 0) return pl;
-  // a split of at least 4 key tiles
-  const int64_t units = all * p.c.hkv;
-  if (units < kFill) pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / units, ceil_div(kmax, KT) / 4));
+  return all;
+}
+
+// The kernel and its splits:
+//  FEW: up to 32 rows a sequence, or fewer than 256 tiles of 32 rows in all: a workgroup per tile, its four
+//    waves split the keys (1871 fp32 rows over up to 320 keys: 15 us, against 24 with tiles of 128
+//    rows; 1024 bf16 rows of 10 heads, 320 tiles, over 96: 6.5, against 5.6).
+//  COPIES (bf16): tiles of 128 rows, keys by LDS-direct copies.
+//  STREAM (fp32, or rows too far apart for 32-bit offsets): tiles of 128 rows, keys by registers.
+// Launches of fewer than kFill workgroups split long key ranges.
+static Plan cross_plan(const AttnProblem &p, const int32_t *kv_lens, const int32_t *kv_index) {
+  Plan pl;
+  int64_t row_tiles, most;
+  const auto any = [](int) { return true; };
+  count_rows(p, row_tiles, most, any);
+  if (row_tiles == 0) return pl;
+  int kmax = 0;
+  for (int i = 0; i < p.n; ++i)
+    if (p.q_lens[i] > 0) kmax = std::max(kmax, kv_lens[kv_index ? kv_index[i] : i]);
+  pl.TR = 128;
+  if (most <= 32 || row_tiles * p.c.hkv < 256) {
+    pl.kind = Plan::FEW;
+    pl.TR = 32;
+    pl.KT = 128;
+    pl.least = 1;
+  } else if (p.dtype == MTE_BF16 && p.near_rows) {
+    pl.kind = Plan::COPIES;
+    pl.KT = 32;
+    pl.least = kStreamLeast;
+  } else {
+    pl.kind = Plan::STREAM;
+    pl.KT = p.dtype == MTE_BF16 ? 64 : 32;
+    pl.least = 1;
+  }
+  const int64_t units = fill_tiles(p, pl, any) * p.c.hkv;
+  const int tiles = std::max(4, 2 * pl.least);       // of keys, for each further split
+  if (units < kFill) pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / units, ceil_div(kmax, pl.KT) / tiles));
+  pl.ws_rows = (int)std::min<int64_t>(pl.TR, most);
   return pl;
 }
 
+// Whether the rows written are more than the caches in front of memory keep until they are read again
+// (32 MB of L2): such stores bypass them. 16 x 4096 rows of 10 heads of 64: 46.2 us against 51.3.
+static int big_out(const AttnProblem &p) {
+  int64_t rows = 0;
+  for (int i = 0; i < p.n; ++i) rows += p.q_lens[i];
+  return rows * p.c.rep * p.c.hkv * p.c.d * (p.dtype == MTE_BF16 ? 2 : 4) > (32 << 20);
+}
+
 int64_t cross_workspace(const AttnProblem &p, const int32_t *kv_lens, int, const int32_t *kv_index) {
-  int rw, KT;
-  const Plan pl = cross_plan(p, kv_lens, kv_index, rw, KT);
-  return pl.floats(p.c.hkv, pad_d(p.c.d)) * 4;
+  return cross_plan(p, kv_lens, kv_index).floats(p.c.hkv, pad_d(p.c.d)) * 4;
 }
 
 // Fills a.seq with the next query sequences that `take` accepts (up to kCondSeqs); returns their tiles.
@@ -847,26 +1393,35 @@ static hipError_t allow_lds(K kern, int bytes) {
                         : hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
-template <typename T, int DP, int RW>
-static hipError_t run_cross(const CrossArgs &a, int tiles, int TR, int KT, hipStream_t s) {
-  const int lds = std::max(2 * KT * DP * (int)sizeof(T) + 32, RW == 4 ? 0 : 3 * (2 + DP / 2) * 64 * 4);
-  auto kern = k_cross<T, DP, RW>;
-  hipError_t e = allow_lds(kern, lds);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(tiles, a.hkv, a.n_split), dim3(kThreads), lds, s, a);
+template <typename T, int DP>
+static hipError_t run_cross(const CrossArgs &a, int tiles, const Plan &pl, hipStream_t s) {
+  const dim3 grid(tiles * a.hkv, a.n_split);
+  hipError_t e;
+  auto kern = pl.kind == Plan::FEW ? k_cross<T, DP, 1> : k_cross<T, DP, 4>;
+  int lds = 2 * pl.KT * DP * (int)sizeof(T) + 32;
+  if (pl.kind == Plan::FEW) lds = std::max(lds, 3 * (2 + DP / 2) * 64 * 4);
+  if constexpr (sizeof(T) == 2) {
+    if (pl.kind == Plan::COPIES) {
+      kern = k_cross_stream<DP>;
+      lds = Stream<DP>::BYTES;
+    }
+  }
+  if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, grid, dim3(kThreads), lds, s, a);
   if ((e = hipGetLastError()) != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL((k_cross_join<T, DP>), dim3(tiles, a.hkv), dim3(kThreads), 0, s, a, TR, KT);
+  hipLaunchKernelGGL((k_cross_join<T, DP>), dim3(tiles * a.hkv), dim3(kThreads), 0, s, a, pl.TR, pl.KT,
+                     pl.least);
   return hipGetLastError();
 }
 
 hipError_t launch_cross(const AttnProblem &p, const void *k, const void *v, const uint8_t *mask, int64_t k_row,
                         int64_t k_head, int64_t v_row, int64_t v_head, const int32_t *kv_lens, int n_kv,
                         const int32_t *kv_index, hipStream_t s) {
-  int rw, KT;
-  const Plan pl = cross_plan(p, kv_lens, kv_index, rw, KT);
+  const Plan pl = cross_plan(p, kv_lens, kv_index);
   const int dp = pad_d(p.c.d);
   CrossArgs a;
   (AttnCommon &)a = p.c;
+  a.big = big_out(p);
   a.k = k;
   a.v = v;
   a.mask = mask;
@@ -893,39 +1448,59 @@ hipError_t launch_cross(const AttnProblem &p, const void *k, const void *v, cons
     const int tiles = next_seqs(a, p, i, row, pl.TR, take);
     if (tiles == 0) continue;
     hipError_t e;
-    if (p.dtype == MTE_BF16) {
-      if (dp == 64) e = rw == 1 ? run_cross<bf16, 64, 1>(a, tiles, pl.TR, KT, s) : run_cross<bf16, 64, 4>(a, tiles, pl.TR, KT, s);
-      else e = rw == 1 ? run_cross<bf16, 128, 1>(a, tiles, pl.TR, KT, s) : run_cross<bf16, 128, 4>(a, tiles, pl.TR, KT, s);
-    } else {
-      if (dp == 64) e = rw == 1 ? run_cross<float, 64, 1>(a, tiles, pl.TR, KT, s) : run_cross<float, 64, 4>(a, tiles, pl.TR, KT, s);
-      else e = rw == 1 ? run_cross<float, 128, 1>(a, tiles, pl.TR, KT, s) : run_cross<float, 128, 4>(a, tiles, pl.TR, KT, s);
-    }
+    if (p.dtype == MTE_BF16)
+      e = dp == 64 ? run_cross<bf16, 64>(a, tiles, pl, s) : run_cross<bf16, 128>(a, tiles, pl, s);
+    else
+      e = dp == 64 ? run_cross<float, 64>(a, tiles, pl, s) : run_cross<float, 128>(a, tiles, pl, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-// Query sequences of up to 32 rows stream the codes (few), longer ones stage them (many); a call
-// with both takes both kernels. The workspace serves one after the other.
+// Query sequences of up to 32 rows stream the codes (few), longer ones stage them (many), whole where
+// the table is no wider than LDS; a call with both takes both kernels. The workspace serves
+// one after the other.
+constexpr int kLds = 160 * 1024;                     // of a compute unit
+static bool few_rows(const AttnProblem &p, int i) { return (int64_t)p.q_lens[i] * p.c.rep <= 32; }
 static Plan kv8_plan(const AttnProblem &p, int width, bool few) {
   Plan pl;
-  pl.TR = few ? 32 : 128;
-  int64_t all = 0, most = 0;
-  for (int i = 0, in = 0, at = 0; i < p.n; ++i) {
-    const int64_t rows = (int64_t)p.q_lens[i] * p.c.rep;
-    if (rows == 0 || (rows <= 32) != few) continue;
-    const int t = ceil_div(rows, pl.TR);
-    most = std::max(most, rows);
-    all += t;
-    at += t;
-    pl.tiles = std::max<int64_t>(pl.tiles, at);
-    if (++in == kCondSeqs) in = at = 0;
+  int64_t row_tiles, most;
+  const auto mine = [&](int i) { return few_rows(p, i) == few; };
+  count_rows(p, row_tiles, most, mine);
+  if (row_tiles == 0) return pl;
+  const int64_t res = (int64_t)width * 32 * p.c.d * 4;
+  if (few) {
+    pl.TR = 32;
+  } else if (res <= kLds) {
+    // LDS is shared by two and more workgroups of four waves where that leaves each half of it, else
+    // eight waves have it to themselves; rows are turned in LDS where there is room (bf16: fp32 is
+    // bound by its products, and has no registers to spare).
+    const int room = p.dtype == MTE_BF16 ? kBox : 0, simd = p.dtype != MTE_BF16 ? 1 : p.c.d == 64 ? 3 : 2;
+    pl.kind = Plan::RESIDENT;
+    pl.nw = res + 4 * room <= kLds / 2 ? 4 : 8;
+    pl.box = room > 0 && res + pl.nw * room <= kLds;
+    pl.lds = (int)res + (pl.box ? pl.nw * room : 0);
+    // Row tiles a wave takes one after the other: the keys are staged once for all of them. Whole
+    // rounds of the workgroups that the chip holds, a staging at the cost of a tile (16 x 1024
+    // queries over 320 tokens: 4 tiles in one round 61.5 us, 2 in two rounds 67).
+    const int64_t slots = 256 * std::max(1, std::min(kLds / pl.lds, 4 * simd / pl.nw));
+    int64_t best = INT64_MAX;
+    int iters = 1;
+    for (int i = 1; i <= 16; ++i) {
+      pl.TR = 32 * pl.nw * i;
+      const int64_t cost = (fill_tiles(p, pl, mine) * p.c.hkv + slots - 1) / slots * (i + 1);
+      if (cost < best) { best = cost; iters = i; }
+    }
+    pl.TR = 32 * pl.nw * iters;
+  } else {
+    pl.kind = Plan::STREAM;
+    pl.TR = 128;
   }
-  if (all == 0) return pl;
+  const int64_t units = fill_tiles(p, pl, mine) * p.c.hkv;
+  if (pl.kind == Plan::RESIDENT) return pl;
   pl.ws_rows = (int)std::min<int64_t>(pl.TR, most);
-  const int64_t units = all * p.c.hkv;
   if (few)
-    pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(4096 / units, ceil_div(width, 2 * kRowsLeast)));
+    pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / units, ceil_div(width, 2 * kRowsLeast)));
   else if (units < kFill)
     pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / units, ceil_div(width, 2 * kTilesLeast)));
   return pl;
@@ -936,18 +1511,23 @@ int64_t kv8_workspace(const AttnProblem &p, int width) {
 }
 
 template <typename T, int D>
-static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, bool few, hipStream_t s) {
-  const dim3 grid(tiles, a.hkv, a.n_split);
+static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, const Plan &pl, hipStream_t s) {
+  const dim3 grid(tiles * a.hkv, a.n_split);
   hipError_t e;
-  if (few) {
-    const int lds = 3 * (2 + D / 2) * 64 * 4;
-    hipLaunchKernelGGL((k_kv8_rows<T, D>), grid, dim3(kThreads), lds, s, a);
-  } else {
-    const int lds = 2 * 4 * (D / 32) * 64 * 16;
-    hipLaunchKernelGGL((k_kv8_tiles<T, D>), grid, dim3(kThreads), lds, s, a);
+  if (pl.kind == Plan::RESIDENT) {
+    constexpr bool B16 = sizeof(T) == 2;
+    auto kern = pl.nw == 4 ? k_kv8_res<T, D, 4, B16> : pl.box ? k_kv8_res<T, D, 8, B16> : k_kv8_res<T, D, 8, false>;
+    if ((e = allow_lds(kern, pl.lds)) != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, grid, dim3(64 * pl.nw), pl.lds, s, a, pl.TR);
+    return hipGetLastError();
   }
+  const bool few = pl.kind == Plan::FEW;
+  if (few)
+    hipLaunchKernelGGL((k_kv8_rows<T, D>), grid, dim3(kThreads), 3 * (2 + D / 2) * 64 * 4, s, a);
+  else
+    hipLaunchKernelGGL((k_kv8_tiles<T, D>), grid, dim3(kThreads), 2 * 4 * (D / 32) * 64 * 16, s, a);
   if ((e = hipGetLastError()) != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL((k_kv8_join<T, D>), dim3(tiles, a.hkv), dim3(kThreads), 0, s, a, few ? 32 : 128,
+  hipLaunchKernelGGL((k_kv8_join<T, D>), dim3(tiles * a.hkv), dim3(kThreads), 0, s, a, pl.TR,
                      few ? kRowsLeast : kTilesLeast);
   return hipGetLastError();
 }
@@ -958,6 +1538,7 @@ hipError_t launch_kv8_attention(const AttnProblem &p, const Kv8View &c, int caus
     if (pl.tiles == 0) continue;
     Kv8AttnArgs a;
     (AttnCommon &)a = p.c;
+    a.big = big_out(p);
     a.c = c;
     a.causal = causal;
     a.n_split = pl.n_split;
@@ -966,16 +1547,16 @@ hipError_t launch_kv8_attention(const AttnProblem &p, const Kv8View &c, int caus
     auto take = [&](int i, CondSeq &sq) {
       sq.k0 = i;
       sq.k_len = 0;
-      return ((int64_t)p.q_lens[i] * a.rep <= 32) == few;
+      return few_rows(p, i) == few;
     };
     for (int i = 0, row = 0; i < p.n;) {
       const int tiles = next_seqs(a, p, i, row, pl.TR, take);
       if (tiles == 0) continue;
       hipError_t e;
       if (p.dtype == MTE_BF16)
-        e = c.d == 64 ? run_kv8<bf16, 64>(a, tiles, few, s) : run_kv8<bf16, 128>(a, tiles, few, s);
+        e = c.d == 64 ? run_kv8<bf16, 64>(a, tiles, pl, s) : run_kv8<bf16, 128>(a, tiles, pl, s);
       else
-        e = c.d == 64 ? run_kv8<float, 64>(a, tiles, few, s) : run_kv8<float, 128>(a, tiles, few, s);
+        e = c.d == 64 ? run_kv8<float, 64>(a, tiles, pl, s) : run_kv8<float, 128>(a, tiles, pl, s);
       if (e != hipSuccess) return e;
     }
   }

@@ -27,6 +27,7 @@ struct AttnCommon {
   int d, hkv, rep;
   int n_seq, n_split, ws_rows;       // ws_rows: rows of a tile's partial result
   int64_t ws_ml;                     // float offset of the (m, l) pairs in ws
+  int big;                           // out is more than the caches hold
 };
 
 struct CrossArgs : AttnCommon {
@@ -63,6 +64,7 @@ struct Kv8RowsArgs {                 // append and read
 struct AttnProblem {
   AttnCommon c;
   int dtype;                         // MTE_F32 / MTE_BF16
+  bool near_rows;                    // key and value rows under 2^24 elements apart: 32 of them are 32-bit offsets
   const int32_t *q_lens;
   int n;
 };

@@ -92,6 +92,10 @@ CROSS = [
     ([2], [2500], 8, 2, 64),                     # a long range of keys, few rows: split and joined
     ([1], [5000], 16, 8, 128), ([130], [1500], 2, 2, 128),
     ([8, 8], [1000, 3], 2, 2, 64),               # a split plan of which one sequence uses one part
+    # enough rows for the tiles of 128: ends inside tiles, no keys, one key, padded heads, groups
+    ([2100, 33], [96, 70], 8, 8, 64), ([1030], [320], 16, 8, 128), ([700, 1, 0, 900], [33, 0, 5, 1], 12, 4, 40),
+    ([1500, 129], [65, 31], 6, 6, 72), ([4099], [64], 4, 2, 128),
+    ([600], [2500], 16, 16, 64), ([520, 3], [1200, 9], 16, 16, 128),   # and split
 ]
 
 
@@ -110,7 +114,8 @@ def test_cross_attention(torch, C, ql, kl, hq, hkv, d, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("ql,kl,hq,hkv,d", [([3, 40, 1], [96, 70, 33], 4, 2, 64), ([1, 1], [200, 31], 16, 8, 128),
-                                            ([200], [130], 2, 2, 128), ([1], [3000], 4, 4, 64)])
+                                            ([200], [130], 2, 2, 128), ([1], [3000], 4, 4, 64),
+                                            ([1100, 40], [96, 70], 16, 8, 128), ([600], [2500], 16, 16, 64)])
 def test_cross_attention_mask(torch, C, ql, kl, hq, hkv, d, dtype):
     """Masked tokens hold infinities and NaN; one sequence is masked whole."""
     _say(f"masked cross {ql} x {kl} {dtype}")
