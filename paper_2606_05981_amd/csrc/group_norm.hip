@@ -2,14 +2,22 @@
 //   y = act((x - mean) / sqrt(var + eps) * gamma[c] + beta[c])
 // over the pixels and the cpg = C / G channels of a group of one image.
 //
-// A workgroup holds a slab of an image in registers -- a bundle of whole groups
-// (neighbouring channels, so that rows are read in runs) times a chunk of pixels; a
-// thread keeps one column of V channels and walks the pixels. Sums go through LDS
-// per group, twice: the mean first, then the squares around it, so that a large mean
-// cancels nowhere. Where the slab is a whole image the same workgroup
-// normalises it from its registers: x is read once, y written once, one launch. Else
-// the chunks leave (mean, squares) in the workspace and a second launch joins them by
-// their counts and normalises. Bound by those bytes.
+// A thread keeps one column of V channels and walks pixels; sums go through LDS per group, twice:
+// the mean first, then the squares around it, so that a large mean cancels nowhere. Two shapes:
+//
+// k_gn, one launch: a workgroup holds a bundle of whole groups (neighbouring channels, so that rows
+// are read in runs) of a whole image in LDS. x is read once, y written once.
+//
+// k_gn_stats + k_gn_apply, where an image does not fit or its workgroups would be too few:
+// workgroups take chunks of pixels over as many groups as they have columns for. A thread runs
+// (count, mean, squares around it) per channel over batches of pixels, the workgroup joins its
+// threads' and leaves (count, mean, squares) of the part in the workspace; the second launch
+// joins the parts while its pixels load. x is read twice, the second time mostly from the caches.
+//
+// Large images are bound by those bytes, small ones by the chain of a launch: loads, two sums
+// through LDS, stores. That chain's code runs once per workgroup, so it is kept short: held
+// in registers and unrolled (16 vectors a thread), the same 8x8x1280 image took 9.1 us, most of it
+// fetching instructions.
 #include <algorithm>
 
 #include "../../include/mte_cond.h"
@@ -26,14 +34,15 @@ template <> struct Raw<8> { typedef u32x2 type; };
 template <> struct Raw<4> { typedef uint32_t type; };
 template <> struct Raw<2> { typedef uint16_t type; };
 
-// Vectors a thread holds: 64 registers of 16-byte or 8-byte ones, 32 of shorter ones.
-constexpr int hold_of(int bytes) { return bytes == 16 ? 16 : 32; }
+constexpr int kBatch = 4;      // vectors of a thread in flight at a time
 
 struct GnArgs : GroupNormArgs {
   int cpg, gb;         // channels per group, groups per bundle
   int ncol;            // columns (of V channels) of a bundle
   int ppi;             // pixels a workgroup takes at a time
-  int chunk;           // pixels per chunk
+  int chunk;           // pixels per workgroup: of k_gn_stats,
+  int apply;           // of k_gn_apply
+  int parts;           // of k_gn_stats: chunks x column parts
   int colparts;        // a bundle wider than a workgroup (then one group): its parts
   int same;            // a column lies inside one group
 };
@@ -57,51 +66,87 @@ template <typename T, int V> struct Vec {
   }
 };
 
-// Sums `v` (per thread and channel of its column) over each group of the bundle: the sum of
-// group i is gs[i * wpg] + .. + gs[i * wpg + wpg - 1] afterwards.
+// Where a thread works: its column, pixel lane and first channel.
+struct Place { int col0, ncol, g0, col, p0, ch; bool on; };
+template <int V, int TH> __device__ __forceinline__ Place place_of(const GnArgs &a, int colpart) {
+  Place w;
+  w.col0 = colpart * TH;
+  w.ncol = min(a.ncol - w.col0, TH);
+  w.g0 = blockIdx.y * a.gb;
+  w.p0 = threadIdx.x / w.ncol;
+  w.col = threadIdx.x - w.p0 * w.ncol;
+  w.on = w.p0 < a.ppi;
+  w.ch = w.g0 * a.cpg + (w.col0 + w.col) * V;
+  return w;
+}
+
+// Threads that sum a group, all groups of the bundle at once: a power of two.
+template <int TH> __device__ __forceinline__ int team_of(int ng) { return 1 << (31 - __builtin_clz(max(TH / ng, 1))); }
+__device__ __forceinline__ float team_sum(float s, int lanes) {   // within a wave
+  for (int m = min(lanes, 64) >> 1; m >= 1; m >>= 1) s += __shfl_xor(s, m, kWave);
+  return s;
+}
+
+// gs[i] = sum over the threads and channels of group i of the bundle of `v` (per thread and
+// channel of its column).
 template <int V, int TH>
-__device__ __forceinline__ void group_sums(const GnArgs &a, float (&v)[V], bool on, int col, int p0, int ncol, int ng,
-                                           int wpg, float *part, float *gs) {
-  constexpr int NW = TH / 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+__device__ __forceinline__ void group_sums(const GnArgs &a, const float (&v)[V], const Place &w, float *part, float *gs) {
+  const int tid = threadIdx.x;
   const int pitch = a.ppi | 1;                      // odd: columns in different banks
+  const int ng = a.gb;
   int per;                                          // entries of a group, in a run
   __syncthreads();                                  // part and gs are free
   if (a.same) {
-    per = (ng == 1 ? ncol : a.cpg / V) * pitch;
+    per = (ng == 1 ? w.ncol : a.cpg / V) * pitch;
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < V; ++e) s += v[e];
-    if (on) part[col * pitch + p0] = s;
-    if (on && p0 == 0 && pitch > a.ppi) part[col * pitch + a.ppi] = 0.f;
+    if (w.on) part[w.col * pitch + w.p0] = s;
+    if (w.p0 == 0 && pitch > a.ppi) part[w.col * pitch + a.ppi] = 0.f;
   } else {
     per = a.cpg * pitch;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      if (on) part[(col * V + e) * pitch + p0] = v[e];
-      if (on && p0 == 0 && pitch > a.ppi) part[(col * V + e) * pitch + a.ppi] = 0.f;
+      if (w.on) part[(w.col * V + e) * pitch + w.p0] = v[e];
+      if (w.p0 == 0 && pitch > a.ppi) part[(w.col * V + e) * pitch + a.ppi] = 0.f;
     }
   }
   __syncthreads();
-  for (int i = wave / wpg; i < ng; i += NW / wpg) { // wave-uniform
+  const int team = team_of<TH>(ng), j0 = tid & (team - 1);
+  for (int i0 = 0; i0 < ng; i0 += TH / team) {      // one round while ng <= TH
+    const int i = i0 + tid / team;
     float s = 0.f;
-    for (int j = (wave % wpg) * 64 + lane; j < per; j += wpg * 64) s += part[i * per + j];
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) s = warp_sum_xor(s, m);
-    if (lane == 0) gs[i * wpg + wave % wpg] = s;
+    if (i < ng) {
+#pragma unroll 4
+      for (int j = j0; j < per; j += team) s += part[i * per + j];
+    }
+    s = team_sum(s, team);
+    if (team <= 64) {
+      if (i < ng && j0 == 0) gs[i] = s;
+    } else {                                        // a team of several waves: one round
+      __syncthreads();                              // part is read
+      if ((tid & 63) == 0) part[tid >> 6] = s;
+      __syncthreads();
+      const int nw = team / 64;
+      if (tid < ng) {
+        s = 0.f;
+        for (int k = 0; k < nw; ++k) s += part[tid * nw + k];
+        gs[tid] = s;
+      }
+    }
   }
   __syncthreads();
 }
 
-template <typename T, int V>
+template <int V>
 __device__ __forceinline__ void normalise(const GnArgs &a, const float *x, const float *mean, const float *rstd,
                                           const float *gam, const float *bet, float *y) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const float z = fmaf((x[e] - mean[e]) * rstd[e], gam[e], bet[e]);
-    y[e] = a.act == MTE_ACT_SILU
-               ? z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z))
-               : z;
+  for (int e = 0; e < V; ++e) y[e] = fmaf((x[e] - mean[e]) * rstd[e], gam[e], bet[e]);
+  if (a.act == MTE_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      y[e] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * y[e]));
   }
 }
 
@@ -114,170 +159,228 @@ __device__ __forceinline__ void affine(const GnArgs &a, int ch, float *gam, floa
   }
 }
 
-// Grid: x = part (chunk x column part), y = bundle, z = image. FUSED: one part, y written here; else
-// (mean, squares) of the part to ws[image][group][part].
-template <typename T, int V, int TH, bool FUSED>
-__global__ __launch_bounds__(TH) void k_gn(GnArgs a) {
+// One launch. Grid: y = bundle, z = image. LDS: gs [gb], part, then the slab [round][thread].
+template <typename T, int V, int TH>
+__global__ __launch_bounds__(TH) void k_gn(GnArgs a, int slab) {
   typedef Vec<T, V> vec;
-  constexpr int HOLD = hold_of(V * sizeof(T));
+  typedef typename vec::raw raw;
   extern __shared__ float lds[];
-  const int tid = threadIdx.x;
-  const int cp = (int)blockIdx.x % a.colparts, chunk = (int)blockIdx.x / a.colparts;
-  const int col0 = cp * TH, ncol = min(a.ncol - col0, TH);
-  const int g0 = blockIdx.y * a.gb, ng = a.gb;
-  const int px0 = chunk * a.chunk, npx = min(a.chunk, a.pixels - px0);
-  const int col = tid % ncol, p0 = tid / ncol;
-  const bool on = p0 < a.ppi;
-  const int ch = g0 * a.cpg + (col0 + col) * V;     // first channel of the column
-  const T *x = (const T *)a.x + (int64_t)blockIdx.z * a.x_image + (int64_t)px0 * a.x_row + ch;
-  constexpr int NW = TH / 64;
-  const int wpg = max(1, NW / ng);
-  float *gs = lds, *part = lds + max(NW, ng) ;
-  typename vec::raw r[HOLD];
+  float *gs = lds, *part = lds + a.gb;
+  raw *mine = (raw *)((char *)lds + slab) + threadIdx.x;
+  const Place w = place_of<V, TH>(a, 0);
+  const T *x = (const T *)a.x + (int64_t)blockIdx.z * a.x_image + w.ch;
+  const int end = w.on ? a.pixels : 0;
   float sum[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) sum[e] = 0.f;
+  for (int p = w.p0, i = 0; p < end; p += kBatch * a.ppi, i += kBatch) {
+    raw r[kBatch];
 #pragma unroll
-  for (int i = 0; i < HOLD; ++i) {
-    const int p = p0 + i * a.ppi;
-    if (on && p < npx) r[i] = vec::load(x + (int64_t)p * a.x_row);
-  }
+    for (int k = 0; k < kBatch; ++k)                // past the end: the last pixel again
+      r[k] = vec::load(x + (int64_t)min(p + k * a.ppi, a.pixels - 1) * a.x_row);
 #pragma unroll
-  for (int i = 0; i < HOLD; ++i) {
-    if (on && p0 + i * a.ppi < npx) {
-      float f[V];
-      vec::unpack(r[i], f);
+    for (int k = 0; k < kBatch; ++k) {
+      if (p + k * a.ppi < a.pixels) {
+        float f[V];
+        vec::unpack(r[k], f);
 #pragma unroll
-      for (int e = 0; e < V; ++e) sum[e] += f[e];
+        for (int e = 0; e < V; ++e) sum[e] += f[e];
+        mine[(i + k) * TH] = r[k];
+      }
     }
   }
-  group_sums<V, TH>(a, sum, on, col, p0, ncol, ng, wpg, part, gs);
-  const float cnt = (float)npx * (float)(ng == 1 ? ncol * V : a.cpg);
-  float mean[V], sq[V];
+  float gam[V], bet[V];
+  affine<T, V>(a, w.ch, gam, bet);
+  group_sums<V, TH>(a, sum, w, part, gs);
+  const float inv = 1.f / ((float)a.pixels * (float)a.cpg);
+  float mean[V], rstd[V];
   int gi[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    gi[e] = ng == 1 ? 0 : ((col0 + col) * V + e) / a.cpg;
-    float s = 0.f;
-    for (int w = 0; w < wpg; ++w) s += gs[gi[e] * wpg + w];
-    mean[e] = s / cnt;
-    sq[e] = 0.f;
+    gi[e] = a.gb == 1 ? 0 : (w.col * V + e) / a.cpg;
+    mean[e] = gs[gi[e]] * inv;
+    sum[e] = 0.f;
   }
+#pragma unroll 2
+  for (int p = w.p0, i = 0; p < end; p += a.ppi, ++i) {
+    float f[V];
+    vec::unpack(mine[i * TH], f);
 #pragma unroll
-  for (int i = 0; i < HOLD; ++i) {
-    if (on && p0 + i * a.ppi < npx) {
+    for (int e = 0; e < V; ++e) sum[e] = fmaf(f[e] - mean[e], f[e] - mean[e], sum[e]);
+  }
+  group_sums<V, TH>(a, sum, w, part, gs);
+#pragma unroll
+  for (int e = 0; e < V; ++e) rstd[e] = 1.f / sqrtf(gs[gi[e]] * inv + a.eps);
+  T *y = (T *)a.y + (int64_t)blockIdx.z * a.y_image + w.ch;
+#pragma unroll 2
+  for (int p = w.p0, i = 0; p < end; p += a.ppi, ++i) {
+    float f[V], o[V];
+    vec::unpack(mine[i * TH], f);
+    normalise<V>(a, f, mean, rstd, gam, bet, o);
+    *(raw *)(y + (int64_t)p * a.y_row) = vec::pack(o);
+  }
+}
+
+// First of two launches. Grid: x = part (chunk x column part), y = bundle, z = image.
+template <typename T, int V, int TH>
+__global__ __launch_bounds__(TH) void k_gn_stats(GnArgs a) {
+  typedef Vec<T, V> vec;
+  extern __shared__ float lds[];
+  float *gs = lds, *part = lds + a.gb;
+  const int chunk = (int)blockIdx.x / a.colparts;
+  const Place w = place_of<V, TH>(a, (int)blockIdx.x - chunk * a.colparts);
+  const int px0 = chunk * a.chunk, npx = min(a.chunk, a.pixels - px0);
+  const T *x = (const T *)a.x + (int64_t)blockIdx.z * a.x_image + (int64_t)px0 * a.x_row + w.ch;
+  // this thread's pixels, a batch at a time: (n, mean, squares) of each channel so far
+  float n = 0.f, mean[V], sq[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) mean[e] = sq[e] = 0.f;
+  constexpr int B = 2 * kBatch;
+  for (int p = w.p0; p < (w.on ? npx : 0); p += a.ppi * B) {
+    const int left = (npx - p + a.ppi - 1) / a.ppi; // pixels of this batch
+    typename vec::raw r[B];
+#pragma unroll
+    for (int i = 0; i < B; ++i)                     // past the end: the last one again, not counted
+      r[i] = vec::load(x + (int64_t)(p + min(i, left - 1) * a.ppi) * a.x_row);
+    float s[V], q[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = q[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
       float f[V];
       vec::unpack(r[i], f);
 #pragma unroll
-      for (int e = 0; e < V; ++e) sq[e] = fmaf(f[e] - mean[e], f[e] - mean[e], sq[e]);
+      for (int e = 0; e < V; ++e) s[e] += i < left ? f[e] : 0.f;
     }
-  }
-  group_sums<V, TH>(a, sq, on, col, p0, ncol, ng, wpg, part, gs);
-  if constexpr (FUSED) {
-    float rstd[V], gam[V], bet[V];
+    const float k = (float)min(left, B), ik = 1.f / k, all = n + k;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float s = 0.f;
-      for (int w = 0; w < wpg; ++w) s += gs[gi[e] * wpg + w];
-      rstd[e] = 1.f / sqrtf(s / cnt + a.eps);
-    }
-    affine<T, V>(a, ch, gam, bet);
-    T *y = (T *)a.y + (int64_t)blockIdx.z * a.y_image + (int64_t)px0 * a.y_row + ch;
+    for (int e = 0; e < V; ++e) s[e] *= ik;
 #pragma unroll
-    for (int i = 0; i < HOLD; ++i) {
-      const int p = p0 + i * a.ppi;
-      if (on && p < npx) {
-        float f[V], o[V];
-        vec::unpack(r[i], f);
-        normalise<T, V>(a, f, mean, rstd, gam, bet, o);
-        *(typename vec::raw *)(y + (int64_t)p * a.y_row) = vec::pack(o);
+    for (int i = 0; i < B; ++i) {
+      float f[V];
+      vec::unpack(r[i], f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = i < left ? f[e] - s[e] : 0.f;
+        q[e] = fmaf(d, d, q[e]);
       }
     }
-  } else {
-    // a thread that has an element of the group writes it: the first of its channels
-    const int parts = gridDim.x;
+    const float share = k / all, cross = n * share;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const int c = (col0 + col) * V + e;
-      if (on && p0 == 0 && (ng == 1 ? col == 0 && e == 0 : c % a.cpg == 0)) {
-        float s = 0.f;
-        for (int w = 0; w < wpg; ++w) s += gs[gi[e] * wpg + w];
-        float *o = a.ws + (((int64_t)blockIdx.z * a.groups + g0 + gi[e]) * parts + blockIdx.x) * 2;
-        o[0] = mean[e];
-        o[1] = s;
-      }
+      const float d = s[e] - mean[e];
+      mean[e] = fmaf(d, share, mean[e]);
+      sq[e] += fmaf(d * d, cross, q[e]);
     }
+    n = all;
   }
+  float t[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) t[e] = n * mean[e];
+  group_sums<V, TH>(a, t, w, part, gs);
+  const float cnt = (float)npx * (float)(a.gb == 1 ? w.ncol * V : a.cpg), inv = 1.f / cnt;
+  float gm[V];
+  int gi[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    gi[e] = a.gb == 1 ? 0 : (w.col * V + e) / a.cpg;
+    gm[e] = gs[gi[e]] * inv;
+    t[e] = fmaf(n * (mean[e] - gm[e]), mean[e] - gm[e], sq[e]);
+  }
+  for (int i = threadIdx.x; i < a.gb; i += TH) {    // (count, mean, squares) of the part
+    float *o = a.ws + (((int64_t)blockIdx.z * a.groups + w.g0 + i) * a.parts + blockIdx.x) * 4;
+    o[0] = cnt;
+    o[1] = gs[i] * inv;
+  }
+  group_sums<V, TH>(a, t, w, part, gs);
+  for (int i = threadIdx.x; i < a.gb; i += TH)
+    a.ws[(((int64_t)blockIdx.z * a.groups + w.g0 + i) * a.parts + blockIdx.x) * 4 + 2] = gs[i];
 }
 
 // The second launch: joins the parts of its groups (counts n_i, means m_i, squares S_i:
-// mean = sum n_i m_i / N, squares = sum S_i + n_i (m_i - mean)^2), then normalises its slab.
-template <typename T, int V, int TH>
+// mean = sum n_i m_i / N, squares = sum S_i + n_i (m_i - mean)^2), then normalises its pixels.
+// Grid: x = chunk of `apply` pixels x column part, y = bundle, z = image. PAST: y is more than the
+// 32 MB of L2 and is stored past it (8 x 128 x 128 x 320: 54.4 us against 57.7).
+template <typename T, int V, int TH, bool PAST>
 __global__ __launch_bounds__(TH) void k_gn_apply(GnArgs a) {
   typedef Vec<T, V> vec;
-  constexpr int HOLD = hold_of(V * sizeof(T));
   extern __shared__ float lds[];                    // [gb][2]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int parts = gridDim.x;
-  const int cp = (int)blockIdx.x % a.colparts, chunk = (int)blockIdx.x / a.colparts;
-  const int col0 = cp * TH, ncol = min(a.ncol - col0, TH);
-  const int g0 = blockIdx.y * a.gb, ng = a.gb;
-  const int px0 = chunk * a.chunk, npx = min(a.chunk, a.pixels - px0);
-  const int col = tid % ncol, p0 = tid / ncol;
-  const bool on = p0 < a.ppi;
-  const int ch = g0 * a.cpg + (col0 + col) * V;
-  const T *x = (const T *)a.x + (int64_t)blockIdx.z * a.x_image + (int64_t)px0 * a.x_row + ch;
-  typename vec::raw r[HOLD];
+  const int tid = threadIdx.x;
+  const int chunk = (int)blockIdx.x / a.colparts;
+  const Place w = place_of<V, TH>(a, (int)blockIdx.x - chunk * a.colparts);
+  const int px0 = chunk * a.apply, npx = w.on ? min(a.apply, a.pixels - px0) : 0;
+  const T *x = (const T *)a.x + (int64_t)blockIdx.z * a.x_image + (int64_t)px0 * a.x_row + w.ch;
+  T *y = (T *)a.y + (int64_t)blockIdx.z * a.y_image + (int64_t)px0 * a.y_row + w.ch;
+  typename vec::raw r[kBatch], rn[kBatch];
+  auto load = [&](int p, typename vec::raw (&to)[kBatch]) {
 #pragma unroll
-  for (int i = 0; i < HOLD; ++i) {
-    const int p = p0 + i * a.ppi;
-    if (on && p < npx) r[i] = vec::load(x + (int64_t)p * a.x_row);
-  }
-  for (int i = wave; i < ng; i += TH / 64) {        // wave-uniform
-    const float *w = a.ws + ((int64_t)blockIdx.z * a.groups + g0 + i) * parts * 2;
-    auto count = [&](int j) {
-      const int n = min(a.chunk, a.pixels - j / a.colparts * a.chunk);
-      return (float)n * (float)(a.colparts > 1 ? min(a.ncol - j % a.colparts * TH, TH) * V : a.cpg);
-    };
+    for (int i = 0; i < kBatch; ++i)
+      if (p + i * a.ppi < npx) to[i] = vec::load(x + (int64_t)(p + i * a.ppi) * a.x_row);
+  };
+  load(w.p0, r);
+  load(w.p0 + kBatch * a.ppi, rn);
+  float gam[V], bet[V];
+  affine<T, V>(a, w.ch, gam, bet);
+  // teams of lanes over the parts of a group, all groups at once; a lane's first PRE parts are in
+  // flight together
+  constexpr int PRE = 8;
+  const int lanes = min(team_of<TH>(a.gb), 64), j0 = tid & (lanes - 1);
+  const float inv = 1.f / ((float)a.pixels * (float)a.cpg);
+  for (int i0 = 0; i0 < a.gb; i0 += TH / lanes) {
+    const int i = i0 + tid / lanes;
+    const f32x4 *ws = (const f32x4 *)a.ws + ((int64_t)blockIdx.z * a.groups + w.g0 + min(i, a.gb - 1)) * a.parts;
+    f32x4 m[PRE];
+#pragma unroll
+    for (int k = 0; k < PRE; ++k) m[k] = j0 + k * lanes < a.parts ? ws[j0 + k * lanes] : f32x4{0.f, 0.f, 0.f, 0.f};
     float s = 0.f;
-    for (int j = lane; j < parts; j += 64) s += count(j) * w[2 * j];
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) s = warp_sum_xor(s, m);
-    const float total = (float)a.pixels * (float)a.cpg, mean = s / total;
-    float q = 0.f;
-    for (int j = lane; j < parts; j += 64) q += w[2 * j + 1] + count(j) * (w[2 * j] - mean) * (w[2 * j] - mean);
+    for (int k = 0; k < PRE; ++k) s = fmaf(m[k][0], m[k][1], s);
+    for (int j = j0 + PRE * lanes; j < a.parts; j += lanes) s = fmaf(ws[j][0], ws[j][1], s);
+    const float mean = team_sum(s, lanes) * inv;
+    s = 0.f;
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) q = warp_sum_xor(q, m);
-    if (lane == 0) {
+    for (int k = 0; k < PRE; ++k) s += fmaf(m[k][0] * (m[k][1] - mean), m[k][1] - mean, m[k][2]);
+    for (int j = j0 + PRE * lanes; j < a.parts; j += lanes)
+      s += fmaf(ws[j][0] * (ws[j][1] - mean), ws[j][1] - mean, ws[j][2]);
+    s = team_sum(s, lanes);
+    if (j0 == 0 && i < a.gb) {
       lds[2 * i] = mean;
-      lds[2 * i + 1] = 1.f / sqrtf(q / total + a.eps);
+      lds[2 * i + 1] = 1.f / sqrtf(s * inv + a.eps);
     }
   }
   __syncthreads();
-  float mean[V], rstd[V], gam[V], bet[V];
+  float mean[V], rstd[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const int gi = ng == 1 ? 0 : ((col0 + col) * V + e) / a.cpg;
+    const int gi = a.gb == 1 ? 0 : (w.col * V + e) / a.cpg;
     mean[e] = lds[2 * gi];
     rstd[e] = lds[2 * gi + 1];
   }
-  affine<T, V>(a, ch, gam, bet);
-  T *y = (T *)a.y + (int64_t)blockIdx.z * a.y_image + (int64_t)px0 * a.y_row + ch;
+  for (int p = w.p0; p < npx; p += kBatch * a.ppi) {
 #pragma unroll
-  for (int i = 0; i < HOLD; ++i) {
-    const int p = p0 + i * a.ppi;
-    if (on && p < npx) {
-      float f[V], o[V];
-      vec::unpack(r[i], f);
-      normalise<T, V>(a, f, mean, rstd, gam, bet, o);
-      *(typename vec::raw *)(y + (int64_t)p * a.y_row) = vec::pack(o);
+    for (int i = 0; i < kBatch; ++i) {
+      if (p + i * a.ppi < npx) {
+        float f[V], o[V];
+        vec::unpack(r[i], f);
+        normalise<V>(a, f, mean, rstd, gam, bet, o);
+        typename vec::raw *to = (typename vec::raw *)(y + (int64_t)(p + i * a.ppi) * a.y_row);
+        if constexpr (PAST) __builtin_nontemporal_store(vec::pack(o), to);
+        else *to = vec::pack(o);
+      }
+      r[i] = rn[i];
     }
+    load(p + 2 * kBatch * a.ppi, rn);
   }
 }
 
+// Two launches: workgroups that keep the chip busy, most parts of an image (every workgroup of the
+// second launch reads those of its groups), batches of its pixels a thread of the second launch
+// takes. One launch: the largest slab.
+constexpr int kFill = 512, kParts = 64, kTurns = 4, kSlab = 128 * 1024;
+
 struct GnPlan {
-  int V, TH, gb, ncol, ppi, chunk, colparts, parts;
-  bool fused;
+  int V, TH, gb, ncol, ppi, chunk, apply, colparts, parts;
+  bool one;
 };
 
 // Widest vector of at most 16 bytes that divides a bundle of n channels and `align` elements.
@@ -291,62 +394,75 @@ int vec_of(int n, int align, int esize) {
 GnPlan plan_of(int n, int pixels, int channels, int groups, int esize, int align) {
   const int cpg = channels / groups;
   GnPlan p;
-  // one launch: the fewest groups whose channels are a run of 64 bytes, if an image of them fits
-  for (int gb = 1; gb <= groups; ++gb) {
-    if (groups % gb) continue;
-    const int w = gb * cpg, v = vec_of(w, align, esize), ncol = w / v;
-    if (w * esize < 64 && gb < groups) continue;
-    for (int th : {256, 1024}) {
-      if (ncol > th) continue;
+  // One launch, if an image of a bundle fits: the fewest groups whose channels are a run of 64 bytes
+  // (32 where that leaves fewer than 64 workgroups), and at least 32 workgroups or next to no
+  // work. us in one / two launches: 1 x 16 x 16 x 1280 9.2 / 12.2, 1 x 32 x 32 x 640 11.4 / 13.2,
+  // 16 x 16 x 16 x 1280 15.0 / 17.8, 16 x 32 x 32 x 640 25.0 / 26.0; 2 x 33 x 31 x 96 (16
+  // workgroups) 14.4 / 12.5.
+  for (int run = 64; run >= 32; run -= 32) {
+    for (int gb = 1; gb <= groups; ++gb) {
+      if (groups % gb) continue;
+      const int w = gb * cpg, v = vec_of(w, align, esize), ncol = w / v;
+      if (w * esize < run && gb < groups) continue;
+      const int th = (int64_t)ncol * pixels <= 2048 && ncol <= 256 ? 256 : 1024;
+      if (ncol > th) break;
       const int ppi = std::min(th / ncol, pixels);
-      if ((int64_t)ppi * hold_of(v * esize) < pixels) continue;
-      p = GnPlan{v, th, gb, ncol, ppi, pixels, 1, 1, true};
-      return p;
+      const int64_t bytes = ((int64_t)pixels + ppi - 1) / ppi * th * v * esize, wgs = (int64_t)n * (groups / gb);
+      if (bytes > kSlab || (wgs < (run == 64 ? 64 : 32) && bytes > 16384)) break;
+      return GnPlan{v, th, gb, ncol, ppi, pixels, pixels, 1, 1, true};
     }
-    break;
   }
   // two launches: as many groups as a workgroup of 256 has columns for
-  p.fused = false;
+  p.one = false;
   p.TH = 256;
   p.gb = 1;
   for (int gb = 1; gb <= groups; ++gb) {
     if (groups % gb) continue;
     const int w = gb * cpg;
-    if (w / vec_of(w, align, esize) <= p.TH) p.gb = gb;
+    if (w / vec_of(w, align, esize) > p.TH) continue;
+    // wider while that leaves kFill workgroups, or rows shorter than two lines
+    if (gb == 1 || p.gb * cpg * esize < 256 || (int64_t)n * (groups / gb) * kParts >= kFill) p.gb = gb;
   }
   p.V = vec_of(p.gb * cpg, align, esize);
   p.ncol = p.gb * cpg / p.V;
   p.colparts = (p.ncol + p.TH - 1) / p.TH;
   p.ppi = p.colparts > 1 ? 1 : std::min(p.TH / p.ncol, pixels);
-  p.chunk = std::min(p.ppi * hold_of(p.V * esize), pixels);
+  // parts of an image: kFill workgroups in all, but at most kParts parts (each workgroup of the
+  // second launch reads them all) of at least one batch
+  const int64_t bundles = (int64_t)n * (groups / p.gb) * p.colparts;
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kParts / p.colparts, kFill / bundles));
+  const int step = p.ppi * 2 * kBatch;
+  p.chunk = (int)std::min<int64_t>(pixels, std::max<int64_t>(1, ((int64_t)pixels + want * step - 1) / (want * step)) * step);
   p.parts = (int)(((int64_t)pixels + p.chunk - 1) / p.chunk) * p.colparts;
+  const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(kTurns, (int64_t)pixels * bundles / ((int64_t)p.ppi * kBatch * kFill)));
+  p.apply = (int)std::min<int64_t>(pixels, p.ppi * kBatch * turns);
   return p;
 }
 
-template <typename T, int V, int TH>
-hipError_t run(const GnArgs &a, const GnPlan &p, hipStream_t s) {
-  const dim3 grid(p.parts, a.groups / p.gb, a.n);
-  const int entries = (a.same ? 1 : V) * std::min(p.ncol, TH) * (p.ppi | 1);
-  const int lds = (std::max(TH / 64, p.gb) + entries) * 4;
-  hipError_t e;
-  auto one = k_gn<T, V, TH, true>;
-  auto two = k_gn<T, V, TH, false>;
-  if (lds > 65536 && (e = hipFuncSetAttribute((const void *)(p.fused ? one : two),
-                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds)) != hipSuccess)
-    return e;
-  if (p.fused) {
-    hipLaunchKernelGGL(one, grid, dim3(TH), lds, s, a);
-    return hipGetLastError();
-  }
-  hipLaunchKernelGGL(two, grid, dim3(TH), lds, s, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL((k_gn_apply<T, V, TH>), grid, dim3(TH), p.gb * 8, s, a);
-  return hipGetLastError();
+template <typename K> hipError_t allow_lds(K kern, int bytes) {
+  return bytes <= 65536 ? hipSuccess
+                        : hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 template <typename T, int V>
-hipError_t run_th(const GnArgs &a, const GnPlan &p, hipStream_t s) {
-  return p.TH == 1024 ? run<T, V, 1024>(a, p, s) : run<T, V, 256>(a, p, s);
+hipError_t run(const GnArgs &a, const GnPlan &p, int esize, hipStream_t s) {
+  const int entries = (a.same ? 1 : V) * std::min(p.ncol, p.TH) * (p.ppi | 1);
+  const int sums = ((p.gb + std::max(entries, 16)) * 4 + 15) & ~15, bundles = a.groups / p.gb;
+  hipError_t e;
+  if (p.one) {
+    auto kern = p.TH == 256 ? k_gn<T, V, 256> : k_gn<T, V, 1024>;
+    const int lds = sums + (a.pixels + p.ppi - 1) / p.ppi * p.TH * V * esize;
+    if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3(1, bundles, a.n), dim3(p.TH), lds, s, a, sums);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((k_gn_stats<T, V, 256>), dim3(p.parts, bundles, a.n), dim3(256), sums, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int chunks = (int)(((int64_t)a.pixels + p.apply - 1) / p.apply);
+  const bool past = (int64_t)a.n * a.pixels * a.channels * esize > (32 << 20);
+  auto apply = past ? k_gn_apply<T, V, 256, true> : k_gn_apply<T, V, 256, false>;
+  hipLaunchKernelGGL(apply, dim3(chunks * p.colparts, bundles, a.n), dim3(256), p.gb * 8, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -357,7 +473,7 @@ int64_t group_norm_workspace(int n, int pixels, int channels, int groups, int dt
   int64_t most = 0;
   for (int align = 1; align <= 8; align *= 2) {
     const GnPlan p = plan_of(n, pixels, channels, groups, es, align);
-    if (!p.fused) most = std::max(most, (int64_t)n * groups * p.parts * 8);
+    if (!p.one) most = std::max(most, (int64_t)n * groups * p.parts * 16);
   }
   return most;
 }
@@ -375,17 +491,19 @@ hipError_t launch_group_norm(const GroupNormArgs &g, int dtype, hipStream_t s) {
   a.ncol = p.ncol;
   a.ppi = p.ppi;
   a.chunk = p.chunk;
+  a.apply = p.apply;
+  a.parts = p.parts;
   a.colparts = p.colparts;
   a.same = p.gb == 1 || a.cpg % p.V == 0;
   if (dtype == MTE_BF16) {
-    if (p.V == 8) return run_th<bf16, 8>(a, p, s);
-    if (p.V == 4) return run_th<bf16, 4>(a, p, s);
-    if (p.V == 2) return run_th<bf16, 2>(a, p, s);
-    return run_th<bf16, 1>(a, p, s);
+    if (p.V == 8) return run<bf16, 8>(a, p, es, s);
+    if (p.V == 4) return run<bf16, 4>(a, p, es, s);
+    if (p.V == 2) return run<bf16, 2>(a, p, es, s);
+    return run<bf16, 1>(a, p, es, s);
   }
-  if (p.V == 4) return run_th<float, 4>(a, p, s);
-  if (p.V == 2) return run_th<float, 2>(a, p, s);
-  return run_th<float, 1>(a, p, s);
+  if (p.V == 4) return run<float, 4>(a, p, es, s);
+  if (p.V == 2) return run<float, 2>(a, p, es, s);
+  return run<float, 1>(a, p, es, s);
 }
 
 }  // namespace mte
