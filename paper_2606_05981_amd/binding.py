@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libmte.so")
 MTE_F32, MTE_BF16 = 0, 1
 MTE_MROPE_SECTIONS, MTE_MROPE_INTERLEAVED = 0, 1
 MTE_WEIGHTS_DTYPE, MTE_WEIGHTS_E4M3 = 0, 1
+MTE_E_CAPACITY = -2
 STATUS = {0: "MTE_OK", -1: "MTE_E_INVALID", -2: "MTE_E_CAPACITY", -3: "MTE_E_HIP",
           -4: "MTE_E_OOM", -5: "MTE_E_UNSUPPORTED"}
 MTE_ACT_NONE, MTE_ACT_SILU = 0, 1
@@ -123,18 +125,15 @@ _sig = {
     "mte_vision_encode": (C.c_int, [_P, _P, C.c_int32, C.c_int32, C.c_int32, _P, _P]),
     "mte_vision_encode_strided": (C.c_int, [_P, _P, C.c_int32, C.c_int32, C.c_int32, _P, C.c_int32, _P]),
     "mte_vision_destroy": (None, [_P]),
-    "mte_cross_attention": (C.c_int, [C.POINTER(mte_attn_shape), _P, _P, _P, _P, C.POINTER(C.c_int32), C.c_int32,
-                                      C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_int32), _P, _P, C.c_int64, _P]),
-    "mte_cross_attention_workspace": (C.c_int64, [C.POINTER(mte_attn_shape), C.POINTER(C.c_int32), C.c_int32,
-                                                  C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_int32)]),
-    "mte_kv8_append": (C.c_int, [C.POINTER(mte_kv8), _P, C.c_int32, C.c_int64, _P, _P, C.c_int64, C.c_int64, _P,
-                                 C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_int32), C.c_int32, _P]),
-    "mte_kv8_read": (C.c_int, [C.POINTER(mte_kv8), _P, C.c_int32, C.c_int64, _P, C.POINTER(C.c_int32), C.c_int32,
-                               _P, _P, C.c_int32, _P]),
-    "mte_kv8_attention": (C.c_int, [C.POINTER(mte_attn_shape), C.POINTER(mte_kv8), _P, C.c_int32, C.c_int64, _P, _P,
-                                    C.POINTER(C.c_int32), C.c_int32, C.c_int32, _P, _P, C.c_int64, _P]),
-    "mte_kv8_attention_workspace": (C.c_int64, [C.POINTER(mte_attn_shape), C.POINTER(C.c_int32), C.c_int32,
-                                                C.c_int32]),
+    # descriptors and host arrays as plain addresses: a ctypes object, bytes of the struct or an int
+    "mte_cross_attention": (C.c_int, [_P, _P, _P, _P, _P, _P, C.c_int32, _P, C.c_int32, _P, _P, _P, C.c_int64, _P]),
+    "mte_cross_attention_workspace": (C.c_int64, [_P, _P, C.c_int32, _P, C.c_int32, _P]),
+    "mte_kv8_append": (C.c_int, [_P, _P, C.c_int32, C.c_int64, _P, _P, C.c_int64, C.c_int64, _P, C.c_int64,
+                                 C.c_int64, C.c_int32, _P, C.c_int32, _P]),
+    "mte_kv8_read": (C.c_int, [_P, _P, C.c_int32, C.c_int64, _P, _P, C.c_int32, _P, _P, C.c_int32, _P]),
+    "mte_kv8_attention": (C.c_int, [_P, _P, _P, C.c_int32, C.c_int64, _P, _P, _P, C.c_int32, C.c_int32, _P, _P,
+                                    C.c_int64, _P]),
+    "mte_kv8_attention_workspace": (C.c_int64, [_P, _P, C.c_int32, C.c_int32]),
     "mte_group_norm": (C.c_int, [_P, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P,
                                  C.c_float, C.c_int32, C.c_int32, _P, C.c_int64, C.c_int64, _P, C.c_int64, _P]),
     "mte_group_norm_workspace": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
@@ -307,48 +306,52 @@ def mte_vision_encode_strided(enc: int, pixels: int, n_images: int, height: int,
                   "mte_vision_encode_strided")
 
 
+# The descriptors of mte_cond.h as bytes (what a call passes): the same layout as the structures above.
+ATTN_SHAPE = struct.Struct("@iiiif4x8q")
+KV8 = struct.Struct("@PPPiii4x")
+assert ATTN_SHAPE.size == C.sizeof(mte_attn_shape) and KV8.size == C.sizeof(mte_kv8)
+
+
 def make_attn_shape(n_q_heads, n_kv_heads, head_dim, dtype, scale, q=(0, 0), k=(0, 0), v=(0, 0),
                     out=(0, 0)) -> mte_attn_shape:
     """q, k, v, out: (row, head) strides in elements."""
     return mte_attn_shape(n_q_heads, n_kv_heads, head_dim, dtype, scale, *q, *k, *v, *out)
 
 
-def mte_cross_attention_workspace(shape: mte_attn_shape, q_lens, n_q: int, kv_lens, n_kv: int, kv_index) -> int:
-    """q_lens, kv_lens, kv_index (or None): int32 arrays as _i32 makes them, as in every call below."""
-    return _check(lib.mte_cross_attention_workspace(C.byref(shape), q_lens, n_q, kv_lens, n_kv, kv_index),
+# shape, cache: bytes (ATTN_SHAPE / KV8) or the structures by reference; q_lens, kv_lens (host), kv_index,
+# new_lens, counts: int32 arrays as _i32 makes them, or their address.
+
+def mte_cross_attention_workspace(shape, q_lens, n_q: int, kv_lens, n_kv: int, kv_index) -> int:
+    return _check(lib.mte_cross_attention_workspace(shape, q_lens, n_q, kv_lens, n_kv, kv_index),
                   "mte_cross_attention_workspace")
 
 
-def mte_cross_attention(shape: mte_attn_shape, q: int, k: int, v: int, key_mask: Optional[int], q_lens, n_q: int,
-                        kv_lens, n_kv: int, kv_index, out: int, workspace: Optional[int], workspace_bytes: int,
-                        stream: int) -> int:
-    return _check(lib.mte_cross_attention(C.byref(shape), q, k, v, key_mask, q_lens, n_q, kv_lens, n_kv, kv_index,
-                                          out, workspace, workspace_bytes, stream), "mte_cross_attention")
+def mte_cross_attention(shape, q: int, k: int, v: int, key_mask: Optional[int], q_lens, n_q: int, kv_lens, n_kv: int,
+                        kv_index, out: int, workspace: Optional[int], workspace_bytes: int, stream: int) -> int:
+    return _check(lib.mte_cross_attention(shape, q, k, v, key_mask, q_lens, n_q, kv_lens, n_kv, kv_index, out,
+                                          workspace, workspace_bytes, stream), "mte_cross_attention")
 
 
-def mte_kv8_append(cache: mte_kv8, table: int, table_width: int, table_row: int, kv_lens: int, k: int, k_row: int,
-                   k_head: int, v: int, v_row: int, v_head: int, dtype: int, new_lens, n: int, stream: int) -> int:
-    return _check(lib.mte_kv8_append(C.byref(cache), table, table_width, table_row, kv_lens, k, k_row, k_head, v,
-                                     v_row, v_head, dtype, new_lens, n, stream), "mte_kv8_append")
+def mte_kv8_append(cache, table: int, table_width: int, table_row: int, kv_lens: int, k: int, k_row: int, k_head: int,
+                   v: int, v_row: int, v_head: int, dtype: int, new_lens, n: int, stream: int) -> int:
+    return _check(lib.mte_kv8_append(cache, table, table_width, table_row, kv_lens, k, k_row, k_head, v, v_row, v_head,
+                                     dtype, new_lens, n, stream), "mte_kv8_append")
 
 
-def mte_kv8_read(cache: mte_kv8, table: int, table_width: int, table_row: int, kv_lens: int, counts, n: int, k: int,
-                 v: int, dtype: int, stream: int) -> int:
-    return _check(lib.mte_kv8_read(C.byref(cache), table, table_width, table_row, kv_lens, counts, n, k, v, dtype,
-                                   stream), "mte_kv8_read")
+def mte_kv8_read(cache, table: int, table_width: int, table_row: int, kv_lens: int, counts, n: int, k: int, v: int,
+                 dtype: int, stream: int) -> int:
+    return _check(lib.mte_kv8_read(cache, table, table_width, table_row, kv_lens, counts, n, k, v, dtype, stream),
+                  "mte_kv8_read")
 
 
-def mte_kv8_attention_workspace(shape: mte_attn_shape, q_lens, n: int, table_width: int) -> int:
-    return _check(lib.mte_kv8_attention_workspace(C.byref(shape), q_lens, n, table_width),
-                  "mte_kv8_attention_workspace")
+def mte_kv8_attention_workspace(shape, q_lens, n: int, table_width: int) -> int:
+    return _check(lib.mte_kv8_attention_workspace(shape, q_lens, n, table_width), "mte_kv8_attention_workspace")
 
 
-def mte_kv8_attention(shape: mte_attn_shape, cache: mte_kv8, table: int, table_width: int, table_row: int,
-                      kv_lens: int, q: int, q_lens, n: int, causal: int, out: int, workspace: Optional[int],
-                      workspace_bytes: int, stream: int) -> int:
-    return _check(lib.mte_kv8_attention(C.byref(shape), C.byref(cache), table, table_width, table_row, kv_lens, q,
-                                        q_lens, n, causal, out, workspace, workspace_bytes, stream),
-                  "mte_kv8_attention")
+def mte_kv8_attention(shape, cache, table: int, table_width: int, table_row: int, kv_lens: int, q: int, q_lens, n: int,
+                      causal: int, out: int, workspace: Optional[int], workspace_bytes: int, stream: int) -> int:
+    return _check(lib.mte_kv8_attention(shape, cache, table, table_width, table_row, kv_lens, q, q_lens, n, causal, out,
+                                        workspace, workspace_bytes, stream), "mte_kv8_attention")
 
 
 def mte_group_norm_workspace(n: int, pixels: int, channels: int, groups: int, dtype: int) -> int:

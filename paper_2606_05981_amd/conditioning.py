@@ -11,6 +11,7 @@ one for the results.
 from __future__ import annotations
 
 import math
+from array import array
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -21,14 +22,18 @@ _DTYPE = {torch.float32: B.MTE_F32, torch.bfloat16: B.MTE_BF16}
 _ACT = {None: B.MTE_ACT_NONE, "none": B.MTE_ACT_NONE, "silu": B.MTE_ACT_SILU}
 
 
+# the current stream's handle without a Stream object around it (4 us of a call of 15)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _on(device: torch.device, stream: Optional[torch.cuda.Stream], used, fn):
     """fn(stream handle) with `device` and the stream current; `used` tensors (None allowed) and
     the results stay allocated until a stream other than their own is done with them."""
     if stream is None:
-        if device.index == torch.cuda.current_device():
-            return fn(torch.cuda.current_stream().cuda_stream)
+        if device.index == torch._C._cuda_getDevice():
+            return fn(_raw_stream(device.index))
         with torch.cuda.device(device):
-            return fn(torch.cuda.current_stream().cuda_stream)
+            return fn(_raw_stream(device.index))
     if stream.device != device:
         raise ValueError(f"stream: expected one of {device}, got one of {stream.device}")
     with torch.cuda.device(device):
@@ -50,14 +55,15 @@ def _rows(name: str, t, dtype: torch.dtype, heads: int, d: int, device: torch.de
     """Checks a [rows, heads, d] tensor and returns its (row, head) strides."""
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name}: expected a [tokens, heads, head_dim] tensor")
-    if not t.is_cuda or t.device != device:
+    if t.device != device:
         raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
     if t.dtype != dtype:
         raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
-    if t.shape[1] != heads or t.shape[2] != d:
+    n, h, c = t.shape
+    if h != heads or c != d:
         raise ValueError(f"{name}: expected shape (*, {heads}, {d}), got {tuple(t.shape)}")
     row, head, one = t.stride()
-    if t.shape[0] <= 1:
+    if n <= 1:
         row = 0
     if heads == 1:
         head = 0
@@ -86,14 +92,22 @@ def _query(q):
 
 
 def _lens(name: str, lens: Sequence[int], rows: Optional[int]):
-    n = len(lens)
-    if rows is not None and sum(lens) != rows:
-        raise ValueError(f"{name}: expected lengths that sum to {rows}, got {sum(lens)}")
-    return (B.C.c_int32 * n)(*lens), n
+    """Host int32 lengths that sum to `rows` -> (the array, to be kept until the call is made, its address, count)."""
+    a = array("i", lens)
+    if rows is not None and sum(a) != rows:
+        raise ValueError(f"{name}: expected lengths that sum to {rows}, got {sum(a)}")
+    return a, a.buffer_info()[0], len(a)
 
 
-def _space(nbytes: int, device: torch.device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _spaced(device: torch.device, where: str, likely: bool, need, call) -> None:
+    """call(workspace address or None, its bytes) with a workspace of need() bytes where it asks for
+    one (likely: it will). A call that lacks it has enqueued nothing."""
+    st = B.MTE_E_CAPACITY if likely else call(None, 0)
+    if st == B.MTE_E_CAPACITY:
+        n = need()
+        ws = torch.empty(n, dtype=torch.uint8, device=device) if n else None
+        st = call(ws.data_ptr() if n else None, n)
+    B._check(st, where)
 
 
 def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: Sequence[int], kv_lens: Sequence[int],
@@ -114,11 +128,11 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: S
     sk, sv = _rows("k", k, dtype, hkv, d, dev), _rows("v", v, dtype, hkv, d, dev)
     if v.shape[0] != k.shape[0]:
         raise ValueError(f"v: expected {k.shape[0]} rows, got {v.shape[0]}")
-    ql, n_q = _lens("q_lens", q_lens, q.shape[0])
-    kl, n_kv = _lens("kv_lens", kv_lens, k.shape[0])
-    if kv_index is not None and len(kv_index) != n_q:
-        raise ValueError(f"kv_index: expected {n_q} entries, got {len(kv_index)}")
-    idx = None if kv_index is None else (B.C.c_int32 * n_q)(*kv_index)
+    q_keep, ql, n_q = _lens("q_lens", q_lens, q.shape[0])
+    kv_keep, kl, n_kv = _lens("kv_lens", kv_lens, k.shape[0])
+    idx_keep, idx, n_idx = (None, None, n_q) if kv_index is None else _lens("kv_index", kv_index, None)
+    if n_idx != n_q:
+        raise ValueError(f"kv_index: expected {n_q} entries, got {n_idx}")
     if key_mask is not None:
         if not isinstance(key_mask, torch.Tensor) or key_mask.dtype not in (torch.uint8, torch.bool) or \
                 key_mask.device != dev or tuple(key_mask.shape) != (k.shape[0],) or not key_mask.is_contiguous():
@@ -131,12 +145,12 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: S
 
     def call(st):
         o = torch.empty((q.shape[0], hq, d), dtype=dtype, device=dev) if out is None else out
-        shape = B.mte_attn_shape(hq, hkv, d, _DTYPE[dtype], sc, *sq, *sk, *sv, *((hq * d, d) if so is None else so))
-        need = B.mte_cross_attention_workspace(shape, ql, n_q, kl, n_kv, idx)
-        ws = _space(need, dev)
-        B.mte_cross_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                              None if key_mask is None else key_mask.data_ptr(), ql, n_q, kl, n_kv, idx, o.data_ptr(),
-                              None if ws is None else ws.data_ptr(), need, st)
+        shape = B.ATTN_SHAPE.pack(hq, hkv, d, _DTYPE[dtype], sc, *sq, *sk, *sv, *((hq * d, d) if so is None else so))
+        _spaced(dev, "mte_cross_attention", False,
+                lambda: B.mte_cross_attention_workspace(shape, ql, n_q, kl, n_kv, idx),
+                lambda ws, n: B.lib.mte_cross_attention(
+                    shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if key_mask is None else key_mask.data_ptr(),
+                    ql, n_q, kl, n_kv, idx, o.data_ptr(), ws, n, st))
         return o
     return _on(dev, stream, (q, k, v, key_mask, out), call)
 
@@ -161,7 +175,7 @@ def kv8_cache(n_blocks: int, n_kv_heads: int, head_dim: int, device="cuda") -> K
 
 
 def _cache(cache, table, kv_lens, n: int, dev: torch.device):
-    """Checks a cache with the table and lengths of n sequences -> (mte_kv8, width, table row)."""
+    """Checks a cache with the table and lengths of n sequences -> (mte_kv8 as bytes, heads, head_dim, width, table row)."""
     kc, vc, sc = cache
     for name, t, dt in (("k_codes", kc, torch.uint8), ("v_codes", vc, torch.uint8), ("scales", sc, torch.float32)):
         if not isinstance(t, torch.Tensor) or t.dtype != dt or t.device != dev or not t.is_contiguous():
@@ -179,21 +193,19 @@ def _cache(cache, table, kv_lens, n: int, dev: torch.device):
     if not isinstance(kv_lens, torch.Tensor) or kv_lens.dtype != torch.int32 or kv_lens.device != dev or \
             tuple(kv_lens.shape) != (n,) or not kv_lens.is_contiguous():
         raise ValueError(f"kv_lens: expected a contiguous int32 tensor of {n} lengths on {dev}")
-    return B.mte_kv8(kc.data_ptr(), vc.data_ptr(), sc.data_ptr(), nb, h, d), table.shape[1], table.stride(0)
+    return B.KV8.pack(kc.data_ptr(), vc.data_ptr(), sc.data_ptr(), nb, h, d), h, d, table.shape[1], table.stride(0)
 
 
 def kv8_append(cache, table: torch.Tensor, kv_lens: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                new_lens: Sequence[int], stream: Optional[torch.cuda.Stream] = None) -> None:
     """mte_kv8_append: rows k, v [sum(new_lens), Hkv, d] become the newest new_lens[i] tokens of each
     sequence, whose lengths afterwards are kv_lens (int32, device); table int32 [n, blocks], device."""
-    n = len(new_lens)
     if not isinstance(k, torch.Tensor) or k.dim() != 3 or not k.is_cuda or k.dtype not in _DTYPE:
         raise ValueError("k: expected a [tokens, heads, head_dim] bf16 or fp32 tensor on the GPU")
     dev = k.device
-    c, width, row = _cache(cache, table, kv_lens, n, dev)
-    sk = _rows("k", k, k.dtype, c.n_kv_heads, c.head_dim, dev)
-    sv = _rows("v", v, k.dtype, c.n_kv_heads, c.head_dim, dev)
-    lens, _ = _lens("new_lens", new_lens, k.shape[0])
+    keep, lens, n = _lens("new_lens", new_lens, k.shape[0])
+    c, h, d, width, row = _cache(cache, table, kv_lens, n, dev)
+    sk, sv = _rows("k", k, k.dtype, h, d, dev), _rows("v", v, k.dtype, h, d, dev)
     if v.shape[0] != k.shape[0]:
         raise ValueError(f"v: expected {k.shape[0]} rows, got {v.shape[0]}")
     _on(dev, stream, (*cache, table, kv_lens, k, v),
@@ -208,15 +220,15 @@ def kv8_read(cache, table: torch.Tensor, kv_lens: torch.Tensor, counts: Sequence
     if dtype not in _DTYPE:
         raise ValueError("dtype: expected torch.bfloat16 or torch.float32")
     dev = cache[0].device
-    c, width, row = _cache(cache, table, kv_lens, len(counts), dev)
-    lens, n = _lens("counts", counts, None)
-    total = sum(counts)
-    if n and min(counts) < 0:
+    keep, lens, n = _lens("counts", counts, None)
+    c, h, d, width, row = _cache(cache, table, kv_lens, n, dev)
+    total = sum(keep)
+    if n and min(keep) < 0:
         raise ValueError("counts: expected lengths of 0 or more")
 
     def call(st):
-        k = torch.empty((total, c.n_kv_heads, c.head_dim), dtype=dtype, device=dev)
-        v = torch.empty_like(k)
+        k = torch.empty((total, h, d), dtype=dtype, device=dev)
+        v = torch.empty((total, h, d), dtype=dtype, device=dev)
         B.mte_kv8_read(c, table.data_ptr(), width, row, kv_lens.data_ptr(), lens, n, k.data_ptr(), v.data_ptr(),
                        _DTYPE[dtype], st)
         return k, v
@@ -231,9 +243,9 @@ def kv8_attention(q: torch.Tensor, cache, table: torch.Tensor, kv_lens: torch.Te
     (append its own token first). The work is split for sequences as long as the table is wide:
     a narrower view table[:, :m] serves shorter ones better."""
     hq, d, dtype, dev = _query(q)
-    c, width, row = _cache(cache, table, kv_lens, len(q_lens), dev)
-    sq = _rows("q", q, dtype, hq, c.head_dim, dev)
-    lens, n = _lens("q_lens", q_lens, q.shape[0])
+    keep, lens, n = _lens("q_lens", q_lens, q.shape[0])
+    c, hkv, dc, width, row = _cache(cache, table, kv_lens, n, dev)
+    sq = _rows("q", q, dtype, hq, dc, dev)
     so = None
     if out is not None:
         so = _rows("out", out, dtype, hq, d, dev)
@@ -242,12 +254,12 @@ def kv8_attention(q: torch.Tensor, cache, table: torch.Tensor, kv_lens: torch.Te
 
     def call(st):
         o = torch.empty((q.shape[0], hq, d), dtype=dtype, device=dev) if out is None else out
-        shape = B.mte_attn_shape(hq, c.n_kv_heads, d, _DTYPE[dtype], sc, *sq, 0, 0, 0, 0,
-                                 *((hq * d, d) if so is None else so))
-        need = B.mte_kv8_attention_workspace(shape, lens, n, width)
-        ws = _space(need, dev)
-        B.mte_kv8_attention(shape, c, table.data_ptr(), width, row, kv_lens.data_ptr(), q.data_ptr(), lens, n,
-                            1 if causal else 0, o.data_ptr(), None if ws is None else ws.data_ptr(), need, st)
+        shape = B.ATTN_SHAPE.pack(hq, hkv, d, _DTYPE[dtype], sc, *sq, 0, 0, 0, 0,
+                                  *((hq * d, d) if so is None else so))
+        _spaced(dev, "mte_kv8_attention", width > 16, lambda: B.mte_kv8_attention_workspace(shape, lens, n, width),
+                lambda ws, nb: B.lib.mte_kv8_attention(shape, c, table.data_ptr(), width, row, kv_lens.data_ptr(),
+                                                       q.data_ptr(), lens, n, 1 if causal else 0, o.data_ptr(), ws, nb,
+                                                       st))
         return o
     return _on(dev, stream, (q, *cache, table, kv_lens, out), call)
 
@@ -283,6 +295,7 @@ def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = Non
             raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {C} values on {dev}")
     xi, xr, px = _pixels("x", x)
     n = x.shape[0]
+    oi = orow = 0
     if out is not None:
         if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != dtype or out.device != dev:
             raise ValueError(f"out: expected a {dtype} tensor of shape {tuple(x.shape)} on {dev}")
@@ -291,12 +304,14 @@ def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = Non
             raise ValueError("out: pixels or images overlap")
 
     def call(st):
-        y = torch.empty(x.shape, dtype=dtype, device=dev) if out is None else out
-        yi, yr, _ = _pixels("out", y)
-        need = B.mte_group_norm_workspace(n, px, C, groups, _DTYPE[dtype])
-        ws = _space(need, dev)
-        B.mte_group_norm(x.data_ptr(), xr, xi, n, px, C, groups, None if gamma is None else gamma.data_ptr(),
-                         None if beta is None else beta.data_ptr(), eps, _ACT[act], _DTYPE[dtype], y.data_ptr(), yr, yi,
-                         None if ws is None else ws.data_ptr(), need, st)
+        if out is None:
+            y, yi, yr = torch.empty(x.shape, dtype=dtype, device=dev), px * C, C
+        else:
+            y, yi, yr = out, oi, orow
+        _spaced(dev, "mte_group_norm", False, lambda: B.mte_group_norm_workspace(n, px, C, groups, _DTYPE[dtype]),
+                lambda ws, nb: B.lib.mte_group_norm(
+                    x.data_ptr(), xr, xi, n, px, C, groups, None if gamma is None else gamma.data_ptr(),
+                    None if beta is None else beta.data_ptr(), eps, _ACT[act], _DTYPE[dtype], y.data_ptr(), yr, yi, ws,
+                    nb, st))
         return y
     return _on(dev, stream, (x, gamma, beta, out), call)

@@ -140,8 +140,8 @@ int mte_cross_attention(const mte_attn_shape *shape, const void *q, const void *
   if (nk > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return MTE_E_INVALID;
   AttnProblem p = problem(*shape, q_lens, n_q);
   const int64_t need = cross_workspace(p, kv_lens, n_kv, kv_index);
-  if (need > 0 && (!workspace || !aligned16(workspace))) return MTE_E_INVALID;
   if (workspace_bytes < need) return MTE_E_CAPACITY;
+  if (need > 0 && (!workspace || !aligned16(workspace))) return MTE_E_INVALID;
   p.c.q = q;
   p.c.out = out;
   p.c.ws = (float *)workspace;
@@ -206,8 +206,8 @@ int mte_kv8_attention(const mte_attn_shape *shape, const mte_kv8 *cache, const i
   if (!q || !out || !aligned16(q) || !aligned16(out)) return MTE_E_INVALID;
   AttnProblem p = problem(*shape, q_lens, n);
   const int64_t need = kv8_workspace(p, table_width);
-  if (need > 0 && (!workspace || !aligned16(workspace))) return MTE_E_INVALID;
   if (workspace_bytes < need) return MTE_E_CAPACITY;
+  if (need > 0 && (!workspace || !aligned16(workspace))) return MTE_E_INVALID;
   p.c.q = q;
   p.c.out = out;
   p.c.ws = (float *)workspace;
@@ -241,8 +241,8 @@ int mte_group_norm(const void *x, int64_t x_row, int64_t x_image, int32_t n, int
   if (!x || !y || (uintptr_t)x % es || (uintptr_t)y % es || (uintptr_t)gamma % es || (uintptr_t)beta % es)
     return MTE_E_INVALID;
   const int64_t need = group_norm_workspace(n, pixels, channels, groups, dtype);
-  if (need > 0 && (!workspace || !aligned16(workspace))) return MTE_E_INVALID;
   if (workspace_bytes < need) return MTE_E_CAPACITY;
+  if (need > 0 && (!workspace || !aligned16(workspace))) return MTE_E_INVALID;
   GroupNormArgs a{x, gamma, beta, y, (float *)workspace, x_row, x_image, y_row, y_image, n, pixels, channels, groups,
                   act, eps};
   return hip(launch_group_norm(a, dtype, stream));

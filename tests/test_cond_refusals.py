@@ -191,4 +191,4 @@ def test_binding_raises(B):
         B.mte_group_norm(P, 320, 0, 1, 64, 320, 33, None, None, 1e-5, 0, 1, P, 320, 0, None, 0, None)
     assert e.value.status == INVALID
     with pytest.raises(B.MteError):
-        B.mte_kv8_attention_workspace(_shape(B, d=80), B._i32([1]), 1, 4)
+        B.mte_kv8_attention_workspace(ctypes.byref(_shape(B, d=80)), B._i32([1]), 1, 4)
