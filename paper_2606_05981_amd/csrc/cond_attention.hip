@@ -38,6 +38,7 @@ template <> struct QFrag<bf16> { typedef bf16x8 type; };
 template <> struct QFrag<float> { typedef f32x4 type; };
 
 constexpr int kThreads = 256;
+constexpr int kMaxParts = 512;                      // of a key range
 
 __device__ __forceinline__ int find_seq(const CondSeq *seq, int n, int tile) {
   int lo = 0, hi = n - 1;
@@ -907,25 +908,82 @@ __device__ __forceinline__ BlockRef block_ref(const Kv8View &c, int id, int g) {
 // Least blocks of a split: below that a partial result costs more than its keys.
 constexpr int kRowsLeast = 8, kTilesLeast = 4;
 
-// Few rows (at most 32 a tile): bound by the codes that stream in. Each of the four waves
+// How the few-row kernel cuts its sequences, of lengths only the device knows, into parts of equal
+// work: all blocks of the launch over `target` parts (for each kv head) give the blocks of one, every
+// sequence has as many as it fills (one at least), and part `at` is found by a running sum over the
+// sequences. Every wave computes the same.
+struct Cut { int seq, lo, hi, first, used; };       // blocks [lo, hi) of a sequence; its parts: first .. first + used - 1
+__device__ __forceinline__ int wave_scan(int x, int lane) {   // inclusive
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d, kWave);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+// by_part: the part is `at`; else the cut of sequence `at` as a whole (lo, hi unused).
+__device__ __forceinline__ Cut cut_of(const Kv8AttnArgs &a, int target, int at, bool by_part, int lane) {
+  static_assert(kCondSeqs == 128, "two sequences a lane");
+  int nb[2], c[2];
+  double total = 0;                                 // up to 128 sequences of 2^26 blocks
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int i = lane + 64 * u;
+    nb[u] = 0;
+    if (i < a.n_seq) nb[u] = (min(max(a.c.kv_lens[a.seq[i].k0], 0), a.c.width * 32) + 31) >> 5;
+    total += nb[u];
+  }
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) total += __shfl_xor(total, m, kWave);
+  const int per = max((int)min(ceil(total / target), 0x1p26), kRowsLeast);
+  int run[2], before = 0;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    c[u] = lane + 64 * u < a.n_seq ? max(1, (nb[u] + per - 1) / per) : 0;
+    run[u] = before + wave_scan(c[u], lane);
+    before = __shfl(run[u], 63, kWave);
+  }
+  Cut w{-1, 0, 0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int i = lane + 64 * u, first = run[u] - c[u];
+    const uint64_t hit = __ballot(by_part ? c[u] > 0 && first <= at && at < run[u] : i == at);
+    if (hit) {                                      // wave-uniform
+      const int l = __builtin_ctzll(hit);
+      w.seq = l + 64 * u;
+      w.first = __shfl(first, l, kWave);
+      w.used = __shfl(c[u], l, kWave);
+      const int n = __shfl(nb[u], l, kWave);
+      w.lo = min((at - w.first) * per, n);
+      w.hi = min(w.lo + per, n);
+    }
+  }
+  w.seq = __builtin_amdgcn_readfirstlane(w.seq);
+  w.lo = __builtin_amdgcn_readfirstlane(w.lo);
+  w.hi = __builtin_amdgcn_readfirstlane(w.hi);
+  w.first = __builtin_amdgcn_readfirstlane(w.first);
+  w.used = __builtin_amdgcn_readfirstlane(w.used);
+  return w;
+}
+
+// Few rows (at most 32 a sequence): bound by the codes that stream in. Each of the four waves
 // takes every fourth block of the split's range and loads its codes straight into MFMA operand
 // order, 16 bytes a lane and 1 KB a load, the next block's while one is computed.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(Kv8AttnArgs a) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(Kv8AttnArgs a, int target) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32;
   extern __shared__ u32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
-  const Unit un = unit_of(a.hkv);
-  const int tile = un.tile, g = un.g, split = blockIdx.y;
-  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
-  const int rows = sq.q_len * a.rep, r0 = (tile - sq.tile0) * 32, r = r0 + lrow;
+  const int part = (int)blockIdx.x / a.hkv, g = (int)blockIdx.x - part * a.hkv;
+  const Cut span = cut_of(a, target, part, true, lane);
+  if (span.seq < 0) return;                         // fewer parts than the grid has room for
+  const CondSeq sq = a.seq[span.seq];
+  const int rows = sq.q_len * a.rep, r = lrow;
   const bool live = r < rows;
   const int qi = live ? r / a.rep : 0;
   const int head = g * a.rep + (live ? r % a.rep : 0);
-  const Seen seen = seen_of(a, sq, r0 / a.rep, (min(r0 + 32, rows) - 1) / a.rep, qi);
-  const Span span = split_span((seen.tile_hi + 31) >> 5, a.n_split, split, kRowsLeast);
-  if (split >= span.used) return;
+  const Seen seen = seen_of(a, sq, 0, sq.q_len - 1, qi);
 
   const int32_t *tab = a.c.table + (int64_t)sq.k0 * a.c.table_row;
   auto id_at = [&](int b) { return b < span.hi ? uniform_at(tab, b) : -1; };
@@ -989,7 +1047,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
   if (span.used == 1)
     store_rows<T, ND>(a, st, top, live, sq.q0 + qi, head, lane);
   else
-    store_part<ND>(a, st, top, live, tile, g, split, lrow, lane);
+    store_part<ND>(a, st, top, live, part, g, 0, lrow, lane);
 }
 
 // Many rows: four waves of 32 rows; two blocks of codes a step are widened once per
@@ -1208,59 +1266,102 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
 
 // ---- joining splits -----------------------------------------------------------------------------
 //
-// out[row] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M = max m_s over the splits that a
-// unit (tile, kv head) used; units of one split wrote their rows themselves. A row is DP / 4
-// lanes of four d.
+// out[row] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M = max m_s over the parts that a unit
+// (tile or sequence, kv head) used; units of one part wrote their rows themselves. A workgroup a row,
+// DP / 4 lanes of four d times as many teams over the parts as it holds, so that the parts of a
+// row are read in one go (64 parts read by one team each after the other: 12 us).
+constexpr int kMostParts = kMaxParts + 1;
+template <typename T, int DP>
+__device__ __forceinline__ void join_row(const AttnCommon &a, const CondSeq &sq, int g, int r, int64_t at, int64_t step,
+                                         int used) {
+  constexpr int LPR = DP / 4, TEAMS = kThreads / LPR;
+  __shared__ float weight[kMostParts];
+  __shared__ float red[4];
+  __shared__ f32x4 sums[TEAMS][LPR];
+  const int tid = threadIdx.x, c = (tid % LPR) * 4, team = tid / LPR;
+  const float *ml = a.ws + a.ws_ml + at * 2, *o = a.ws + at * DP + c;
+  float M = -INFINITY;
+  for (int s = tid; s < used; s += kThreads) {
+    weight[s] = ml[s * step * 2];
+    M = fmaxf(M, weight[s]);
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) M = warp_max_xor(M, k);
+  if ((tid & 63) == 0) red[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float mr = M == -INFINITY ? 0.f : M;
+  __syncthreads();
+  float l = 0.f;
+  for (int s = tid; s < used; s += kThreads) {
+    const float f = __builtin_amdgcn_exp2f(weight[s] - mr);
+    weight[s] = f;
+    l += f * ml[s * step * 2 + 1];
+  }
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) l = warp_sum_xor(l, k);
+  if ((tid & 63) == 0) red[tid >> 6] = l;
+  __syncthreads();
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = team; s < used; s += TEAMS) {
+    const f32x4 x = *(const f32x4 *)(o + s * step * DP);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += weight[s] * x[e];
+  }
+  sums[team][tid % LPR] = acc;
+  __syncthreads();
+  if (team > 0 || c >= a.d) return;
+#pragma unroll
+  for (int k = 1; k < TEAMS; ++k) {
+    const f32x4 x = sums[k][tid];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += x[e];
+  }
+  l = red[0] + red[1] + red[2] + red[3];
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  T *row = (T *)a.out + (int64_t)(sq.q0 + r / a.rep) * a.o_row + (int64_t)(g * a.rep + r % a.rep) * a.o_head;
+  if constexpr (sizeof(T) == 4)
+    *(f32x4 *)(row + c) = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+  else
+    *(bf16x4 *)(row + c) = bf16x4{(bf16)(acc[0] * inv), (bf16)(acc[1] * inv), (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
+}
+// Grid: x = (tile, kv head), y = row of the tile.
 template <typename T, int DP, typename A, typename SPAN>
-__device__ __forceinline__ void join_body(const A &a, int TR, SPAN used_of) {
-  constexpr int LPR = DP / 4;
+__device__ __forceinline__ void join_tile(const A &a, int TR, SPAN used_of) {
   const Unit un = unit_of(a.hkv);
-  const int tile = un.tile, g = un.g;
-  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
-  const int rows = sq.q_len * a.rep, r0 = (tile - sq.tile0) * TR;
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, un.tile)];
+  const int rows = sq.q_len * a.rep, r0 = (un.tile - sq.tile0) * TR, i = blockIdx.y;
+  if (r0 + i >= rows) return;
   const int used = used_of(sq, (min(r0 + TR, rows) - 1) / a.rep);
   if (used == 1) return;
-  const int c = (threadIdx.x % LPR) * 4;
-  for (int i = threadIdx.x / LPR; i < min(TR, rows - r0); i += kThreads / LPR) {
-    const int64_t at = (((int64_t)tile * a.hkv + g) * a.n_split) * a.ws_rows + i;
-    const float *ml = a.ws + a.ws_ml + at * 2, *o = a.ws + at * DP + c;
-    float M = -INFINITY;
-    for (int s = 0; s < used; ++s) M = fmaxf(M, ml[(int64_t)s * a.ws_rows * 2]);
-    const float mr = M == -INFINITY ? 0.f : M;
-    float l = 0.f;
-    f32x4 acc{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < used; ++s) {
-      const float f = __builtin_amdgcn_exp2f(ml[(int64_t)s * a.ws_rows * 2] - mr);
-      l += f * ml[(int64_t)s * a.ws_rows * 2 + 1];
-      const f32x4 x = *(const f32x4 *)(o + (int64_t)s * a.ws_rows * DP);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += f * x[e];
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    const int r = r0 + i;
-    T *row = (T *)a.out + (int64_t)(sq.q0 + r / a.rep) * a.o_row + (int64_t)(g * a.rep + r % a.rep) * a.o_head;
-    if (c < a.d) {
-      if constexpr (sizeof(T) == 4)
-        *(f32x4 *)(row + c) = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
-      else
-        *(bf16x4 *)(row + c) = bf16x4{(bf16)(acc[0] * inv), (bf16)(acc[1] * inv), (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
-    }
-  }
+  join_row<T, DP>(a, sq, un.g, r0 + i, ((int64_t)un.tile * a.hkv + un.g) * a.n_split * a.ws_rows + i, a.ws_rows, used);
 }
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads) void k_cross_join(CrossArgs a, int TR, int KT, int least) {
-  join_body<T, DP>(a, TR, [&](const CondSeq &sq, int) {
+  join_tile<T, DP>(a, TR, [&](const CondSeq &sq, int) {
     return split_span((sq.k_len + KT - 1) / KT, a.n_split, 0, least).used;
   });
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void k_kv8_join(Kv8AttnArgs a, int TR, int least) {
-  join_body<T, DP>(a, TR, [&](const CondSeq &sq, int last_tok) {
-    return split_span((seen_of(a, sq, 0, last_tok, 0).tile_hi + 31) >> 5, a.n_split, 0, least).used;
+__global__ __launch_bounds__(kThreads) void k_kv8_tiles_join(Kv8AttnArgs a) {
+  join_tile<T, DP>(a, 128, [&](const CondSeq &sq, int last_tok) {
+    return split_span((seen_of(a, sq, 0, last_tok, 0).tile_hi + 31) >> 5, a.n_split, 0, kTilesLeast).used;
   });
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads) void k_kv8_rows_join(Kv8AttnArgs a, int target) {
+  const Unit un = unit_of(a.hkv);
+  const CondSeq sq = a.seq[un.tile];
+  const int i = blockIdx.y;
+  if (i >= sq.q_len * a.rep) return;
+  const Cut w = cut_of(a, target, un.tile, false, threadIdx.x & 63);
+  if (w.used == 1) return;
+  join_row<T, DP>(a, sq, un.g, i, ((int64_t)w.first * a.hkv + un.g) * a.ws_rows + i, (int64_t)a.hkv * a.ws_rows,
+                  w.used);
 }
 
 // ---- plans --------------------------------------------------------------------------------------
@@ -1272,11 +1373,12 @@ struct Plan {
   enum { FEW, COPIES, STREAM, RESIDENT } kind = FEW;
   int TR = 0, KT = 0, n_split = 1, ws_rows = 0;
   int least = 0;                                    // key tiles of a split
+  int target = 0;                                   // cached attention with few rows: parts (cut_of), 0: none
   int nw = 4, lds = 0;                              // RESIDENT: waves, LDS bytes,
   bool box = false;                                 // and whether they hold kBox a wave
   int64_t tiles = 0;                                // of the launch (of kCondSeqs sequences) with the most
   int64_t floats(int hkv, int dp) const {
-    return n_split > 1 ? tiles * hkv * n_split * (int64_t)ws_rows * (dp + 2) : 0;
+    return n_split > 1 || target > 0 ? tiles * hkv * n_split * (int64_t)ws_rows * (dp + 2) : 0;
   }
   int64_t ml(int hkv, int dp) const { return tiles * hkv * n_split * (int64_t)ws_rows * dp; }
 };
@@ -1285,6 +1387,7 @@ int pad_d(int d) { return d <= 64 ? 64 : 128; }
 
 // Workgroups that fill the 256 compute units with two each; a launch below it splits long key ranges.
 constexpr int kFill = 512;
+static_assert(kFill <= kMaxParts, "splits of one unit");
 
 }  // namespace
 
@@ -1409,7 +1512,7 @@ static hipError_t run_cross(const CrossArgs &a, int tiles, const Plan &pl, hipSt
   if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
   hipLaunchKernelGGL(kern, grid, dim3(kThreads), lds, s, a);
   if ((e = hipGetLastError()) != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL((k_cross_join<T, DP>), dim3(tiles * a.hkv), dim3(kThreads), 0, s, a, pl.TR, pl.KT,
+  hipLaunchKernelGGL((k_cross_join<T, DP>), dim3(tiles * a.hkv, a.ws_rows), dim3(kThreads), 0, s, a, pl.TR, pl.KT,
                      pl.least);
   return hipGetLastError();
 }
@@ -1499,9 +1602,13 @@ static Plan kv8_plan(const AttnProblem &p, int width, bool few) {
   const int64_t units = fill_tiles(p, pl, mine) * p.c.hkv;
   if (pl.kind == Plan::RESIDENT) return pl;
   pl.ws_rows = (int)std::min<int64_t>(pl.TR, most);
-  if (few)
-    pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / units, ceil_div(width, 2 * kRowsLeast)));
-  else if (units < kFill)
+  if (few) {
+    // parts for each kv head: of kFill workgroups, no more than the widest tables fill; the
+    // partial results of all that the lengths may lead to
+    pl.target = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / p.c.hkv, pl.tiles * ceil_div(width, kRowsLeast)));
+    if (ceil_div(width, kRowsLeast) > 1) pl.tiles += pl.target;
+    else pl.target = 0;                             // no sequence is cut
+  } else if (units < kFill)
     pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / units, ceil_div(width, 2 * kTilesLeast)));
   return pl;
 }
@@ -1521,14 +1628,17 @@ static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, const Plan &pl, hipSt
     hipLaunchKernelGGL(kern, grid, dim3(64 * pl.nw), pl.lds, s, a, pl.TR);
     return hipGetLastError();
   }
-  const bool few = pl.kind == Plan::FEW;
-  if (few)
-    hipLaunchKernelGGL((k_kv8_rows<T, D>), grid, dim3(kThreads), 3 * (2 + D / 2) * 64 * 4, s, a);
-  else
-    hipLaunchKernelGGL((k_kv8_tiles<T, D>), grid, dim3(kThreads), 2 * 4 * (D / 32) * 64 * 16, s, a);
+  if (pl.kind == Plan::FEW) {                       // a tile is a sequence
+    const int target = std::max(pl.target, 1);
+    const dim3 parts((tiles + (pl.target > 0 ? target : 0)) * a.hkv);
+    hipLaunchKernelGGL((k_kv8_rows<T, D>), parts, dim3(kThreads), 3 * (2 + D / 2) * 64 * 4, s, a, target);
+    if ((e = hipGetLastError()) != hipSuccess || pl.target == 0) return e;
+    hipLaunchKernelGGL((k_kv8_rows_join<T, D>), dim3(tiles * a.hkv, a.ws_rows), dim3(kThreads), 0, s, a, target);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((k_kv8_tiles<T, D>), grid, dim3(kThreads), 2 * 4 * (D / 32) * 64 * 16, s, a);
   if ((e = hipGetLastError()) != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL((k_kv8_join<T, D>), dim3(tiles * a.hkv), dim3(kThreads), 0, s, a, pl.TR,
-                     few ? kRowsLeast : kTilesLeast);
+  hipLaunchKernelGGL((k_kv8_tiles_join<T, D>), dim3(tiles * a.hkv, a.ws_rows), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
