@@ -1605,7 +1605,8 @@ static Plan kv8_plan(const AttnProblem &p, int width, bool few) {
   if (few) {
     // parts for each kv head: of kFill workgroups, no more than the widest tables fill; the
     // partial results of all that the lengths may lead to
-    pl.target = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / p.c.hkv, pl.tiles * ceil_div(width, kRowsLeast)));
+    const int fill = p.dtype == MTE_BF16 ? kFill : kFill / 2;   // fp32: one workgroup a compute unit
+    pl.target = (int)std::max<int64_t>(1, std::min<int64_t>(fill / p.c.hkv, pl.tiles * ceil_div(width, kRowsLeast)));
     if (ceil_div(width, kRowsLeast) > 1) pl.tiles += pl.target;
     else pl.target = 0;                             // no sequence is cut
   } else if (units < kFill)
