@@ -375,8 +375,8 @@ __global__ __launch_bounds__(TH) void k_gn_apply(GnArgs a) {
 
 // Two launches: workgroups that keep the chip busy, most parts of an image (every workgroup of the
 // second launch reads those of its groups), batches of its pixels a thread of the second launch
-// takes. One launch: the largest slab.
-constexpr int kFill = 512, kParts = 64, kTurns = 4, kSlab = 128 * 1024;
+// takes. One launch: the largest slab, and what a workgroup can have in all.
+constexpr int kFill = 512, kParts = 64, kTurns = 4, kSlab = 128 * 1024, kLds = 160 * 1024;
 
 struct GnPlan {
   int V, TH, gb, ncol, ppi, chunk, apply, colparts, parts;
@@ -388,6 +388,12 @@ int vec_of(int n, int align, int esize) {
   int v = 16 / esize;
   while (v > 1 && (n % v || align % v)) v >>= 1;
   return v;
+}
+
+// LDS of group_sums: an entry per pixel lane and column, or channel where a column spans groups.
+int sums_bytes(int gb, int cpg, int v, int ncol, int ppi) {
+  const int entries = (gb == 1 || cpg % v == 0 ? 1 : v) * ncol * (ppi | 1);
+  return ((gb + std::max(entries, 16)) * 4 + 15) & ~15;
 }
 
 // `align`: the elements that every address and stride is a multiple of.
@@ -408,7 +414,7 @@ GnPlan plan_of(int n, int pixels, int channels, int groups, int esize, int align
       if (ncol > th) break;
       const int ppi = std::min(th / ncol, pixels);
       const int64_t bytes = ((int64_t)pixels + ppi - 1) / ppi * th * v * esize, wgs = (int64_t)n * (groups / gb);
-      if (bytes > kSlab || (wgs < (run == 64 ? 64 : 32) && bytes > 16384)) break;
+      if (bytes > kSlab || bytes + sums_bytes(gb, cpg, v, ncol, ppi) > kLds || (wgs < (run == 64 ? 64 : 32) && bytes > 16384)) break;
       return GnPlan{v, th, gb, ncol, ppi, pixels, pixels, 1, 1, true};
     }
   }
@@ -446,8 +452,7 @@ template <typename K> hipError_t allow_lds(K kern, int bytes) {
 
 template <typename T, int V>
 hipError_t run(const GnArgs &a, const GnPlan &p, int esize, hipStream_t s) {
-  const int entries = (a.same ? 1 : V) * std::min(p.ncol, p.TH) * (p.ppi | 1);
-  const int sums = ((p.gb + std::max(entries, 16)) * 4 + 15) & ~15, bundles = a.groups / p.gb;
+  const int sums = sums_bytes(p.gb, a.cpg, V, std::min(p.ncol, p.TH), p.ppi), bundles = a.groups / p.gb;
   hipError_t e;
   if (p.one) {
     auto kern = p.TH == 256 ? k_gn<T, V, 256> : k_gn<T, V, 1024>;

@@ -519,6 +519,8 @@ NORMS = [
     (2, (16, 16), 640, 32), (1, (64, 64), 320, 32), (2, (33, 31), 96, 32), (1, (64, 65), 33, 11),
     (1, (40, 40), 2560, 32), (1, (3, 3), 5120, 1), (2, (17, 1), 9000, 2), (1, (100, 100), 64, 1), (1, (64, 64), 5, 5),
     (4, (2, 3), 24, 4), (1, (128, 64), 32, 8),
+    # a full slab and sums per channel: together more than a workgroup's LDS
+    (8, (40, 40), 320, 32), (4, (40, 40), 96, 8),
 ]
 
 
