@@ -232,11 +232,13 @@ __device__ __forceinline__ void store_rows(const AttnCommon &a, Rows<ND> &st, fl
   }
 }
 
-// Partial state of row r of unit (tile, g) and split: O unnormalised (times vscale), m, l.
+// Partial state of row r of unit (tile, g) and split: O / l (times vscale: no larger than the values,
+// so that nothing overflows before the parts are joined), m, l.
 template <int ND>
 __device__ __forceinline__ void store_part(const AttnCommon &a, Rows<ND> &st, float vscale, bool live, int tile, int g,
                                            int split, int r, int lane) {
   const float l = st.l + __shfl_xor(st.l, 32, kWave);
+  const float inv = l > 0.f ? vscale / l : 0.f;
   if (!live) return;
   const int64_t at = (((int64_t)tile * a.hkv + g) * a.n_split + split) * a.ws_rows + r;
   float *o = a.ws + at * (32 * ND) + 4 * (lane >> 5);
@@ -244,8 +246,8 @@ __device__ __forceinline__ void store_part(const AttnCommon &a, Rows<ND> &st, fl
   for (int n = 0; n < ND; ++n)
 #pragma unroll
     for (int b = 0; b < 4; ++b)
-      *(f32x4 *)(o + 32 * n + 8 * b) = f32x4{st.o[n][4 * b] * vscale, st.o[n][4 * b + 1] * vscale,
-                                            st.o[n][4 * b + 2] * vscale, st.o[n][4 * b + 3] * vscale};
+      *(f32x4 *)(o + 32 * n + 8 * b) = f32x4{st.o[n][4 * b] * inv, st.o[n][4 * b + 1] * inv, st.o[n][4 * b + 2] * inv,
+                                            st.o[n][4 * b + 3] * inv};
   if (lane < 32) {
     float *ml = a.ws + a.ws_ml + at * 2;
     ml[0] = st.m;
@@ -1266,7 +1268,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
 
 // ---- joining splits -----------------------------------------------------------------------------
 //
-// out[row] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, M = max m_s over the parts that a unit
+// out[row] = sum_s w_s O_s / sum_s w_s, w_s = 2^(m_s - M) l_s, M = max m_s, over the parts that a unit
 // (tile or sequence, kv head) used; units of one part wrote their rows themselves. A workgroup a row,
 // DP / 4 lanes of four d times as many teams over the parts as it holds, so that the parts of a
 // row are read in one go (64 parts read by one team each after the other: 12 us).
@@ -1294,20 +1296,21 @@ __device__ __forceinline__ void join_row(const AttnCommon &a, const CondSeq &sq,
   __syncthreads();
   float l = 0.f;
   for (int s = tid; s < used; s += kThreads) {
-    const float f = __builtin_amdgcn_exp2f(weight[s] - mr);
-    weight[s] = f;
-    l += f * ml[s * step * 2 + 1];
+    weight[s] = __builtin_amdgcn_exp2f(weight[s] - mr) * ml[s * step * 2 + 1];
+    l += weight[s];
   }
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) l = warp_sum_xor(l, k);
   if ((tid & 63) == 0) red[tid >> 6] = l;
   __syncthreads();
+  l = red[0] + red[1] + red[2] + red[3];
+  const float inv = l > 0.f ? 1.f / l : 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int s = team; s < used; s += TEAMS) {
     const f32x4 x = *(const f32x4 *)(o + s * step * DP);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += weight[s] * x[e];
+    for (int e = 0; e < 4; ++e) acc[e] += weight[s] * inv * x[e];
   }
   sums[team][tid % LPR] = acc;
   __syncthreads();
@@ -1318,13 +1321,11 @@ __device__ __forceinline__ void join_row(const AttnCommon &a, const CondSeq &sq,
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += x[e];
   }
-  l = red[0] + red[1] + red[2] + red[3];
-  const float inv = l > 0.f ? 1.f / l : 0.f;
   T *row = (T *)a.out + (int64_t)(sq.q0 + r / a.rep) * a.o_row + (int64_t)(g * a.rep + r % a.rep) * a.o_head;
   if constexpr (sizeof(T) == 4)
-    *(f32x4 *)(row + c) = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    *(f32x4 *)(row + c) = acc;
   else
-    *(bf16x4 *)(row + c) = bf16x4{(bf16)(acc[0] * inv), (bf16)(acc[1] * inv), (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
+    *(bf16x4 *)(row + c) = bf16x4{(bf16)acc[0], (bf16)acc[1], (bf16)acc[2], (bf16)acc[3]};
 }
 // Grid: x = (tile, kv head), y = row of the tile.
 template <typename T, int DP, typename A, typename SPAN>

@@ -9,9 +9,10 @@ scale * sum |q| |k| of the row, both from the oracle:
    denominator: 2 (D + 2 u) A each;
  - sums over n keys, in fp32 and joined over splits: (n + 16) u A twice (O and l);
  - bf16: the probabilities' rounding u16 A and the result's u16 |o|; fp32: u |o|;
- - cache: bf16 calls round probabilities to fp16, 2^-11 A, and below 2^-22 of a row's largest by an
-   absolute 2^-33 (exponent offset 2^8 against fp16's 2^-25), a value of at most vmax each: n 2^-33
-   vmax; fp32 calls carry two fp16 terms: 2^-22 A and the same absolute part.
+ - cache: bf16 calls round probabilities to fp16, 2^-11 A, and small ones by half fp16's smallest
+   step, 2^-25, where the row's largest is held as 2^7 at least (it lies in [2^7, 2^15], so that the
+   reference may lag): 2^-25 / 2^7 = 2^-32 of it, on a value of at most vmax each: n 2^-32 vmax;
+   fp32 calls carry two fp16 terms: 2^-22 A and the same absolute part.
 """
 import sys
 
@@ -55,7 +56,7 @@ def _tol(ref, mag, reach, n, d, dtype, cached=0.0):
     D = (d + 4) * U * reach[..., None] + 2 * U
     t = 4 * D * mag + 2 * (n + 16) * U * mag
     if cached:
-        t = t + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * mag + n * 2.0 ** -33 * cached
+        t = t + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * mag + n * 2.0 ** -32 * cached
     elif dtype == "bf16":
         t = t + U16 * mag
     return t + (U16 if dtype == "bf16" else U) * (np.abs(ref) + t) + 1e-30
@@ -504,6 +505,26 @@ def test_kv8_many_sequences(torch, C):
         parts.append(O.attend(_f64(q[at:at + n]), k, v, np.ones((n, k.shape[0]), bool), 1 / 8))
         at += n
     _compare(got, *(np.concatenate([p[x] for p in parts]) for x in range(3)), 60, 64, "bf16", 8.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl", [([1], [4000]), ([40], [3000]), ([40], [64])])
+def test_kv8_largest_values(torch, C, ql, kl, dtype):
+    """Values next to fp32's largest: sums are kept in units of the scale, partial results as means."""
+    _say("cached, largest values", ql, kl, dtype)
+    h, d = 2, 64
+    cache = C.kv8_cache((kl[0] + 31) // 32, h, d)
+    table = torch.arange(cache.scales.shape[0], dtype=torch.int32, device="cuda")[None]
+    g = torch.Generator().manual_seed(90)
+    v = (torch.rand(kl[0], h, d, generator=g) * 2.9e38).cuda()
+    k = _randn(torch, 91, kl[0], h, d, dtype="f32")
+    kv = _i32(torch, kl)
+    C.kv8_append(cache, table, kv, k, v, kl)
+    q = _randn(torch, 92, sum(ql), 4, d, dtype=dtype)
+    got = C.kv8_attention(q, cache, table, kv, ql)
+    (kk, vv), = _held(torch, cache, table, kl)
+    ref = O.attend(_f64(q), kk, vv, np.ones((ql[0], kl[0]), bool), 1 / 8)
+    _compare(got, *ref, kl[0], d, dtype, np.abs(vv).max())
 
 
 # ---- group norm ---------------------------------------------------------------------------------
