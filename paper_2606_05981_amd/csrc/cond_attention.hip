@@ -513,8 +513,9 @@ __device__ __forceinline__ void attend_steps(Rows<ND> &st, int n, SC scores, MA 
     mask(i, s0);
     mask(i + 1, s1);
     const float ref = st.raise(fmaxf(max16(s0, -INFINITY) * factor(i), max16(s1, -INFINITY) * factor(i + 1)));
-    const P p0 = probs(i, s0, ref), p1 = probs(i + 1, s1, ref);
+    const P p0 = probs(i, s0, ref);                 // (may rescale O: before the block's values, after those before)
     values(i, p0);
+    const P p1 = probs(i + 1, s1, ref);
     values(i + 1, p1);
   }
   if (i < n) {
@@ -1147,8 +1148,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
     store_part<ND>(a, st, vr.top, live, tile, g, split, wave * 32 + lrow, lane);
 }
 
-// Many rows over a cache that fits LDS whole once widened: the counterpart of k_cross_res. Lane j holds
-// block j's scales and how many of its tokens count (none: no such block).
+// Many rows over a cache that fits LDS whole once widened. Lane j holds block j's scales and how many of
+// its tokens count (none: no such block). O is in units of the largest value scale so far, as in the
+// other kernels: one for all blocks, of which a causal row sees the first, would push that row's
+// probabilities below fp16.
 template <typename T, int D, int NW, bool BOX>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void k_kv8_res(Kv8AttnArgs a, int chunk) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32, NF = D / 8;
@@ -1194,10 +1197,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
       count = min(all.kv - lane * 32, 32);
     }
   }
-  float vref = vs;
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) vref = warp_max_xor(vref, m);
-  const float ratio = vs > 0.f ? vs / vref : 0.f;
   for (int j = wave; j < nk; j += NW) {
     const int id = uniform_at(tab, j);
     const bool ok = id >= 0 && id < a.c.n_blocks;
@@ -1240,6 +1239,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
     const Seen seen = seen_of(a, sq, r0 / a.rep, (min(r0 + 32, rows) - 1) / a.rep, r / a.rep);
     Rows<ND> st;
     st.init();
+    VRef vr;
     auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
     attend_steps<ND, CodeProbs<T>>(
         st, (seen.tile_hi + 31) >> 5,
@@ -1250,16 +1250,16 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
         },
         [&](int i) { return lane_of(ks, i); },
         [&](int i, const f32x16 &s, float ref) {
-          return code_probs<T>(s, lane_of(ks, i), ref - kPOff, lane_of(ratio, i), st.l);
+          return code_probs<T>(s, lane_of(ks, i), ref - kPOff, vr.ratio(st, lane_of(vs, i)), st.l);
         },
         [&](int i, const CodeProbs<T> &p) {
           const u32x4 *fr = codes + (i * NF + NK) * 64 + lane;
           code_values<T, ND>(st.o, p, [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(2 * n + f) * 64]); });
         });
     if constexpr (BOX) {
-      store_tile<T, ND>(a, st, vref, TileRows(a, sq, r0, rows), g, box, lane);
+      store_tile<T, ND>(a, st, vr.top, TileRows(a, sq, r0, rows), g, box, lane);
     } else {
-      store_rows<T, ND>(a, st, vref, q.live, q.tok, q.head, lane);
+      store_rows<T, ND>(a, st, vr.top, q.live, q.tok, q.head, lane);
       if (sizeof(T) == 2) q = qn;
       else if (more) load_own(r0 + NW * 32, q);
     }

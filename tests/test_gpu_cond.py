@@ -508,6 +508,27 @@ def test_kv8_many_sequences(torch, C):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,width", [(16, 40, None), (64, 64, None), (64, 64, 30)])
+def test_kv8_values_of_unseen_blocks(torch, C, ql, kl, width, dtype):
+    """A causal row's result does not depend on how large the values are that it does not see."""
+    _say("cached, values of unseen blocks", ql, kl, width, dtype)
+    h, d = 2, 64
+    v = torch.randn(kl, h, d, generator=torch.Generator().manual_seed(93))
+    v[32:] *= 2.0 ** 40
+    cache, table, kv, _, _ = _fill(torch, C, [kl], h, d, width=width)
+    k = _randn(torch, 94, kl, h, d)
+    C.kv8_append(cache, table, kv, k, v.to(torch.bfloat16).cuda(), [kl])
+    q = _randn(torch, 95, ql, 4, d, dtype=dtype)
+    got = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
+    (kk, vv), = _held(torch, cache, table, [kl])
+    see = np.arange(kl)[None] <= kl - ql + np.arange(ql)[:, None]
+    ref = O.attend(_f64(q), kk, vv, see, 1 / 8)
+    edge = 32 - (kl - ql)                         # rows before it see the first block only
+    for part, m in ((slice(0, edge), 32), (slice(edge, ql), kl)):
+        _compare(got[part], *(x[part] for x in ref), m, d, dtype, np.abs(vv[:m]).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("ql,kl", [([1], [4000]), ([40], [3000]), ([40], [64])])
 def test_kv8_largest_values(torch, C, ql, kl, dtype):
     """Values next to fp32's largest: sums are kept in units of the scale, partial results as means."""
