@@ -625,7 +625,8 @@ __device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, fl
 // Tiles: keys [32][NCH chunks], values the same, chunk c of row r at c ^ key_swz / value_chunk: whole
 // rows for the copies, free of bank conflicts for the operand reads. Rows past the end repeat the
 // last one; their scores are masked, and value rows that must not count (past the end, masked)
-// are overwritten with zeros by the wave that copied them.
+// are overwritten with zeros by the wave that copied them. Chunks past head_dim are not copied and
+// stay zero (a lane that skips a copy leaves its 16 bytes alone; no copy is skipped whole).
 // The ring's idle slots turn the rows (QTile): before the first barrier the last ones, after the
 // last barrier those that the last tile does not use.
 template <int NCH> __device__ __forceinline__ int key_swz(int r, int c) { return c ^ (r & (NCH - 1)); }
@@ -665,8 +666,8 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
       const int r = RPC * (wave * CP + i) + lane / NCH, p = lane % NCH;
       const int row = min(r, klen - 1 - t * 32);
       const int kc = key_swz<NCH>(r, p) * 8, vc = value_chunk<NCH, true>(r, p) * 8;
-      dma16(kb, (uint32_t)(row * (int)a.k_row + (kc < a.d ? kc : 0)) * 2u, to + i * 1024);
-      dma16(vb, (uint32_t)(row * (int)a.v_row + (vc < a.d ? vc : 0)) * 2u, to + (S::TILE + i * 64) * 16);
+      if (kc < a.d) dma16(kb, (uint32_t)(row * (int)a.k_row + kc) * 2u, to + i * 1024);
+      if (vc < a.d) dma16(vb, (uint32_t)(row * (int)a.v_row + vc) * 2u, to + (S::TILE + i * 64) * 16);
     }
   };
   const TileRows rw(a, sq, r0, rows);
@@ -684,6 +685,16 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
       qt.spread(box, j, lane);
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) qf[4 * j + kk] = __builtin_bit_cast(bf16x8, qt.chunk(box, 2 * kk + h, lane));
+    }
+  }
+  if (a.d < DP) {                                   // uniform
+    __syncthreads();                                // the rows are turned
+#pragma unroll
+    for (int i = 0; i < S::NB * CP; ++i) {          // the rows that this wave copies, of every slot
+      const int r = RPC * (wave * CP + i % CP) + lane / NCH, p = lane % NCH;
+      u32x4 *at = lds + (i / CP) * 2 * S::TILE + (wave * CP + i % CP) * 64 + lane;
+      if (key_swz<NCH>(r, p) * 8 >= a.d) at[0] = u32x4{0, 0, 0, 0};
+      if (value_chunk<NCH, true>(r, p) * 8 >= a.d) at[S::TILE] = u32x4{0, 0, 0, 0};
     }
   }
   Rows<ND> st;

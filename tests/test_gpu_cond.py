@@ -138,6 +138,20 @@ def test_cross_attention_mask(torch, C, ql, kl, hq, hkv, d, dtype):
         assert not bool(got[ql[0]:ql[0] + ql[1]].any())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,hq,hkv,d", [(9, 4, 2, 40), (2100, 8, 4, 40), (2100, 8, 4, 72), (2100, 4, 2, 128)])
+def test_cross_attention_infinite_scores(torch, C, ql, hq, hkv, d, dtype):
+    """A key whose score is -inf weighs nothing, also where head_dim is padded."""
+    _say(f"cross with scores of -inf {ql} rows of {d} {dtype}")
+    q = _randn(torch, 80, ql, hq, d, dtype=dtype)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    k, v = _randn(torch, 81, 96, hkv, d, dtype=dtype), _randn(torch, 82, 96, hkv, d, dtype=dtype)
+    gone = np.arange(96) % 5 == 1
+    ref = O.cross(_f64(q), _f64(k), _f64(v), [ql], [96], key_mask=~gone)
+    k[torch.from_numpy(gone).cuda(), :, 0] = float("-inf")
+    _compare(C.cross_attention(q, k, v, [ql], [96]), *ref, 96, d, dtype)
+
+
 def test_cross_attention_index(torch, C):
     """One frame's conditioning for all, the same one twice, an order that goes back, and one that
     nobody reads."""
