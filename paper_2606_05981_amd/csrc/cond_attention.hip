@@ -906,7 +906,7 @@ __device__ __forceinline__ Seen seen_of(const Kv8AttnArgs &a, const CondSeq &sq,
 }
 
 // What scores of a block's key codes are multiplied by; never 0, so that a masked score stays -inf.
-__device__ __forceinline__ float key_factor(float ks, float sc) { return fmaxf(ks * sc, 0x1p-126f); }
+__device__ __forceinline__ float key_factor(float ks, float sc) { return fmaxf(ks * sc, 0x1p-149f); }
 
 // A block of the pool, or none: its number times heads + g, and its scales (vs < 0: none).
 struct BlockRef { int64_t at; float ks, vs; };

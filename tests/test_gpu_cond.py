@@ -542,6 +542,26 @@ def test_kv8_values_of_unseen_blocks(torch, C, ql, kl, width, dtype):
         _compare(got[part], *(x[part] for x in ref), m, d, dtype, np.abs(vv[:m]).max())
 
 
+@pytest.mark.parametrize("ql,kl", [([1], [4000]), ([40], [3000]), ([40], [64])])
+def test_kv8_smallest_keys(torch, C, ql, kl):
+    """Keys at the smallest scale under queries that make up for it."""
+    _say("cached, smallest keys", ql, kl)
+    h, d = 2, 64
+    cache = C.kv8_cache((kl[0] + 31) // 32, h, d)
+    table = torch.arange(cache.scales.shape[0], dtype=torch.int32, device="cuda")[None]
+    k, v = _randn(torch, 96, kl[0], h, d, dtype="f32") * 2.0 ** -126, _randn(torch, 97, kl[0], h, d, dtype="f32")
+    kv = _i32(torch, kl)
+    C.kv8_append(cache, table, kv, k, v, kl)
+    assert bool((cache.scales[..., 0] == 2.0 ** -126).all())
+    q = _randn(torch, 98, sum(ql), 4, d, dtype="f32") * 2.0 ** 120
+    got = C.kv8_attention(q, cache, table, kv, ql)
+    (kk, vv), = _held(torch, cache, table, kl)
+    ref = O.attend(_f64(q), kk, vv, np.ones((ql[0], kl[0]), bool), 1 / 8)
+    # what scores are multiplied by, 1.44 * 2^-129, is subnormal: off by 2^-150 at most, 2^-21.5 of itself,
+    # less than 6 u more
+    _compare(got, *ref, kl[0], d + 6, "f32", np.abs(vv).max())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("ql,kl", [([1], [4000]), ([40], [3000]), ([40], [64])])
 def test_kv8_largest_values(torch, C, ql, kl, dtype):
