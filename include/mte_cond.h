@@ -60,8 +60,9 @@ typedef struct {
 /* Cross attention of packed sequences. For query i of sequence b, head h:
  *   out[i, h] = sum_j softmax_j(scale q[i, h] . k[j, g]) v[j, g],  g = h / (Hq/Hkv),
  * j over the tokens of key/value sequence kv_index[b] whose key_mask is not 0. A
- * query with no such token (an empty sequence, or all masked) gets zeros. What a
- * masked token's k and v hold (infinities, NaN) does not reach the output.
+ * query with no such token (an empty sequence, or all masked, or all scores -inf) gets zeros.
+ * What a masked token's k and v hold (infinities, NaN) does not reach the output.
+ * Sums are of p up to 2^8: values beyond 2^100 may end as infinities.
  *  q, out:   device, sum(q_lens) rows, sequences back to back in q_lens order.
  *  k, v:     device, sum(kv_lens) rows, back to back in kv_lens order.
  *  key_mask: device uint8[sum(kv_lens)], or NULL (all tokens count).
@@ -71,9 +72,9 @@ typedef struct {
  *            itself, n_q == n_kv.
  *  workspace: device, at least mte_cross_attention_workspace(...) bytes, aligned to
  *            16; NULL where that is 0.
- * head_dim: a multiple of 8, at most 128. The result does not depend on what
- * else runs or on the other sequences of the call, but for how a long key range
- * is split (mte_cross_attention_workspace > 0), which goes by the whole call.
+ * head_dim: a multiple of 8, at most 128. The result does not depend on what else
+ * runs. Which kernel takes the rows and how a long key range is split goes by the
+ * whole call, so that other sequences may change the last bits of a result.
  * Errors: MTE_E_INVALID (null, negative length, bad index, heads, dtype, scale,
  * strides or alignment, a sum of lengths beyond 2^31 - 1), MTE_E_UNSUPPORTED
  * (head_dim), MTE_E_CAPACITY (workspace_bytes), MTE_E_HIP. No query rows at all
@@ -137,8 +138,8 @@ int mte_kv8_append(const mte_kv8 *cache, const int32_t *table, int32_t table_wid
                    hipStream_t stream);
 
 /* The newest counts[i] tokens of each sequence as rows: k and v (device, dtype,
- * contiguous [sum(counts), Hkv, d], aligned to 16 bytes) receive code * scale, exact
- * in both types, of tokens kv_lens[i] - counts[i] .. kv_lens[i] - 1, packed back to
+ * contiguous [sum(counts), Hkv, d], aligned to 16 bytes) receive code * scale (exact,
+ * but for bf16 magnitudes below 2^-126: they are rounded to its multiples of 2^-133) of tokens kv_lens[i] - counts[i] .. kv_lens[i] - 1, packed back to
  * back (rows of tokens before the first or beyond the table: zeros). counts: HOST
  * int32[n], each >= 0. Errors as mte_kv8_append. */
 int mte_kv8_read(const mte_kv8 *cache, const int32_t *table, int32_t table_width, int64_t table_row,

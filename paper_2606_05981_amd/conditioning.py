@@ -187,7 +187,7 @@ def _cache(cache, table, kv_lens, n: int, dev: torch.device):
             tuple(sc.shape) != (nb, h, 2):
         raise ValueError(f"cache: shapes {tuple(kc.shape)}, {tuple(vc.shape)}, {tuple(sc.shape)} do not fit together")
     if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.device != dev or \
-            table.dim() != 2 or table.shape[0] != n or table.shape[1] == 0 or \
+            table.dim() != 2 or table.shape[0] != n or not 0 < table.shape[1] < 1 << 26 or \
             (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError(f"table: expected an int32 [{n}, blocks] tensor on {dev} with contiguous rows")
     if not isinstance(kv_lens, torch.Tensor) or kv_lens.dtype != torch.int32 or kv_lens.device != dev or \
@@ -220,6 +220,8 @@ def kv8_read(cache, table: torch.Tensor, kv_lens: torch.Tensor, counts: Sequence
     if dtype not in _DTYPE:
         raise ValueError("dtype: expected torch.bfloat16 or torch.float32")
     dev = cache[0].device
+    if dev.type != "cuda":
+        raise ValueError("cache: expected tensors on the GPU")
     keep, lens, n = _lens("counts", counts, None)
     c, h, d, width, row = _cache(cache, table, kv_lens, n, dev)
     total = sum(keep)
@@ -295,6 +297,9 @@ def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = Non
             raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {C} values on {dev}")
     xi, xr, px = _pixels("x", x)
     n = x.shape[0]
+    if not 0 < groups < 1 << 31 or max(n, px, C) >= 1 << 31:      # (counted in 31 bits)
+        raise ValueError(f"x, groups: expected fewer than 2^31 images, pixels, channels and groups, got {n} of {px} of "
+                         f"{C} in {groups}")
     oi = orow = 0
     if out is not None:
         if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != dtype or out.device != dev:

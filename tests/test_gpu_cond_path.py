@@ -231,3 +231,15 @@ def test_wrappers_refuse(torch, C):
                 dict(stream=object())):
         with pytest.raises((ValueError, MteError, AttributeError)):
             C.group_norm(**{**dict(x=x, groups=8), **bad})
+
+
+def test_sizes_past_31_bits_are_refused(torch, C):
+    """Sizes that the C interface counts in 31 bits raise instead of wrapping round."""
+    x = torch.zeros(1, 1, 8, dtype=torch.bfloat16, device="cuda")
+    for bad in (dict(x=x.expand(1, (1 << 32) + 1, 8), groups=1), dict(x=x.expand((1 << 32) + 1, 1, 8), groups=1),
+                dict(x=x, groups=(1 << 32) + 1)):
+        with pytest.raises(ValueError):
+            C.group_norm(**bad)
+    cache = [t.cpu() for t in C.kv8_cache(1, 2, 64)]
+    with pytest.raises(ValueError):
+        C.kv8_read(cache, torch.zeros(1, 1, dtype=torch.int32), torch.ones(1, dtype=torch.int32), [1])
