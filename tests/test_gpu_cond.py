@@ -229,6 +229,37 @@ def test_cross_attention_strides_past_32_bits(torch, C):
     assert torch.equal(plain, C.cross_attention(far, k, v, [4], [4], out=far))
 
 
+@pytest.mark.parametrize("ql,kl,d", [(8500, 70, 64), (8500, 70, 104), (20, 600, 64)])
+def test_cross_attention_rows_far_apart(torch, C, ql, kl, d):
+    """Keys too far apart for 32-bit offsets within a tile, under many rows and few."""
+    _say(f"cross, {ql} rows over keys 2^24 elements apart")
+    step = 1 << 24
+    buf = torch.empty((kl - 1) * step + 2 * d, dtype=torch.bfloat16, device="cuda")
+    k, v = (buf.as_strided((kl, 1, d), (step, d, 1), x) for x in (0, d))
+    k.copy_(_randn(torch, 23, kl, 1, d)), v.copy_(_randn(torch, 24, kl, 1, d))
+    q = _randn(torch, 25, ql, 2, d, std=1.5)
+    mask = torch.rand(kl, generator=torch.Generator().manual_seed(26)) < 0.7
+    for m in (None, mask):
+        got = C.cross_attention(q, k, v, [ql], [kl], key_mask=None if m is None else m.cuda())
+        _compare(got, *O.cross(_f64(q), _f64(k), _f64(v), [ql], [kl], key_mask=None if m is None else m.numpy()), kl, d,
+                 "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_cross_attention_index_split(torch, C, dtype):
+    """Several sequences, long and short, over one long one that is split; a masked half."""
+    _say("cross with kv_index, split", dtype)
+    ql, kl, idx = [3, 30, 0, 1], [5, 3300], [1, 1, 0, 0]
+    q = _randn(torch, 27, sum(ql), 4, 64, dtype=dtype)
+    k, v = _randn(torch, 28, sum(kl), 2, 64, dtype=dtype), _randn(torch, 29, sum(kl), 2, 64, dtype=dtype)
+    mask = torch.ones(sum(kl), dtype=torch.bool)
+    mask[400:2000] = False                        # whole parts see nothing
+    for m in (None, mask):
+        got = C.cross_attention(q, k, v, ql, kl, kv_index=idx, key_mask=None if m is None else m.cuda())
+        ref = O.cross(_f64(q), _f64(k), _f64(v), ql, kl, idx, key_mask=None if m is None else m.numpy())
+        _compare(got, *ref, max(kl), 64, dtype)
+
+
 # ---- the cache ----------------------------------------------------------------------------------
 
 
@@ -580,6 +611,30 @@ def test_kv8_largest_values(torch, C, ql, kl, dtype):
     (kk, vv), = _held(torch, cache, table, kl)
     ref = O.attend(_f64(q), kk, vv, np.ones((ql[0], kl[0]), bool), 1 / 8)
     _compare(got, *ref, kl[0], d, dtype, np.abs(vv).max())
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_kv8_many_sequences_cut(torch, C, causal):
+    """More sequences than one launch takes, long ones among them, each cut into its own number of parts;
+    lengths that change under the same call."""
+    _say("cached, 150 sequences, long ones cut", causal)
+    rng = np.random.default_rng(68)
+    kl = [int(x) for x in rng.integers(0, 50, 150)]
+    kl[3], kl[40], kl[127], kl[128], kl[149] = 2000, 700, 900, 1100, 33
+    ql = [int(x) for x in rng.integers(0, 3, 150)]
+    ql[3], ql[40], ql[127], ql[128] = 1, 2, 1, 2
+    cache, table, _, _, _ = _fill(torch, C, kl, 2, 64, spread=False)
+    q = _randn(torch, 69, sum(ql), 4, 64)
+    held = _held(torch, cache, table, kl)
+    for lens in (kl, [x // 2 for x in kl], [x if i == 128 else min(x, 1) for i, x in enumerate(kl)]):
+        got = C.kv8_attention(q, cache, table, _i32(torch, lens), ql, causal=causal)
+        parts, at = [], 0
+        for (k, v), n, m in zip(held, ql, lens):
+            see = np.arange(m)[None] <= m - n + np.arange(n)[:, None] if causal else np.ones((n, m), bool)
+            parts.append(O.attend(_f64(q[at:at + n]), k[:m], v[:m], see, 1 / 8))
+            at += n
+        _compare(got, *(np.concatenate([p[x] for p in parts]) for x in range(3)), 2000, 64, "bf16",
+                 max(np.abs(v).max() for _, v in held if v.size))
 
 
 # ---- group norm ---------------------------------------------------------------------------------

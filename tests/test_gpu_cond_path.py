@@ -149,6 +149,43 @@ def test_captured_reads(torch, C):
             assert torch.equal(a, b), s
 
 
+def test_two_graphs(torch, C):
+    """Two captured graphs of split calls and a two-launch norm, replayed in turn and on two streams at
+    once: their workspaces are their own."""
+    _say("two graphs")
+    xs = [_randn(torch, 200 + i, 3, 4, 64) for i in range(2)]
+    k, v = _randn(torch, 202, 4000, 2, 64), _randn(torch, 203, 4000, 2, 64)
+    im = [_randn(torch, 204 + i, 2, 64, 64, 64) for i in range(2)]
+    cache = C.kv8_cache(125, 2, 64)
+    table, kv = torch.arange(125, dtype=torch.int32, device="cuda")[None], _i32(torch, [4000])
+    C.kv8_append(cache, table, kv, k, v, [4000])
+
+    def run(i):
+        return (C.cross_attention(xs[i], k, v, [3], [4000]), C.kv8_attention(xs[i], cache, table, kv, [3], causal=True),
+                C.group_norm(im[i], 8, act="silu"))
+    want = [run(i) for i in range(2)]
+    torch.cuda.synchronize()
+    graphs, got = [], []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(run(i))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for both in (False, True, True, False):
+        for i in (0, 1):
+            for t in got[i]:
+                t.zero_()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i] if both else torch.cuda.current_stream()):
+                for _ in range(3):
+                    graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert all(torch.equal(a, b) for a, b in zip(got[i], want[i])), (both, i)
+
+
 def test_streams(torch, C):
     """Calls on two streams at once, inputs of one stream read on another (ordered by the caller and
     dropped right after), and a stream handed over by argument."""
