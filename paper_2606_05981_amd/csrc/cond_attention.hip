@@ -21,8 +21,7 @@
 #include <algorithm>
 
 #include "../../include/mte.h"
-#include "common.h"
-#include "cond_launch.h"
+#include "cond_device.h"
 
 namespace mte {
 
@@ -39,15 +38,6 @@ template <> struct QFrag<float> { typedef f32x4 type; };
 
 constexpr int kThreads = 256;
 constexpr int kMaxParts = 512;                      // of a key range
-
-__device__ __forceinline__ int find_seq(const CondSeq *seq, int n, int tile) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (seq[mid].tile0 <= tile) lo = mid; else hi = mid - 1;
-  }
-  return lo;
-}
 
 // The workgroup's tile and kv head, heads next to each other: the workgroups that run together then read
 // and write whole rows of q and out between them (head-major order: 4 to 10% slower).

@@ -9,23 +9,13 @@
 #include <algorithm>
 
 #include "../../include/mte.h"
-#include "common.h"
-#include "cond_launch.h"
+#include "cond_device.h"
 
 namespace mte {
 
 namespace {
 
 constexpr int kThreads = 256;
-
-__device__ __forceinline__ int find_seq8(const CondSeq *seq, int n, int tile) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (seq[mid].tile0 <= tile) lo = mid; else hi = mid - 1;
-  }
-  return lo;
-}
 
 // Position of token t of a block in a row of the value codes.
 __device__ __forceinline__ int v_pos(int t) { return 16 * ((t >> 2) & 1) + 8 * (t >> 4) + 4 * ((t >> 3) & 1) + (t & 3); }
@@ -59,21 +49,17 @@ __device__ __forceinline__ void value4(uint32_t w, float *x) {
   x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
 }
 
-__device__ __forceinline__ void load16(const float *p, float *x) {
+// 16 elements of a row as loaded, and as floats.
+template <typename T> struct Row16 { u32x4 w[sizeof(T)]; };
+template <typename T> __device__ __forceinline__ void load16(const T *p, Row16<T> &r) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const f32x4 v = ((const f32x4 *)p)[i];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
-  }
+  for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = ((const u32x4 *)p)[i];
 }
-__device__ __forceinline__ void load16(const bf16 *p, float *x) {
+template <typename T> __device__ __forceinline__ void floats16(const Row16<T> &r, float *x) {
+  T t[16];
+  __builtin_memcpy(t, &r, sizeof(t));
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const bf16x8 v = ((const bf16x8 *)p)[i];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[8 * i + e] = (float)v[e];
-  }
+  for (int e = 0; e < 16; ++e) x[e] = to_f32(t[e]);
 }
 __device__ __forceinline__ void store16(float *p, const float *x) {
 #pragma unroll
@@ -114,27 +100,45 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t sv[D * VP];
   __shared__ float smax[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const CondSeq sq = a.seq[find_seq8(a.seq, a.n_seq, blockIdx.x)];
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, blockIdx.x)];
   const int g = blockIdx.y;
   const Where w = block_of(a.c, sq, (int)blockIdx.x - sq.tile0, g);
   // the whole workgroup: a sequence shorter than its new rows, or longer than its table, is not written
-  if (!w.ok || w.start < 0 || w.kv > (int64_t)a.c.width * 32) return;
+  if (w.start < 0 || w.kv > (int64_t)a.c.width * 32) return;
   const int sub = tid % (32 * PC), tok = sub / PC, pc = sub % PC;
   const int first = D == 128 ? 0 : tid / (32 * PC); // tensor of the thread (D = 64)
   const int pos = w.b * 32 + tok;                   // token of the sequence
   const bool fresh = pos >= w.start && pos < w.kv, kept = pos < w.start;
   const bool any_kept = w.b * 32 < w.start;
-  float x[NT][16], mx[2] = {0.f, 0.f};
+  // All that is read is in flight at once: the rows, which do not wait for the table, then the block.
+  Row16<T> raw[NT] = {};
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int ten = D == 128 ? t : first;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[t][e] = 0.f;
     if (fresh) {
       const int64_t row = sq.q0 + (pos - w.start);
-      if (ten == 0) load16((const T *)a.k + row * a.k_row + (int64_t)g * a.k_head + pc * 16, x[t]);
-      else load16((const T *)a.v + row * a.v_row + (int64_t)g * a.v_head + pc * 16, x[t]);
+      if (ten == 0) load16((const T *)a.k + row * a.k_row + (int64_t)g * a.k_head + pc * 16, raw[t]);
+      else load16((const T *)a.v + row * a.v_row + (int64_t)g * a.v_head + pc * 16, raw[t]);
     }
+  }
+  if (!w.ok) return;                                // the whole workgroup
+  uint8_t *kc = a.c.k_codes + w.at * (32 * D), *vc = a.c.v_codes + w.at * (32 * D);
+  const bool turn = any_kept && (D == 128 || first == 1);
+  constexpr int VT = D == 128 ? 256 : 128;          // threads that read the block's value codes, 16 bytes each
+  const int vi = D == 128 ? tid : tid - 128;
+  static_assert(32 * D / 16 == VT, "one chunk a thread");
+  u32x4 k_old{0, 0, 0, 0}, v_old{0, 0, 0, 0};
+  float s_old[2] = {0.f, 0.f};
+  if (any_kept) {                                   // workgroup-uniform
+    s_old[0] = a.c.scales[w.at * 2];
+    s_old[1] = a.c.scales[w.at * 2 + 1];
+    if (kept && (D == 128 || first == 0)) k_old = *(const u32x4 *)(kc + (pc * 32 + tok) * 16);
+    if (turn) v_old = ((const u32x4 *)vc)[vi];
+  }
+  float x[NT][16], mx[2] = {0.f, 0.f};
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    floats16(raw[t], x[t]);
     float m = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[t][e]));
@@ -147,6 +151,7 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
     for (int s = 32; s >= 1; s >>= 1) mx[t] = warp_max_xor(mx[t], s);
     if (lane == 0) smax[t][wave] = mx[t];
   }
+  if (turn) *(u32x4 *)(sv + (vi >> 1) * VP + (vi & 1) * 16) = v_old;   // [d][pos]
   __syncthreads();
   int e_new[2], e_old[2];
 #pragma unroll
@@ -154,26 +159,18 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
     e_new[t] = scale_exp(fmaxf(fmaxf(smax[t][0], smax[t][1]), fmaxf(smax[t][2], smax[t][3])));
     e_old[t] = e_new[t];
     if (any_kept) {
-      const float s = a.c.scales[w.at * 2 + t];
-      e_old[t] = (int)((__float_as_uint(s) >> 23) & 0xFF) - 127;
+      e_old[t] = (int)((__float_as_uint(s_old[t]) >> 23) & 0xFF) - 127;
       e_new[t] = max(e_new[t], e_old[t]);
     }
   }
-  uint8_t *kc = a.c.k_codes + w.at * (32 * D), *vc = a.c.v_codes + w.at * (32 * D);
   // older tokens: their values in units of the old scale, then like new rows of that size
-  if (any_kept && (D == 128 || first == 1)) {       // value codes: LDS [d][pos]
-    constexpr int N = 32 * D / 16;                  // 16-byte chunks
-    for (int i = D == 128 ? tid : tid - 128; i < N; i += D == 128 ? 256 : 128)
-      *(u32x4 *)(sv + (i >> 1) * VP + (i & 1) * 16) = ((const u32x4 *)vc)[i];
-  }
-  if (any_kept) __syncthreads();                    // workgroup-uniform
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int ten = D == 128 ? t : first;
     if (kept) {
       u32x4 o;
       if (ten == 0) {
-        o = *(const u32x4 *)(kc + (pc * 32 + tok) * 16);
+        o = k_old;
       } else {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -213,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void k_kv8_read(Kv8RowsArgs a) {
   constexpr int VP = 48;
   __shared__ __attribute__((aligned(16))) uint8_t sv[D * VP];
   const int tid = threadIdx.x;
-  const CondSeq sq = a.seq[find_seq8(a.seq, a.n_seq, blockIdx.x)];
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, blockIdx.x)];
   const int g = blockIdx.y;
   const Where w = block_of(a.c, sq, (int)blockIdx.x - sq.tile0, g);
   uint8_t *kc = a.c.k_codes + w.at * (32 * D), *vc = a.c.v_codes + w.at * (32 * D);
