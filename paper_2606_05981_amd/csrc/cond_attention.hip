@@ -19,6 +19,8 @@
 // workgroup (joined through LDS) and over workgroups (partial O, m, l in the
 // workspace, joined by k_cond_join).
 #include <algorithm>
+#include <climits>
+#include <cmath>
 
 #include "../../include/mte.h"
 #include "cond_device.h"
@@ -50,8 +52,28 @@ __device__ __forceinline__ Unit unit_of(int hkv) {
   return u;
 }
 
-// Least key tiles of a split of k_cross_stream.
-constexpr int kStreamLeast = 8;
+// A unit of cross attention: a tile of TR rows over a part of the keys of its sequence. The host cuts every
+// key range of nt tiles into parts_of(nt, per) parts, `per` for the whole launch; the units of a
+// sequence are its row tiles for the first part, then for the next.
+__host__ __device__ __forceinline__ int parts_of(int nt, int per) {   // parts of about `per`: 1/2 to 3/2 of it, or the rest
+  return nt <= per ? 1 : (nt + per / 2) / per;
+}
+struct Part { int row_tile, split, used, lo, hi; };     // key tiles [lo, hi)
+__device__ __forceinline__ Part part_of(const CondSeq &sq, int local, int rows, int TR, int nt, int per) {
+  Part p;
+  p.used = parts_of(nt, per);
+  p.split = 0;
+  p.row_tile = local;
+  if (p.used > 1) {
+    const int tiles = (rows + TR - 1) / TR;
+    p.split = local / tiles;
+    p.row_tile = local - p.split * tiles;
+  }
+  const int each = nt / p.used, more = nt % p.used;     // the first `more` parts have one tile more
+  p.lo = p.split * each + min(p.split, more);
+  p.hi = p.lo + each + (p.split < more);
+  return p;
+}
 
 // Key tiles [lo, hi) of split `split` of n_split over nt key tiles; used: the splits
 // that have any (at least 1). A split takes at least `least` tiles.
@@ -352,12 +374,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
   const int lrow = lane & 31, h = lane >> 5;
   const int rw = wave % RW, kw = wave / RW;
   const Unit un = unit_of(a.hkv);
-  const int tile = un.tile, g = un.g, split = blockIdx.y;
+  const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int klen = sq.k_len, rows = sq.q_len * a.rep;
-  const int r0 = (tile - sq.tile0) * 32 * RW + rw * 32;   // first row of the wave
-  const Span span = split_span((klen + KT - 1) / KT, a.n_split, split, 1);
-  if (split >= span.used) return;                   // the whole workgroup
+  const Part span = part_of(sq, tile - sq.tile0, rows, 32 * RW, (klen + KT - 1) / KT, a.per);
+  const int r0 = span.row_tile * 32 * RW + rw * 32; // first row of the wave
   const int r = r0 + lrow;
   const bool live = r < rows;
   const int64_t tok = sq.q0 + (live ? r / a.rep : 0);
@@ -462,7 +483,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
   }
   if (r0 >= rows) return;
   if (span.used == 1) store_rows<T, ND>(a, st, 1.f, live, tok, head, lane);
-  else store_part<ND>(a, st, 1.f, live, tile, g, split, rw * 32 + lrow, lane);
+  else store_part<ND>(a, st, 1.f, live, tile, g, 0, rw * 32 + lrow, lane);
 }
 
 // Lane j: which keys of the 32-key tile t0 + j count (a bit each), for up to 64 tiles.
@@ -635,12 +656,11 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
   const Unit un = unit_of(a.hkv);
-  const int tile = un.tile, g = un.g, split = blockIdx.y;
+  const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
-  const int klen = sq.k_len, nk = (klen + 31) >> 5;
-  const int rows = sq.q_len * a.rep, r0 = (tile - sq.tile0) * 128 + wave * 32;
-  const Span span = split_span(nk, a.n_split, split, kStreamLeast);
-  if (split >= span.used) return;                   // the whole workgroup
+  const int klen = sq.k_len, rows = sq.q_len * a.rep;
+  const Part span = part_of(sq, tile - sq.tile0, rows, 128, (klen + 31) >> 5, a.per);
+  const int r0 = span.row_tile * 128 + wave * 32;
 
   const bf16 *kg = (const bf16 *)a.k + (int64_t)sq.k0 * a.k_row + (int64_t)g * a.k_head;
   const bf16 *vg = (const bf16 *)a.v + (int64_t)sq.k0 * a.v_row + (int64_t)g * a.v_head;
@@ -718,7 +738,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
   }
   if (r0 >= rows) return;
   if (span.used > 1) {
-    store_part<ND>(a, st, 1.f, r0 + lrow < rows, tile, g, split, wave * 32 + lrow, lane);
+    store_part<ND>(a, st, 1.f, r0 + lrow < rows, tile, g, 0, wave * 32 + lrow, lane);
     return;
   }
   // all slots but the last tile's and the one before hold nothing that is still read
@@ -888,7 +908,7 @@ struct Seen { int kv, tile_lo, tile_hi, row_hi; };
 __device__ __forceinline__ Seen seen_of(const Kv8AttnArgs &a, const CondSeq &sq, int first_tok, int last_tok, int tok) {
   Seen v;
   v.kv = min(max(uniform_at(a.c.kv_lens, sq.k0), 0), a.c.width * 32);
-  const int before = v.kv - sq.q_len + 1;           // keys of token 0, causal
+  const int before = v.kv - sq.k_len + 1;           // keys of token 0, causal
   v.tile_lo = a.causal ? min(max(before + first_tok, 0), v.kv) : v.kv;
   v.tile_hi = a.causal ? min(max(before + last_tok, 0), v.kv) : v.kv;
   v.row_hi = a.causal ? min(max(before + tok, 0), v.kv) : v.kv;
@@ -934,7 +954,12 @@ __device__ __forceinline__ Cut cut_of(const Kv8AttnArgs &a, int target, int at, 
   for (int u = 0; u < 2; ++u) {
     const int i = lane + 64 * u;
     nb[u] = 0;
-    if (i < a.n_seq) nb[u] = (min(max(a.c.kv_lens[a.seq[i].k0], 0), a.c.width * 32) + 31) >> 5;
+    if (i < a.n_seq) {
+      const CondSeq &sq = a.seq[i];
+      int len = min(max(a.c.kv_lens[sq.k0], 0), a.c.width * 32);
+      if (a.causal) len = max(len - (sq.k_len - sq.q_len), 0);   // what its last row sees
+      nb[u] = (len + 31) >> 5;
+    }
     total += nb[u];
   }
 #pragma unroll
@@ -970,7 +995,7 @@ __device__ __forceinline__ Cut cut_of(const Kv8AttnArgs &a, int target, int at, 
   return w;
 }
 
-// Few rows (at most 32 a sequence): bound by the codes that stream in. Each of the four waves
+// Few rows (at most 32 a sequence, or chunk of one): bound by the codes that stream in. Each of the four waves
 // takes every fourth block of the split's range and loads its codes straight into MFMA operand
 // order, 16 bytes a lane and 1 KB a load, the next block's while one is computed.
 template <typename T, int D>
@@ -1274,6 +1299,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
 // DP / 4 lanes of four d times as many teams over the parts as it holds, so that the parts of a
 // row are read in one go (64 parts read by one team each after the other: 12 us).
 constexpr int kMostParts = kMaxParts + 1;
+template <typename T>
+__device__ __forceinline__ void store_joined(const AttnCommon &a, const CondSeq &sq, int g, int r, int c, const f32x4 &x) {
+  T *row = (T *)a.out + (int64_t)(sq.q0 + r / a.rep) * a.o_row + (int64_t)(g * a.rep + r % a.rep) * a.o_head;
+  if constexpr (sizeof(T) == 4)
+    *(f32x4 *)(row + c) = x;
+  else
+    *(bf16x4 *)(row + c) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+}
 template <typename T, int DP>
 __device__ __forceinline__ void join_row(const AttnCommon &a, const CondSeq &sq, int g, int r, int64_t at, int64_t step,
                                          int used) {
@@ -1322,36 +1355,71 @@ __device__ __forceinline__ void join_row(const AttnCommon &a, const CondSeq &sq,
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += x[e];
   }
-  T *row = (T *)a.out + (int64_t)(sq.q0 + r / a.rep) * a.o_row + (int64_t)(g * a.rep + r % a.rep) * a.o_head;
-  if constexpr (sizeof(T) == 4)
-    *(f32x4 *)(row + c) = acc;
-  else
-    *(bf16x4 *)(row + c) = bf16x4{(bf16)acc[0], (bf16)acc[1], (bf16)acc[2], (bf16)acc[3]};
+  store_joined<T>(a, sq, g, r, c, acc);
 }
-// Grid: x = (tile, kv head), y = row of the tile.
-template <typename T, int DP, typename A, typename SPAN>
-__device__ __forceinline__ void join_tile(const A &a, int TR, SPAN used_of) {
+// Few parts of many rows: a row for each DP / 4 lanes, its parts all in flight (10000 rows of two parts: 5 us, a
+// workgroup a row 12).
+constexpr int kFewParts = 8;
+template <typename T, int DP>
+__device__ __forceinline__ void join_few(const AttnCommon &a, const CondSeq &sq, int g, int r, int64_t at, int64_t step,
+                                         int used) {
+  const int c = (threadIdx.x % (DP / 4)) * 4;
+  const float *ml = a.ws + a.ws_ml + at * 2, *o = a.ws + at * DP + c;
+  float w[kFewParts], lp[kFewParts], M = -INFINITY, l = 0.f;
+  f32x4 x[kFewParts], acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < kFewParts; ++s) {
+    const int64_t k = min(s, used - 1) * step;
+    w[s] = s < used ? ml[k * 2] : -INFINITY;
+    lp[s] = s < used ? ml[k * 2 + 1] : 0.f;
+    x[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (s < used) x[s] = *(const f32x4 *)(o + k * DP);
+    M = fmaxf(M, w[s]);
+  }
+  const float mr = M == -INFINITY ? 0.f : M;
+#pragma unroll
+  for (int s = 0; s < kFewParts; ++s) {
+    w[s] = __builtin_amdgcn_exp2f(w[s] - mr) * lp[s];
+    l += w[s];
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int s = 0; s < kFewParts; ++s)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += w[s] * inv * x[s][e];
+  if (c < a.d) store_joined<T>(a, sq, g, r, c, acc);
+}
+// The row of a tile of TR that a thread joins, given the grid's y: WIDE, one a workgroup.
+template <int DP, bool WIDE> __device__ __forceinline__ int join_index() {
+  return WIDE ? blockIdx.y : blockIdx.y * (kThreads / (DP / 4)) + threadIdx.x / (DP / 4);
+}
+
+// Grid: x = (row tile, kv head), y = rows of the tile (join_index). The sequences are those that were
+// split: k0 = their first unit, k_len = its parts, tile0 = their first tile here.
+template <typename T, int DP, bool WIDE>
+__global__ __launch_bounds__(kThreads) void k_cross_join(CrossArgs a, int TR) {
   const Unit un = unit_of(a.hkv);
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, un.tile)];
-  const int rows = sq.q_len * a.rep, r0 = (un.tile - sq.tile0) * TR, i = blockIdx.y;
-  if (r0 + i >= rows) return;
-  const int used = used_of(sq, (min(r0 + TR, rows) - 1) / a.rep);
-  if (used == 1) return;
-  join_row<T, DP>(a, sq, un.g, r0 + i, ((int64_t)un.tile * a.hkv + un.g) * a.n_split * a.ws_rows + i, a.ws_rows, used);
+  const int rows = sq.q_len * a.rep, t = un.tile - sq.tile0, i = join_index<DP, WIDE>(), tiles = (rows + TR - 1) / TR;
+  if (i >= TR || t * TR + i >= rows) return;
+  const int64_t at = ((int64_t)(sq.k0 + t) * a.hkv + un.g) * a.ws_rows + i, step = (int64_t)tiles * a.hkv * a.ws_rows;
+  if constexpr (WIDE) join_row<T, DP>(a, sq, un.g, t * TR + i, at, step, sq.k_len);
+  else join_few<T, DP>(a, sq, un.g, t * TR + i, at, step, sq.k_len);
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void k_cross_join(CrossArgs a, int TR, int KT, int least) {
-  join_tile<T, DP>(a, TR, [&](const CondSeq &sq, int) {
-    return split_span((sq.k_len + KT - 1) / KT, a.n_split, 0, least).used;
-  });
-}
-
-template <typename T, int DP>
+// Grid: x = (tile, kv head), y = rows of the tile.
+template <typename T, int DP, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_kv8_tiles_join(Kv8AttnArgs a) {
-  join_tile<T, DP>(a, 128, [&](const CondSeq &sq, int last_tok) {
-    return split_span((seen_of(a, sq, 0, last_tok, 0).tile_hi + 31) >> 5, a.n_split, 0, kTilesLeast).used;
-  });
+  const Unit un = unit_of(a.hkv);
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, un.tile)];
+  const int rows = sq.q_len * a.rep, r0 = (un.tile - sq.tile0) * 128, i = join_index<DP, WIDE>();
+  if (i >= 128 || r0 + i >= rows) return;
+  const int last = (min(r0 + 128, rows) - 1) / a.rep;
+  const int used = split_span((seen_of(a, sq, 0, last, 0).tile_hi + 31) >> 5, a.n_split, 0, kTilesLeast).used;
+  if (used == 1) return;
+  const int64_t at = ((int64_t)un.tile * a.hkv + un.g) * a.n_split * a.ws_rows + i;
+  if constexpr (WIDE) join_row<T, DP>(a, sq, un.g, r0 + i, at, a.ws_rows, used);
+  else join_few<T, DP>(a, sq, un.g, r0 + i, at, a.ws_rows, used);
 }
 
 template <typename T, int DP>
@@ -1374,13 +1442,14 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 struct Plan {
   enum { FEW, COPIES, STREAM, RESIDENT } kind = FEW;
   int TR = 0, KT = 0, n_split = 1, ws_rows = 0;
-  int least = 0;                                    // key tiles of a split
+  int per = 0;                                      // cross attention: key tiles of a part (part_of)
   int target = 0;                                   // cached attention with few rows: parts (cut_of), 0: none
   int nw = 4, lds = 0;                              // RESIDENT: waves, LDS bytes,
   bool box = false;                                 // and whether they hold kBox a wave
+  bool split = false;                               // cross attention: some sequence has parts
   int64_t tiles = 0;                                // of the launch (of kCondSeqs sequences) with the most
   int64_t floats(int hkv, int dp) const {
-    return n_split > 1 || target > 0 ? tiles * hkv * n_split * (int64_t)ws_rows * (dp + 2) : 0;
+    return n_split > 1 || target > 0 || split ? tiles * hkv * n_split * (int64_t)ws_rows * (dp + 2) : 0;
   }
   int64_t ml(int hkv, int dp) const { return tiles * hkv * n_split * (int64_t)ws_rows * dp; }
 };
@@ -1429,34 +1498,51 @@ static int64_t fill_tiles(const AttnProblem &p, Plan &pl, TAKE take) {
 //    rows; 1024 bf16 rows of 10 heads, 320 tiles, over 96: 6.5, against 5.6).
 //  COPIES (bf16): tiles of 128 rows, keys by LDS-direct copies.
 //  STREAM (fp32, or rows too far apart for 32-bit offsets): tiles of 128 rows, keys by registers.
-// Launches of fewer than kFill workgroups split long key ranges.
+// Key ranges are cut into parts of the work that fills the chip once, kFill workgroups (and not below
+// 512 keys of FEW, 256 of the others: partial results and their join cost as much): few rows over
+// long keys are cut, and so is one long range among many short ones, whose workgroups would run
+// on alone (12 heads, 1500 rows of 9 sequences over 6 to 963 keys, those under 12 rows: 14.3 us, whole
+// 27.8; against it, 2500 rows of 8 heads over 356: 18.0, whole 14.0).
 static Plan cross_plan(const AttnProblem &p, const int32_t *kv_lens, const int32_t *kv_index) {
   Plan pl;
   int64_t row_tiles, most;
   const auto any = [](int) { return true; };
   count_rows(p, row_tiles, most, any);
   if (row_tiles == 0) return pl;
-  int kmax = 0;
-  for (int i = 0; i < p.n; ++i)
-    if (p.q_lens[i] > 0) kmax = std::max(kmax, kv_lens[kv_index ? kv_index[i] : i]);
   pl.TR = 128;
+  int least;
   if (most <= 32 || row_tiles * p.c.hkv < 256) {
     pl.kind = Plan::FEW;
     pl.TR = 32;
     pl.KT = 128;
-    pl.least = 1;
+    least = 4;
   } else if (p.dtype == MTE_BF16 && p.near_rows) {
     pl.kind = Plan::COPIES;
     pl.KT = 32;
-    pl.least = kStreamLeast;
+    least = 8;
   } else {
     pl.kind = Plan::STREAM;
     pl.KT = p.dtype == MTE_BF16 ? 64 : 32;
-    pl.least = 1;
+    least = 256 / pl.KT;
   }
-  const int64_t units = fill_tiles(p, pl, any) * p.c.hkv;
-  const int tiles = std::max(4, 2 * pl.least);       // of keys, for each further split
-  if (units < kFill) pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(kFill / units, ceil_div(kmax, pl.KT) / tiles));
+  const auto each = [&](auto fn) {                   // row tiles and key tiles of every sequence with rows
+    for (int i = 0; i < p.n; ++i)
+      if (p.q_lens[i] > 0) fn(ceil_div((int64_t)p.q_lens[i] * p.c.rep, pl.TR), ceil_div(kv_lens[kv_index ? kv_index[i] : i], pl.KT));
+  };
+  double work = 0;
+  each([&](int rows, int keys) { work += (double)rows * keys; });
+  pl.per = (int)std::min(std::max((double)least, std::ceil(work * p.c.hkv / kFill)), 0x1p30);
+  // no more parts than a join takes
+  each([&](int, int keys) { pl.per = std::max(pl.per, ceil_div(keys, kMaxParts - 1)); });
+  int64_t at = 0;
+  int in = 0;
+  each([&](int rows, int keys) {
+    const int used = parts_of(keys, pl.per);
+    pl.split |= used > 1;
+    if (used > 1) at += (int64_t)rows * used;        // (place_units: the others have no partial results)
+    pl.tiles = std::max(pl.tiles, at);
+    if (++in == kCondSeqs) in = at = 0;
+  });
   pl.ws_rows = (int)std::min<int64_t>(pl.TR, most);
   return pl;
 }
@@ -1498,9 +1584,29 @@ static hipError_t allow_lds(K kern, int bytes) {
                         : hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
+// Workgroups for the rows of a tile (join_index).
+template <int DP> int join_grid(int parts, int rows) { return parts > kFewParts ? rows : ceil_div(rows, kThreads / (DP / 4)); }
+
+// The units of a launch's sequences: first those of split ones (the workspace ends after them), then longest
+// first, so that the last workgroups to start are the shortest.
+static int place_units(CrossArgs &a, const Plan &pl) {
+  const auto rank = [&](const CondSeq &q) {
+    const int nt = ceil_div(q.k_len, pl.KT);
+    return parts_of(nt, pl.per) > 1 ? INT_MAX : nt;
+  };
+  std::stable_sort(a.seq, a.seq + a.n_seq, [&](const CondSeq &x, const CondSeq &y) { return rank(x) > rank(y); });
+  int units = 0;
+  for (int i = 0; i < a.n_seq; ++i) {
+    CondSeq &q = a.seq[i];
+    q.tile0 = units;
+    units += ceil_div((int64_t)q.q_len * a.rep, pl.TR) * parts_of(ceil_div(q.k_len, pl.KT), pl.per);
+  }
+  return units;
+}
+
 template <typename T, int DP>
-static hipError_t run_cross(const CrossArgs &a, int tiles, const Plan &pl, hipStream_t s) {
-  const dim3 grid(tiles * a.hkv, a.n_split);
+static hipError_t run_cross(CrossArgs &a, const Plan &pl, hipStream_t s) {
+  const int units = place_units(a, pl);
   hipError_t e;
   auto kern = pl.kind == Plan::FEW ? k_cross<T, DP, 1> : k_cross<T, DP, 4>;
   int lds = 2 * pl.KT * DP * (int)sizeof(T) + 32;
@@ -1512,10 +1618,24 @@ static hipError_t run_cross(const CrossArgs &a, int tiles, const Plan &pl, hipSt
     }
   }
   if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, grid, dim3(kThreads), lds, s, a);
-  if ((e = hipGetLastError()) != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL((k_cross_join<T, DP>), dim3(tiles * a.hkv, a.ws_rows), dim3(kThreads), 0, s, a, pl.TR, pl.KT,
-                     pl.least);
+  hipLaunchKernelGGL(kern, dim3(units * a.hkv), dim3(kThreads), lds, s, a);
+  if ((e = hipGetLastError()) != hipSuccess || !pl.split) return e;
+  int n = 0, tiles = 0, most = 0;
+  for (int i = 0; i < a.n_seq; ++i) {
+    CondSeq q = a.seq[i];
+    const int used = parts_of(ceil_div(q.k_len, pl.KT), pl.per);
+    if (used == 1) continue;
+    q.k0 = q.tile0;
+    q.k_len = used;
+    most = std::max(most, used);
+    q.tile0 = tiles;
+    tiles += ceil_div((int64_t)q.q_len * a.rep, pl.TR);
+    a.seq[n++] = q;
+  }
+  if (n == 0) return e;                             // none in this launch
+  a.n_seq = n;
+  auto join = most > kFewParts ? k_cross_join<T, DP, true> : k_cross_join<T, DP, false>;
+  hipLaunchKernelGGL(join, dim3(tiles * a.hkv, join_grid<DP>(most, a.ws_rows)), dim3(kThreads), 0, s, a, pl.TR);
   return hipGetLastError();
 }
 
@@ -1534,7 +1654,8 @@ hipError_t launch_cross(const AttnProblem &p, const void *k, const void *v, cons
   a.k_head = k_head;
   a.v_row = v_row;
   a.v_head = v_head;
-  a.n_split = pl.n_split;
+  a.per = pl.per;
+  a.n_split = 1;
   a.ws_rows = pl.ws_rows;
   a.ws_ml = pl.ml(a.hkv, dp);
   // first key row of the sequence a query sequence names: a running sum, taken up again from the
@@ -1554,23 +1675,59 @@ hipError_t launch_cross(const AttnProblem &p, const void *k, const void *v, cons
     if (tiles == 0) continue;
     hipError_t e;
     if (p.dtype == MTE_BF16)
-      e = dp == 64 ? run_cross<bf16, 64>(a, tiles, pl, s) : run_cross<bf16, 128>(a, tiles, pl, s);
+      e = dp == 64 ? run_cross<bf16, 64>(a, pl, s) : run_cross<bf16, 128>(a, pl, s);
     else
-      e = dp == 64 ? run_cross<float, 64>(a, tiles, pl, s) : run_cross<float, 128>(a, tiles, pl, s);
+      e = dp == 64 ? run_cross<float, 64>(a, pl, s) : run_cross<float, 128>(a, pl, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-// Query sequences of up to 32 rows stream the codes (few), longer ones stage them (many), whole where
-// the table is no wider than LDS; a call with both takes both kernels. The workspace serves
-// one after the other.
+// Few rows stream the codes, in chunks of as many tokens as 32 rows hold, each read as a sequence of its own;
+// many stage them, whole where the table is no wider than LDS. A call with both takes both kernels,
+// the workspace serving one after the other. Which sequences are few goes by the tiles of 32 rows of
+// the call, times kv heads (us few / many):
+//   below kFewTiles, all: 508 queries of 2 x 2 heads of 128 over 59 to 682 tokens 16.8 / 29.1; against it,
+//     50 of 8 heads of 64 over 257, 11.0 / 9.4; above it 250 of 2 x 8 heads over 320 19.5 / 14.7;
+//   below kFill, those of two tiles: 16 x 30 of 2 x 8 heads over 200 9.4 / 10.2, 9 of 1 to 39 of 20
+//     heads over 20 to 825 (one kernel instead of two) 15.0 / 24.9;
+//   else those of one: 64 x 60 of 10 heads over 100 15.2 / 10.3.
 constexpr int kLds = 160 * 1024;                     // of a compute unit
-static bool few_rows(const AttnProblem &p, int i) { return (int64_t)p.q_lens[i] * p.c.rep <= 32; }
+constexpr int kFewTiles = 96;
+struct Few {
+  int chunk;                                        // tokens of a chunk; 0: one token has more than 32 rows
+  int64_t rows;                                     // the most rows of a few sequence
+  explicit Few(const AttnProblem &p) : chunk(32 / p.c.rep) {
+    int64_t tiles = 0;
+    for (int i = 0; chunk > 0 && i < p.n; ++i) tiles += ceil_div(p.q_lens[i], chunk);
+    tiles *= p.c.hkv;
+    rows = tiles < kFewTiles ? INT64_MAX : tiles < kFill ? 64 : 32;
+  }
+  bool takes(const AttnProblem &p, int i) const { return chunk > 0 && (int64_t)p.q_lens[i] * p.c.rep <= rows; }
+};
+// Fills a.seq with the next chunks of few sequences (from query `done` of sequence i); returns how many.
+static int next_chunks(Kv8AttnArgs &a, const AttnProblem &p, const Few &fw, int &i, int &row, int &done) {
+  a.n_seq = 0;
+  while (i < p.n && a.n_seq < kCondSeqs) {
+    const int len = p.q_lens[i], left = len - done;
+    if (left > 0 && fw.takes(p, i)) {
+      const int n = std::min(fw.chunk, left);
+      a.seq[a.n_seq] = CondSeq{row + done, n, i, left, a.n_seq};
+      ++a.n_seq;
+      done += n;
+      if (done < len) continue;
+    }
+    row += len;
+    done = 0;
+    ++i;
+  }
+  return a.n_seq;
+}
 static Plan kv8_plan(const AttnProblem &p, int width, bool few) {
   Plan pl;
   int64_t row_tiles, most;
-  const auto mine = [&](int i) { return few_rows(p, i) == few; };
+  const Few fw(p);
+  const auto mine = [&](int i) { return fw.takes(p, i) == few; };
   count_rows(p, row_tiles, most, mine);
   if (row_tiles == 0) return pl;
   const int64_t res = (int64_t)width * 32 * p.c.d * 4;
@@ -1605,6 +1762,10 @@ static Plan kv8_plan(const AttnProblem &p, int width, bool few) {
   if (pl.kind == Plan::RESIDENT) return pl;
   pl.ws_rows = (int)std::min<int64_t>(pl.TR, most);
   if (few) {
+    int64_t chunks = 0;
+    for (int i = 0; i < p.n; ++i)
+      if (mine(i)) chunks += ceil_div(p.q_lens[i], fw.chunk);
+    pl.tiles = std::min<int64_t>(chunks, kCondSeqs);
     // parts for each kv head: of kFill workgroups, no more than the widest tables fill; the
     // partial results of all that the lengths may lead to
     const int fill = p.dtype == MTE_BF16 ? kFill : kFill / 2;   // fp32: one workgroup a compute unit
@@ -1631,7 +1792,7 @@ static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, const Plan &pl, hipSt
     hipLaunchKernelGGL(kern, grid, dim3(64 * pl.nw), pl.lds, s, a, pl.TR);
     return hipGetLastError();
   }
-  if (pl.kind == Plan::FEW) {                       // a tile is a sequence
+  if (pl.kind == Plan::FEW) {                       // a tile is a chunk
     const int target = std::max(pl.target, 1);
     const dim3 parts((tiles + (pl.target > 0 ? target : 0)) * a.hkv);
     hipLaunchKernelGGL((k_kv8_rows<T, D>), parts, dim3(kThreads), 3 * (2 + D / 2) * 64 * 4, s, a, target);
@@ -1641,11 +1802,13 @@ static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, const Plan &pl, hipSt
   }
   hipLaunchKernelGGL((k_kv8_tiles<T, D>), grid, dim3(kThreads), 2 * 4 * (D / 32) * 64 * 16, s, a);
   if ((e = hipGetLastError()) != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL((k_kv8_tiles_join<T, D>), dim3(tiles * a.hkv, a.ws_rows), dim3(kThreads), 0, s, a);
+  auto join = a.n_split > kFewParts ? k_kv8_tiles_join<T, D, true> : k_kv8_tiles_join<T, D, false>;
+  hipLaunchKernelGGL(join, dim3(tiles * a.hkv, join_grid<D>(a.n_split, a.ws_rows)), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_kv8_attention(const AttnProblem &p, const Kv8View &c, int causal, hipStream_t s) {
+  const Few fw(p);
   for (const bool few : {true, false}) {
     const Plan pl = kv8_plan(p, c.width, few);
     if (pl.tiles == 0) continue;
@@ -1659,11 +1822,11 @@ hipError_t launch_kv8_attention(const AttnProblem &p, const Kv8View &c, int caus
     a.ws_ml = pl.ml(a.hkv, c.d);
     auto take = [&](int i, CondSeq &sq) {
       sq.k0 = i;
-      sq.k_len = 0;
-      return few_rows(p, i) == few;
+      sq.k_len = p.q_lens[i];
+      return fw.takes(p, i) == few;
     };
-    for (int i = 0, row = 0; i < p.n;) {
-      const int tiles = next_seqs(a, p, i, row, pl.TR, take);
+    for (int i = 0, row = 0, done = 0; i < p.n;) {
+      const int tiles = few ? next_chunks(a, p, fw, i, row, done) : next_seqs(a, p, i, row, pl.TR, take);
       if (tiles == 0) continue;
       hipError_t e;
       if (p.dtype == MTE_BF16)

@@ -13,15 +13,16 @@ constexpr int kCondSeqs = 128;
 
 struct CondSeq {
   int q0, q_len;   // first packed query (or appended / read) row, rows
-  int k0, k_len;   // first packed key row, key rows; the cache operators: k0 = row of the block table
-  int tile0;       // first tile of the sequence in the launch
+  int k0, k_len;   // first packed key row, key rows; the cache operators: row of the block table; attention
+                   // over it: queries of the sequence from q0 on (a chunk's: more than q_len)
+  int tile0;       // first tile (or unit: tile and part of the keys) of the sequence in the launch
 };
 
 // What the three attention kernels share. Strides in elements.
 struct AttnCommon {
   const void *q;
   void *out;
-  float *ws;                         // partial results: see k_cond_join
+  float *ws;                         // partial results: see join_row
   int64_t q_row, q_head, o_row, o_head;
   float sc;                          // scale * log2(e)
   int d, hkv, rep;
@@ -34,6 +35,7 @@ struct CrossArgs : AttnCommon {
   const void *k, *v;
   const uint8_t *mask;
   int64_t k_row, k_head, v_row, v_head;
+  int per;                           // key tiles of a part
   CondSeq seq[kCondSeqs];
 };
 

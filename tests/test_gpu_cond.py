@@ -439,6 +439,10 @@ CACHED = [
     ([100, 1, 33, 1], [320, 96, 33, 2000], 12, 4, 64),   # both kernels in one call
     ([20], [3000], 4, 2, 128),                     # rows past one tile, keys split
     ([16], [40], 8, 4, 64), ([17], [40], 8, 4, 64),
+    # enough rows for the tiles of 128: over tables that fit LDS, of each width, and that do not
+    ([600, 1, 90], [320, 96, 77], 16, 8, 128), ([1030, 70], [128, 500], 16, 8, 128), ([700, 33], [640, 31], 8, 8, 64),
+    ([410, 40], [96, 40], 10, 10, 64), ([900, 65], [900, 700], 12, 4, 64), ([300, 170], [1500, 200], 16, 16, 128),
+    ([40, 3], [50, 700], 66, 2, 64),               # 33 heads: one token is more than 32 rows
 ]
 
 
@@ -553,17 +557,18 @@ def test_kv8_many_sequences(torch, C):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("ql,kl,width", [(16, 40, None), (64, 64, None), (64, 64, 30)])
-def test_kv8_values_of_unseen_blocks(torch, C, ql, kl, width, dtype):
+@pytest.mark.parametrize("ql,kl,width,hq,h", [(16, 40, None, 4, 2), (64, 64, None, 4, 2), (64, 64, 30, 4, 2),
+                                              (300, 310, None, 32, 4), (300, 310, 40, 32, 4)])
+def test_kv8_values_of_unseen_blocks(torch, C, ql, kl, width, hq, h, dtype):
     """A causal row's result does not depend on how large the values are that it does not see."""
     _say("cached, values of unseen blocks", ql, kl, width, dtype)
-    h, d = 2, 64
+    d = 64
     v = torch.randn(kl, h, d, generator=torch.Generator().manual_seed(93))
     v[32:] *= 2.0 ** 40
     cache, table, kv, _, _ = _fill(torch, C, [kl], h, d, width=width)
     k = _randn(torch, 94, kl, h, d)
     C.kv8_append(cache, table, kv, k, v.to(torch.bfloat16).cuda(), [kl])
-    q = _randn(torch, 95, ql, 4, d, dtype=dtype)
+    q = _randn(torch, 95, ql, hq, d, dtype=dtype)
     got = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
     (kk, vv), = _held(torch, cache, table, [kl])
     see = np.arange(kl)[None] <= kl - ql + np.arange(ql)[:, None]
