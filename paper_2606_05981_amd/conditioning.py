@@ -144,7 +144,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: S
     sc = 1.0 / math.sqrt(d) if scale is None else float(scale)
 
     def call(st):
-        o = torch.empty((q.shape[0], hq, d), dtype=dtype, device=dev) if out is None else out
+        o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         shape = B.ATTN_SHAPE.pack(hq, hkv, d, _DTYPE[dtype], sc, *sq, *sk, *sv, *((hq * d, d) if so is None else so))
         _spaced(dev, "mte_cross_attention", False,
                 lambda: B.mte_cross_attention_workspace(shape, ql, n_q, kl, n_kv, idx),
@@ -174,8 +174,8 @@ def kv8_cache(n_blocks: int, n_kv_heads: int, head_dim: int, device="cuda") -> K
                     torch.full((n_blocks, n_kv_heads, 2), 2.0 ** -126, dtype=torch.float32, device=device))
 
 
-def _cache(cache, table, kv_lens, n: int, dev: torch.device):
-    """Checks a cache with the table and lengths of n sequences -> (mte_kv8 as bytes, heads, head_dim, width, table row)."""
+def _refuse_cache(cache, table, kv_lens, n: int, dev: torch.device):
+    """Raises for what does not fit of a cache with the table and lengths of n sequences."""
     kc, vc, sc = cache
     for name, t, dt in (("k_codes", kc, torch.uint8), ("v_codes", vc, torch.uint8), ("scales", sc, torch.float32)):
         if not isinstance(t, torch.Tensor) or t.dtype != dt or t.device != dev or not t.is_contiguous():
@@ -183,17 +183,33 @@ def _cache(cache, table, kv_lens, n: int, dev: torch.device):
     if vc.dim() != 4:
         raise ValueError("cache v_codes: expected [blocks, heads, head_dim, 32]")
     nb, h, d, _ = vc.shape
-    if tuple(vc.shape) != (nb, h, d, 32) or tuple(kc.shape) != (nb, h, d // 16, 32, 16) or \
-            tuple(sc.shape) != (nb, h, 2):
+    if vc.shape != (nb, h, d, 32) or kc.shape != (nb, h, d // 16, 32, 16) or sc.shape != (nb, h, 2):
         raise ValueError(f"cache: shapes {tuple(kc.shape)}, {tuple(vc.shape)}, {tuple(sc.shape)} do not fit together")
     if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.device != dev or \
             table.dim() != 2 or table.shape[0] != n or not 0 < table.shape[1] < 1 << 26 or \
             (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError(f"table: expected an int32 [{n}, blocks] tensor on {dev} with contiguous rows")
-    if not isinstance(kv_lens, torch.Tensor) or kv_lens.dtype != torch.int32 or kv_lens.device != dev or \
-            tuple(kv_lens.shape) != (n,) or not kv_lens.is_contiguous():
-        raise ValueError(f"kv_lens: expected a contiguous int32 tensor of {n} lengths on {dev}")
-    return B.KV8.pack(kc.data_ptr(), vc.data_ptr(), sc.data_ptr(), nb, h, d), h, d, table.shape[1], table.stride(0)
+    raise ValueError(f"kv_lens: expected a contiguous int32 tensor of {n} lengths on {dev}")
+
+
+def _cache(cache, table, kv_lens, n: int, dev: torch.device):
+    """Checks a cache with the table and lengths of n sequences -> (mte_kv8 as bytes, heads, head_dim, width, table row)."""
+    kc, vc, sc = cache
+    try:
+        nb, h, d, _ = vc.shape
+        width, i = table.shape[1], dev.index
+        fits = (kc.dtype is vc.dtype is torch.uint8 and sc.dtype is torch.float32 and
+                table.dtype is kv_lens.dtype is torch.int32 and
+                kc.get_device() == vc.get_device() == sc.get_device() == table.get_device() == kv_lens.get_device() == i and
+                vc.shape == (nb, h, d, 32) and kc.shape == (nb, h, d // 16, 32, 16) and sc.shape == (nb, h, 2) and
+                table.shape == (n, width) and 0 < width < 1 << 26 and (width == 1 or table.stride(1) == 1) and
+                kv_lens.shape == (n,) and kc.is_contiguous() and vc.is_contiguous() and sc.is_contiguous() and
+                kv_lens.is_contiguous())
+    except (AttributeError, ValueError, IndexError):
+        fits = False
+    if not fits:
+        _refuse_cache(cache, table, kv_lens, n, dev)
+    return B.KV8.pack(kc.data_ptr(), vc.data_ptr(), sc.data_ptr(), nb, h, d), h, d, width, table.stride(0)
 
 
 def kv8_append(cache, table: torch.Tensor, kv_lens: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -255,7 +271,7 @@ def kv8_attention(q: torch.Tensor, cache, table: torch.Tensor, kv_lens: torch.Te
     sc = 1.0 / math.sqrt(d) if scale is None else float(scale)
 
     def call(st):
-        o = torch.empty((q.shape[0], hq, d), dtype=dtype, device=dev) if out is None else out
+        o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         shape = B.ATTN_SHAPE.pack(hq, hkv, d, _DTYPE[dtype], sc, *sq, 0, 0, 0, 0,
                                   *((hq * d, d) if so is None else so))
         _spaced(dev, "mte_kv8_attention", width > 16, lambda: B.mte_kv8_attention_workspace(shape, lens, n, width),
@@ -268,16 +284,17 @@ def kv8_attention(q: torch.Tensor, cache, table: torch.Tensor, kv_lens: torch.Te
 
 def _pixels(name: str, t: torch.Tensor):
     """(image stride, row stride, pixels) of a channels-last [N, P, C] or [N, H, W, C] tensor."""
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: expected contiguous channels (the last dimension), got strides {t.stride()}")
-    if t.dim() == 3:
-        row, px = t.stride(1), t.shape[1]
+    shape, st = t.shape, t.stride()
+    if shape[-1] > 1 and st[-1] != 1:
+        raise ValueError(f"{name}: expected contiguous channels (the last dimension), got strides {st}")
+    if len(shape) == 3:
+        row, px = st[1], shape[1]
     else:
-        h, w = t.shape[1], t.shape[2]
-        if h > 1 and w > 1 and t.stride(1) != w * t.stride(2):
-            raise ValueError(f"{name}: expected pixels at one stride, got strides {t.stride()}")
-        row, px = t.stride(2) if w > 1 else t.stride(1), h * w
-    return t.stride(0) if t.shape[0] > 1 else 0, row if px > 1 else 0, px
+        h, w = shape[1], shape[2]
+        if h > 1 and w > 1 and st[1] != w * st[2]:
+            raise ValueError(f"{name}: expected pixels at one stride, got strides {st}")
+        row, px = st[2] if w > 1 else st[1], h * w
+    return st[0] if shape[0] > 1 else 0, row if px > 1 else 0, px
 
 
 def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None,
@@ -310,7 +327,7 @@ def group_norm(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = Non
 
     def call(st):
         if out is None:
-            y, yi, yr = torch.empty(x.shape, dtype=dtype, device=dev), px * C, C
+            y, yi, yr = torch.empty_like(x, memory_format=torch.contiguous_format), px * C, C
         else:
             y, yi, yr = out, oi, orow
         _spaced(dev, "mte_group_norm", False, lambda: B.mte_group_norm_workspace(n, px, C, groups, _DTYPE[dtype]),

@@ -1,23 +1,24 @@
-// Attention of packed queries to conditioning tokens: keys and values as rows
-// (k_cross), or as e4m3 codes in blocks of 32 tokens (k_kv8_rows, k_kv8_tiles).
+// Attention of packed queries to conditioning tokens: keys and values as rows (k_cross,
+// k_cross_stream), or as e4m3 codes in blocks of 32 tokens (k_kv8_rows, k_kv8_tiles, k_kv8_res).
 //
 //   o[i, h] = sum_j p_ij v[j, g],  p_ij = exp(s_ij - m_i) / sum_j exp(s_ij - m_i),
 //   s_ij = scale q[i, h] . k[j, g],  g = h / rep
 //
-// Rows. The rep query heads of a kv head read the same keys, so the rows of a
-// matrix tile are (token, head) pairs: row r of a sequence is token r / rep, head
-// g rep + r % rep. One query with grouped heads fills rep rows, not one.
+// Rows. The rep query heads of a kv head read the same keys, so the rows of a matrix tile are (token,
+// head) pairs: row r of a sequence is token r / rep, head g rep + r % rep. One query with grouped
+// heads fills rep rows, not one.
 //
-// Matrix core forms (32x32, as in attention.hip): S^T = K Q^T leaves each lane the
-// scores of one row (lane % 32) for 16 of 32 keys, key 8 (r / 4) + 4 (lane / 32) +
-// r % 4 in register r, so maxima and sums are per-lane loops and one exchange between
-// the wave's halves, and the probabilities are already the B operand of
-// O^T = V^T P^T, if V^T is read with its keys in that same order.
+// Matrix core forms (32x32, as in attention.hip): S^T = K Q^T leaves each lane the scores of one row
+// (lane % 32) for 16 of 32 keys, key 8 (r / 4) + 4 (lane / 32) + r % 4 in register r, so maxima and
+// sums are per-lane loops and one exchange between the wave's halves, and the probabilities are
+// already the B operand of O^T = V^T P^T, if V^T is read with its keys in that same order.
 //
-// One pass over the keys with the running maximum m and sum l of each row (fp32,
-// log2 units); O is rescaled where m moved. Key ranges may be split: over waves of a
-// workgroup (joined through LDS) and over workgroups (partial O, m, l in the
-// workspace, joined by k_cond_join).
+// One pass over the keys with a running reference m and sum l of each row (fp32, log2 units); O is
+// rescaled where m moves. Key ranges may be split: over the waves of a workgroup (joined through
+// LDS) and over workgroups (O / l, m, l of each part in the workspace, joined by a second launch).
+//
+// Roundings to fewer than 32 bits: the probabilities, as the operand of the second product (Probs,
+// CodeProbs), and the result. Scores, m, l, O and the joins are fp32.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -269,10 +270,13 @@ __device__ __forceinline__ void store_part(const AttnCommon &a, Rows<ND> &st, fl
 
 // ---- keys and values as rows --------------------------------------------------------------------
 //
-// A workgroup of four waves serves 32 RW rows of one sequence and kv head; the other
-// 4 / RW ways of its waves split the keys of a tile (few rows: RW = 1). Key tiles go
-// global -> registers -> LDS, the next tile's loads in flight while one is computed;
-// rows past the end and masked value rows become zeros on the way.
+// k_cross: a workgroup of four waves serves 32 RW rows of one sequence and kv head; the other 4 / RW ways of
+// its waves split the keys of a tile (few rows: RW = 1). Key tiles go global -> registers -> LDS, the
+// next tile's loads in flight while one is computed (where the registers hold them: not fp32 tiles of
+// 128 keys of 128); rows past the end and masked value rows become zeros on the way.
+// Bound by latency: launch, sequence table, first loads, softmax, store, one after the other (16 x 1
+// tokens of 2 x 8 heads of 128 over 96: 7.5 us for 6.4 MB); fp32 by its matrix instructions, an eighth of
+// bf16's rate (12 x 918 rows of 8 heads over 3 to 287 keys: 59.6 us, 50 TFLOP/s).
 // LDS: keys as 16-byte chunks in the order of the MFMA operand ([32 keys][chunk c]:
 // lane = key), the key index xored with the chunk so that neither the row-wise
 // writes nor the operand reads meet in a bank; values as rows, chunks xored so that the
@@ -640,6 +644,11 @@ __device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, fl
 // stay zero (a lane that skips a copy leaves its 16 bytes alone; no copy is skipped whole).
 // The ring's idle slots turn the rows (QTile): before the first barrier the last ones, after the
 // last barrier those that the last tile does not use.
+// Bound by the rows in and out where the keys are few (16 x 4096 rows of 10 heads of 64 over 96 keys: 46 us,
+// 3.7 TB/s; the same copies without any arithmetic 40), by both where they are not (32 x 1000 of 2 x 8 heads
+// of 128 over 102 to 319: 107 us, 510 TFLOP/s, 2.7 TB/s; rows alone 53, with the key copies 78). Six or eight
+// waves a workgroup (125 to 155 us), the keys whole in LDS (129), scores of one tile among the value
+// products of the one before (registers spill) and XCD-contiguous tiles (114 to 130) were slower.
 template <int NCH> __device__ __forceinline__ int key_swz(int r, int c) { return c ^ (r & (NCH - 1)); }
 template <int DP> struct Stream {
   static constexpr int NCH = DP / 8, TILE = 32 * NCH;     // chunks a row; 16-byte chunks of a tile's keys
@@ -997,7 +1006,9 @@ __device__ __forceinline__ Cut cut_of(const Kv8AttnArgs &a, int target, int at, 
 
 // Few rows (at most 32 a sequence, or chunk of one): bound by the codes that stream in. Each of the four waves
 // takes every fourth block of the split's range and loads its codes straight into MFMA operand
-// order, 16 bytes a lane and 1 KB a load, the next block's while one is computed.
+// order, 16 bytes a lane and 1 KB a load, the next block's while one is computed. One token of 2 x 8 heads
+// of 128 over 131071: 59.5 us with the join, 4.5 TB/s; 32 over 96 to 8192: 56.3 us, 4.1 TB/s (parts of
+// equal tables instead of equal work: 115).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(Kv8AttnArgs a, int target) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32;
@@ -1081,7 +1092,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
 
 // Many rows: four waves of 32 rows; two blocks of codes a step are widened once per
 // workgroup on their way into LDS, in MFMA operand order (1 KB of lanes a fragment,
-// free of bank conflicts), the next step's codes in flight in registers.
+// free of bank conflicts), the next step's codes in flight in registers. Bound by the matrix instructions
+// and the softmax between them, at one or two waves a SIMD (1000 of 2 x 8 heads of 128 over 1000,
+// causal, in four parts: 31.5 us, 130 TFLOP/s).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(Kv8AttnArgs a) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32;
@@ -1177,7 +1190,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
 // Many rows over a cache that fits LDS whole once widened. Lane j holds block j's scales and how many of
 // its tokens count (none: no such block). O is in units of the largest value scale so far, as in the
 // other kernels: one for all blocks, of which a causal row sees the first, would push that row's
-// probabilities below fp16.
+// probabilities below fp16. A wave takes several row tiles over codes widened once.
+// Bound by the matrix instructions and the softmax between them, and by the one pass of staging that a
+// workgroup waits for (16 x 1024 of 2 x 8 heads of 128 over 320: 61.5 us, 700 TFLOP/s, 2.4 TB/s).
 template <typename T, int D, int NW, bool BOX>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void k_kv8_res(Kv8AttnArgs a, int chunk) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32, NF = D / 8;

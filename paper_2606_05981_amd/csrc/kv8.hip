@@ -3,9 +3,12 @@
 // A workgroup serves one block of 32 tokens and one kv head, keys and values: a
 // thread holds 16 consecutive d of one token. The maximum of the block's new rows
 // fixes the scale, codes go out 16 bytes a thread; values are turned through LDS
-// ([d][32 tokens], the tokens in the matrix core's order). Bound by the rows read and
-// codes written once each; a block that holds older tokens is read, merged and
-// written whole (8 KB a head of 128).
+// ([d][32 tokens], the tokens in the matrix core's order). A block that holds older
+// tokens is read, merged and written whole (8 KB a head of 128).
+// Long appends and reads are bound by the rows and codes, each moved once, and by all workgroups
+// being resident at once, so that reading, scaling and writing hardly overlap (16 x 320 tokens of 8
+// heads of 128: append 12.7 us, read 9.5 us, 2.5 and 3.3 TB/s); single tokens by the chain of length, table,
+// block, maximum, codes (64 sequences: append 6.9 us, read 4.9 us).
 #include <algorithm>
 
 #include "../../include/mte.h"
