@@ -545,14 +545,16 @@ __device__ __forceinline__ void attend_steps(Rows<ND> &st, int n, SC scores, MA 
 constexpr int kBox = 4096;          // a wave's LDS for it
 // A store that leaves nothing in L2 (written out: as a branch of two stores of one value the
 // compiler makes one plain store of it).
-__device__ __forceinline__ void store_past_caches(u32x4 *p, const u32x4 &x) {
-  asm volatile("global_store_dwordx4 %0, %1, off nt" ::"v"(p), "v"(x) : "memory");
+__device__ __forceinline__ void store_past_caches(char *base, uint32_t off, const u32x4 &x) {
+  asm volatile("global_store_dwordx4 %0, %1, %2 nt" ::"v"(off), "v"(x), "s"(base) : "memory");
 }
 // Rows of a tile between memory and the lanes that own them, 128 bytes of a row at a time: a load or
 // store takes 8 whole lines (8 lanes each), and 4 KB of LDS of the wave's own turn them (chunks
 // xored with the row: neither side meets in a bank). Straight from the owning lanes an access
 // would take 32 bytes of 32 rows: on 65536 rows of 10 heads of 64, copied, 40 us against 31.5.
-// The rows of the tile: r0 .. of `rows`, token r / rep and head g rep + r % rep.
+// The rows of the tile: r0 .. of `rows`, token r / rep and head g rep + r % rep. Their addresses are a
+// wave-uniform base and 32-bit offsets (the host's AttnProblem::near_tiles): products of 64 bits are
+// quarter-rate instructions (16 x 4096 rows of 10 heads of 64: 44.8 us, with them 46.0).
 struct TileRows {
   int64_t tok0;        // token of row r0, absolute
   int rem0, left;      // r0 % rep, rows that exist
@@ -564,28 +566,32 @@ struct TileRows {
     left = rows - r0;
     inv = 1.f / (float)a.rep;
   }
-  // token offset of row r0 + i and its head within the group (small numbers: exact in fp32)
-  __device__ __forceinline__ int split(int i, int rep, int &head) const {
-    const int x = rem0 + i, t = (int)(((float)x + 0.5f) * inv);
-    head = x - t * rep;
-    return t;
+  template <typename T> __device__ __forceinline__ T *base(T *p, int64_t row, int64_t head, int g, int rep) const {
+    const uint64_t x = (uint64_t)(uintptr_t)(p + tok0 * row + (int64_t)(g * rep) * head);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (T *)(uintptr_t)((uint64_t)hi << 32 | lo);
+  }
+  // elements from the base to row r0 + i
+  __device__ __forceinline__ uint32_t offset(int i, int64_t row, int64_t head, int rep) const {
+    if (rep == 1) return __umul24(i, (uint32_t)row);
+    const int x = rem0 + i, t = (int)(((float)x + 0.5f) * inv);   // small numbers: exact in fp32
+    return __umul24(t, (uint32_t)row) + (uint32_t)(x - t * rep) * (uint32_t)head;
   }
 };
 template <typename T, int DP> struct QTile {
   static constexpr int PARTS = DP * sizeof(T) / 128, E = 16 / sizeof(T);
   u32x4 x[PARTS * 4];
   __device__ __forceinline__ void load(const AttnCommon &a, const TileRows &t, int g, int lane) {
+    const char *base = (const char *)t.base((const T *)a.q, a.q_row, a.q_head, g, a.rep);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = 8 * i + (lane >> 3);
-      int head;
-      const int tok = t.split(r, a.rep, head);
-      const T *row = (const T *)a.q + (t.tok0 + tok) * a.q_row + (int64_t)(g * a.rep + head) * a.q_head;
+      const uint32_t off = t.offset(r, a.q_row, a.q_head, a.rep);
 #pragma unroll
       for (int j = 0; j < PARTS; ++j) {
         const int c = (8 * j + (lane & 7)) * E;
         x[4 * j + i] = u32x4{0, 0, 0, 0};
-        if (r < t.left && c < a.d) x[4 * j + i] = *(const u32x4 *)(row + c);
+        if (r < t.left && c < a.d) x[4 * j + i] = *(const u32x4 *)(base + (off + c) * (uint32_t)sizeof(T));
       }
     }
   }
@@ -606,6 +612,10 @@ __device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, fl
   const float l = st.l + __shfl_xor(st.l, 32, kWave);
   const float inv = l > 0.f ? vscale / l : 0.f;
   const int r = lane & 31, h = lane >> 5;
+  char *base = (char *)t.base((T *)a.out, a.o_row, a.o_head, g, a.rep);
+  uint32_t off[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) off[i] = t.offset(8 * i + (lane >> 3), a.o_row, a.o_head, a.rep);
 #pragma unroll
   for (int j = 0; j < PARTS; ++j) {
     if constexpr (sizeof(T) == 4) {
@@ -622,12 +632,10 @@ __device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, fl
     for (int i = 0; i < 4; ++i) {
       const u32x4 x = box[64 * i + (lane & 56) + ((lane & 7) ^ (lane >> 3))];
       const int row = 8 * i + (lane >> 3), c = (8 * j + (lane & 7)) * E;
-      int head;
-      const int tok = t.split(row, a.rep, head);
-      u32x4 *to = (u32x4 *)((T *)a.out + (t.tok0 + tok) * a.o_row + (int64_t)(g * a.rep + head) * a.o_head + c);
+      const uint32_t at = (off[i] + c) * (uint32_t)sizeof(T);
       if (row < t.left && c < a.d) {
-        if (a.big) store_past_caches(to, x);
-        else *to = x;
+        if (a.big) store_past_caches(base, at, x);
+        else *(u32x4 *)(base + at) = x;
       }
     }
   }
@@ -685,8 +693,8 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
       const int r = RPC * (wave * CP + i) + lane / NCH, p = lane % NCH;
       const int row = min(r, klen - 1 - t * 32);
       const int kc = key_swz<NCH>(r, p) * 8, vc = value_chunk<NCH, true>(r, p) * 8;
-      if (kc < a.d) dma16(kb, (uint32_t)(row * (int)a.k_row + kc) * 2u, to + i * 1024);
-      if (vc < a.d) dma16(vb, (uint32_t)(row * (int)a.v_row + vc) * 2u, to + (S::TILE + i * 64) * 16);
+      if (kc < a.d) dma16(kb, (__umul24(row, (uint32_t)a.k_row) + kc) * 2u, to + i * 1024);
+      if (vc < a.d) dma16(vb, (__umul24(row, (uint32_t)a.v_row) + vc) * 2u, to + (S::TILE + i * 64) * 16);
     }
   };
   const TileRows rw(a, sq, r0, rows);
@@ -1531,7 +1539,7 @@ static Plan cross_plan(const AttnProblem &p, const int32_t *kv_lens, const int32
     pl.TR = 32;
     pl.KT = 128;
     least = 4;
-  } else if (p.dtype == MTE_BF16 && p.near_rows) {
+  } else if (p.dtype == MTE_BF16 && p.near_rows && p.near_tiles) {
     pl.kind = Plan::COPIES;
     pl.KT = 32;
     least = 8;
@@ -1752,7 +1760,7 @@ static Plan kv8_plan(const AttnProblem &p, int width, bool few) {
     // LDS is shared by two and more workgroups of four waves where that leaves each half of it, else
     // eight waves have it to themselves; rows are turned in LDS where there is room (bf16: fp32 is
     // bound by its products, and has no registers to spare).
-    const int room = p.dtype == MTE_BF16 ? kBox : 0, simd = p.dtype != MTE_BF16 ? 1 : p.c.d == 64 ? 3 : 2;
+    const int room = p.dtype == MTE_BF16 && p.near_tiles ? kBox : 0, simd = p.dtype != MTE_BF16 ? 1 : p.c.d == 64 ? 3 : 2;
     pl.kind = Plan::RESIDENT;
     pl.nw = res + 4 * room <= kLds / 2 ? 4 : 8;
     pl.box = room > 0 && res + pl.nw * room <= kLds;
@@ -1802,7 +1810,8 @@ static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, const Plan &pl, hipSt
   hipError_t e;
   if (pl.kind == Plan::RESIDENT) {
     constexpr bool B16 = sizeof(T) == 2;
-    auto kern = pl.nw == 4 ? k_kv8_res<T, D, 4, B16> : pl.box ? k_kv8_res<T, D, 8, B16> : k_kv8_res<T, D, 8, false>;
+    auto kern = pl.box ? (pl.nw == 4 ? k_kv8_res<T, D, 4, B16> : k_kv8_res<T, D, 8, B16>)
+                       : (pl.nw == 4 ? k_kv8_res<T, D, 4, false> : k_kv8_res<T, D, 8, false>);
     if ((e = allow_lds(kern, pl.lds)) != hipSuccess) return e;
     hipLaunchKernelGGL(kern, grid, dim3(64 * pl.nw), pl.lds, s, a, pl.TR);
     return hipGetLastError();

@@ -67,6 +67,7 @@ struct AttnProblem {
   AttnCommon c;
   int dtype;                         // MTE_F32 / MTE_BF16
   bool near_rows;                    // key and value rows under 2^24 elements apart: 32 of them are 32-bit offsets
+  bool near_tiles;                   // the same of the query and result rows of a tile, heads of a group included
   const int32_t *q_lens;
   int n;
 };

@@ -245,6 +245,27 @@ def test_cross_attention_rows_far_apart(torch, C, ql, kl, d):
                  "bf16")
 
 
+@pytest.mark.parametrize("step", [1 << 29, 1 << 30])
+def test_attention_heads_far_apart(torch, C, step):
+    """Many rows of queries and results whose heads lie as far apart as 32-bit offsets reach, and farther."""
+    _say(f"attention, heads {step} elements apart")
+    n, hq, hkv, d = 2100, 4, 2, 64
+    buf = torch.empty((hq - 1) * step + n * d, dtype=torch.bfloat16, device="cuda")
+    far = buf.as_strided((n, hq, d), (d, step, 1))
+    q = _randn(torch, 86, n, hq, d)
+    k, v = _randn(torch, 87, 96, hkv, d), _randn(torch, 88, 96, hkv, d)
+    ref = O.cross(_f64(q), _f64(k), _f64(v), [n], [96])
+    cache = C.kv8_cache(3, hkv, d)
+    table, kv = _i32(torch, [[2, 0, 1]]), _i32(torch, [96])
+    C.kv8_append(cache, table, kv, k, v, [96])
+    plain = C.kv8_attention(q, cache, table, kv, [n])
+    far.copy_(q)
+    _compare(C.cross_attention(far, k, v, [n], [96], out=far), *ref, 96, d, "bf16")
+    far.copy_(q)
+    got = C.kv8_attention(far, cache, table, kv, [n], out=far)
+    assert got is far and torch.equal(plain, far)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_cross_attention_index_split(torch, C, dtype):
     """Several sequences, long and short, over one long one that is split; a masked half."""
