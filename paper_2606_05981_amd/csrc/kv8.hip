@@ -23,6 +23,11 @@ constexpr int kThreads = 256;
 // Position of token t of a block in a row of the value codes.
 __device__ __forceinline__ int v_pos(int t) { return 16 * ((t >> 2) & 1) + 8 * (t >> 4) + 4 * ((t >> 3) & 1) + (t & 3); }
 
+// LDS row of the 32 value codes of one d: 16-byte aligned, and 16 rows (a thread's) and 4 tokens on lie in
+// banks of their own (without the last term all pieces of d meet in one: 2 of an append's 12.7 us).
+__device__ __forceinline__ int v_row(int d) { return d * 48 + (d >> 4) * 32; }
+constexpr int v_bytes(int D) { return D * 48 + (D >> 4) * 32; }
+
 // Exponent of the smallest 2^e >= 2^-126 with amax <= 448 * 2^e (448 = 0.875 * 2^9, amax =
 // f * 2^x with f in [0.5, 1)); infinities take the largest, 2^120.
 __device__ __forceinline__ int scale_exp(float amax) {
@@ -99,8 +104,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
   constexpr int PC = D / 16;
   constexpr int NT = D == 128 ? 2 : 1;              // tensors a thread serves
-  constexpr int VP = 48;                            // LDS row of 32 value codes: 16-byte aligned, spread over banks
-  __shared__ __attribute__((aligned(16))) uint8_t sv[D * VP];
+  __shared__ __attribute__((aligned(16))) uint8_t sv[v_bytes(D)];
   __shared__ float smax[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, blockIdx.x)];
@@ -154,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
     for (int s = 32; s >= 1; s >>= 1) mx[t] = warp_max_xor(mx[t], s);
     if (lane == 0) smax[t][wave] = mx[t];
   }
-  if (turn) *(u32x4 *)(sv + (vi >> 1) * VP + (vi & 1) * 16) = v_old;   // [d][pos]
+  if (turn) *(u32x4 *)(sv + v_row(vi >> 1) + (vi & 1) * 16) = v_old;   // [d][pos]
   __syncthreads();
   int e_new[2], e_old[2];
 #pragma unroll
@@ -179,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
         for (int q = 0; q < 4; ++q) {
           uint32_t b = 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) b |= (uint32_t)sv[(pc * 16 + 4 * q + e) * VP + v_pos(tok)] << (8 * e);
+          for (int e = 0; e < 4; ++e) b |= (uint32_t)sv[v_row(pc * 16 + 4 * q + e) + v_pos(tok)] << (8 * e);
           o[q] = b;
         }
       }
@@ -197,12 +201,12 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sv[(pc * 16 + 4 * q + i) * VP + v_pos(tok)] = (uint8_t)(o[q] >> (8 * i));
+        for (int i = 0; i < 4; ++i) sv[v_row(pc * 16 + 4 * q + i) + v_pos(tok)] = (uint8_t)(o[q] >> (8 * i));
     }
   }
   __syncthreads();
   for (int i = tid; i < 32 * D / 16; i += kThreads)
-    ((u32x4 *)vc)[i] = *(const u32x4 *)(sv + (i >> 1) * VP + (i & 1) * 16);
+    ((u32x4 *)vc)[i] = *(const u32x4 *)(sv + v_row(i >> 1) + (i & 1) * 16);
   if (tid < 2) a.c.scales[w.at * 2 + tid] = ldexpf(1.f, tid == 0 ? e_new[0] : e_new[1]);
 }
 
@@ -210,8 +214,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void k_kv8_read(Kv8RowsArgs a) {
   constexpr int PC = D / 16;
   constexpr int NT = D == 128 ? 2 : 1;
-  constexpr int VP = 48;
-  __shared__ __attribute__((aligned(16))) uint8_t sv[D * VP];
+  __shared__ __attribute__((aligned(16))) uint8_t sv[v_bytes(D)];
   const int tid = threadIdx.x;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, blockIdx.x)];
   const int g = blockIdx.y;
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void k_kv8_read(Kv8RowsArgs a) {
   uint8_t *kc = a.c.k_codes + w.at * (32 * D), *vc = a.c.v_codes + w.at * (32 * D);
   if (w.ok) {
     for (int i = tid; i < 32 * D / 16; i += kThreads)
-      *(u32x4 *)(sv + (i >> 1) * VP + (i & 1) * 16) = ((const u32x4 *)vc)[i];
+      *(u32x4 *)(sv + v_row(i >> 1) + (i & 1) * 16) = ((const u32x4 *)vc)[i];
   }
   __syncthreads();
   const int sub = tid % (32 * PC), tok = sub / PC, pc = sub % PC;
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void k_kv8_read(Kv8RowsArgs a) {
       } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          x[e] = __builtin_amdgcn_cvt_f32_fp8((int)sv[(pc * 16 + e) * VP + v_pos(tok)], 0);
+          x[e] = __builtin_amdgcn_cvt_f32_fp8((int)sv[v_row(pc * 16 + e) + v_pos(tok)], 0);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] *= s;
