@@ -552,6 +552,8 @@ __device__ __forceinline__ void store_past_caches(char *base, uint32_t off, cons
 // store takes 8 whole lines (8 lanes each), and 4 KB of LDS of the wave's own turn them (chunks
 // xored with the row: neither side meets in a bank). Straight from the owning lanes an access
 // would take 32 bytes of 32 rows: on 65536 rows of 10 heads of 64, copied, 40 us against 31.5.
+// Place of chunk c of row r in a box.
+__device__ __forceinline__ int box_at(int r, int c) { return r * 8 + (c ^ (r & 7)); }
 // The rows of the tile: r0 .. of `rows`, token r / rep and head g rep + r % rep. Their addresses are a
 // wave-uniform base and 32-bit offsets (the host's AttnProblem::near_tiles): products of 64 bits are
 // quarter-rate instructions (16 x 4096 rows of 10 heads of 64: 44.8 us, with them 46.0).
@@ -598,11 +600,10 @@ template <typename T, int DP> struct QTile {
   // part j into the wave's 4 KB; then chunk c (of 8) of this lane's row
   __device__ __forceinline__ void spread(u32x4 *box, int j, int lane) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) box[64 * i + (lane & 56) + ((lane & 7) ^ (lane >> 3))] = x[4 * j + i];
+    for (int i = 0; i < 4; ++i) box[box_at(8 * i + (lane >> 3), lane & 7)] = x[4 * j + i];
   }
   static __device__ __forceinline__ u32x4 chunk(const u32x4 *box, int c, int lane) {
-    const int r = lane & 31;
-    return box[r * 8 + (c ^ (r & 7))];
+    return box[box_at(lane & 31, c)];
   }
 };
 template <typename T, int ND>
@@ -621,17 +622,17 @@ __device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, fl
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int b = 0; b < 4; ++b)
-        box[r * 8 + ((2 * b + h) ^ (r & 7))] =
+        box[box_at(r, 2 * b + h)] =
             __builtin_bit_cast(u32x4, f32x4{st.o[j][4 * b] * inv, st.o[j][4 * b + 1] * inv, st.o[j][4 * b + 2] * inv,
                                             st.o[j][4 * b + 3] * inv});
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) box[r * 8 + ((2 * q + h) ^ (r & 7))] = out_chunk(st.o[2 * j + (q >> 1)], q & 1, inv);
+      for (int q = 0; q < 4; ++q) box[box_at(r, 2 * q + h)] = out_chunk(st.o[2 * j + (q >> 1)], q & 1, inv);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const u32x4 x = box[64 * i + (lane & 56) + ((lane & 7) ^ (lane >> 3))];
       const int row = 8 * i + (lane >> 3), c = (8 * j + (lane & 7)) * E;
+      const u32x4 x = box[box_at(row, lane & 7)];
       const uint32_t at = (off[i] + c) * (uint32_t)sizeof(T);
       if (row < t.left && c < a.d) {
         if (a.big) store_past_caches(base, at, x);
@@ -657,7 +658,8 @@ __device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, fl
 // of 128 over 102 to 319: 107 us, 510 TFLOP/s, 2.7 TB/s; rows alone 53, with the key copies 78). Six or eight
 // waves a workgroup (125 to 155 us), the keys whole in LDS (129), scores of one tile among the value
 // products of the one before (registers spill) and XCD-contiguous tiles (114 to 130) were slower.
-template <int NCH> __device__ __forceinline__ int key_swz(int r, int c) { return c ^ (r & (NCH - 1)); }
+// (of 8 chunks, two rows fill the banks: swizzled by the pair, a quarter of the conflicts that r & 7 leaves)
+template <int NCH> __device__ __forceinline__ int key_swz(int r, int c) { return c ^ (NCH == 8 ? (r >> 1) & 7 : r & (NCH - 1)); }
 template <int DP> struct Stream {
   static constexpr int NCH = DP / 8, TILE = 32 * NCH;     // chunks a row; 16-byte chunks of a tile's keys
   static constexpr int NB = DP == 64 ? 4 : 3;             // two slots for the first tiles, and the waves' kBox
