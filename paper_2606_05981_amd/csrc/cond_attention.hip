@@ -653,9 +653,9 @@ __device__ __forceinline__ void store_tile(const AttnCommon &a, Rows<ND> &st, fl
 // stay zero (a lane that skips a copy leaves its 16 bytes alone; no copy is skipped whole).
 // The ring's idle slots turn the rows (QTile): before the first barrier the last ones, after the
 // last barrier those that the last tile does not use.
-// Bound by the rows in and out where the keys are few (16 x 4096 rows of 10 heads of 64 over 96 keys: 46 us,
-// 3.7 TB/s; the same copies without any arithmetic 40), by both where they are not (32 x 1000 of 2 x 8 heads
-// of 128 over 102 to 319: 107 us, 510 TFLOP/s, 2.7 TB/s; rows alone 53, with the key copies 78). Six or eight
+// Bound by the rows in and out where the keys are few (16 x 4096 rows of 10 heads of 64 over 96 keys: 44.3 us,
+// 3.9 TB/s; the same copies without any arithmetic 40), by both where they are not (32 x 1000 of 2 x 8 heads
+// of 128 over 102 to 319: 103 us, 540 TFLOP/s, 2.8 TB/s; rows alone 53, with the key copies 78). Six or eight
 // waves a workgroup (125 to 155 us), the keys whole in LDS (129), scores of one tile among the value
 // products of the one before (registers spill) and XCD-contiguous tiles (114 to 130) were slower.
 // (of 8 chunks, two rows fill the banks: swizzled by the pair, a quarter of the conflicts that r & 7 leaves)

@@ -7,8 +7,8 @@
 // tokens is read, merged and written whole (8 KB a head of 128).
 // Long appends and reads are bound by the rows and codes, each moved once, and by all workgroups
 // being resident at once, so that reading, scaling and writing hardly overlap (16 x 320 tokens of 8
-// heads of 128: append 12.7 us, read 9.5 us, 2.5 and 3.3 TB/s); single tokens by the chain of length, table,
-// block, maximum, codes (64 sequences: append 6.9 us, read 4.9 us).
+// heads of 128: append 11.0 us, read 9.6 us, 2.9 and 3.3 TB/s); single tokens by the chain of length, table,
+// block, maximum, codes (64 sequences: append 6.3 us, read 4.6 us).
 #include <algorithm>
 
 #include "../../include/mte.h"
