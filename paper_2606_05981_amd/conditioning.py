@@ -146,7 +146,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: S
     def call(st):
         o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         shape = B.ATTN_SHAPE.pack(hq, hkv, d, _DTYPE[dtype], sc, *sq, *sk, *sv, *((hq * d, d) if so is None else so))
-        _spaced(dev, "mte_cross_attention", False,
+        _spaced(dev, "mte_cross_attention", n_kv > 0 and max(kv_keep) >= 384,
                 lambda: B.mte_cross_attention_workspace(shape, ql, n_q, kl, n_kv, idx),
                 lambda ws, n: B.lib.mte_cross_attention(
                     shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if key_mask is None else key_mask.data_ptr(),

@@ -54,15 +54,15 @@ __device__ __forceinline__ Unit unit_of(int hkv) {
 }
 
 // A unit of cross attention: a tile of TR rows over a part of the keys of its sequence. The host cuts every
-// key range of nt tiles into parts_of(nt, per) parts, `per` for the whole launch; the units of a
+// key range of nt tiles into parts_of(nt, cut) parts, `cut` for the whole launch; the units of a
 // sequence are its row tiles for the first part, then for the next.
-__host__ __device__ __forceinline__ int parts_of(int nt, int per) {   // parts of about `per`: 1/2 to 3/2 of it, or the rest
-  return nt <= per ? 1 : (nt + per / 2) / per;
+__host__ __device__ __forceinline__ int parts_of(int nt, const KeyCut &c) {   // whole, or parts of 4/5 to 5/4 of `per`
+  return nt < c.from || nt < 2 * c.per ? 1 : (nt + c.per / 2) / c.per;
 }
 struct Part { int row_tile, split, used, lo, hi; };     // key tiles [lo, hi)
-__device__ __forceinline__ Part part_of(const CondSeq &sq, int local, int rows, int TR, int nt, int per) {
+__device__ __forceinline__ Part part_of(const CondSeq &sq, int local, int rows, int TR, int nt, const KeyCut &cut) {
   Part p;
-  p.used = parts_of(nt, per);
+  p.used = parts_of(nt, cut);
   p.split = 0;
   p.row_tile = local;
   if (p.used > 1) {
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
   const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int klen = sq.k_len, rows = sq.q_len * a.rep;
-  const Part span = part_of(sq, tile - sq.tile0, rows, 32 * RW, (klen + KT - 1) / KT, a.per);
+  const Part span = part_of(sq, tile - sq.tile0, rows, 32 * RW, (klen + KT - 1) / KT, a.cut);
   const int r0 = span.row_tile * 32 * RW + rw * 32; // first row of the wave
   const int r = r0 + lrow;
   const bool live = r < rows;
@@ -678,7 +678,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
   const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int klen = sq.k_len, rows = sq.q_len * a.rep;
-  const Part span = part_of(sq, tile - sq.tile0, rows, 128, (klen + 31) >> 5, a.per);
+  const Part span = part_of(sq, tile - sq.tile0, rows, 128, (klen + 31) >> 5, a.cut);
   const int r0 = span.row_tile * 128 + wave * 32;
 
   const bf16 *kg = (const bf16 *)a.k + (int64_t)sq.k0 * a.k_row + (int64_t)g * a.k_head;
@@ -1467,7 +1467,7 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 struct Plan {
   enum { FEW, COPIES, STREAM, RESIDENT } kind = FEW;
   int TR = 0, KT = 0, n_split = 1, ws_rows = 0;
-  int per = 0;                                      // cross attention: key tiles of a part (part_of)
+  KeyCut cut{0, 0};                                 // cross attention: see part_of
   int target = 0;                                   // cached attention with few rows: parts (cut_of), 0: none
   int nw = 4, lds = 0;                              // RESIDENT: waves, LDS bytes,
   bool box = false;                                 // and whether they hold kBox a wave
@@ -1523,11 +1523,14 @@ static int64_t fill_tiles(const AttnProblem &p, Plan &pl, TAKE take) {
 //    rows; 1024 bf16 rows of 10 heads, 320 tiles, over 96: 6.5, against 5.6).
 //  COPIES (bf16): tiles of 128 rows, keys by LDS-direct copies.
 //  STREAM (fp32, or rows too far apart for 32-bit offsets): tiles of 128 rows, keys by registers.
-// Key ranges are cut into parts of the work that fills the chip once, kFill workgroups (and not below
-// 512 keys of FEW, 256 of the others: partial results and their join cost as much): few rows over
-// long keys are cut, and so is one long range among many short ones, whose workgroups would run
-// on alone (12 heads, 1500 rows of 9 sequences over 6 to 963 keys, those under 12 rows: 14.3 us, whole
-// 27.8; against it, 2500 rows of 8 heads over 356: 18.0, whole 14.0).
+// Key ranges are cut into parts of the work that fills the chip once, kFill workgroups: few rows over long keys
+// are cut, and so is one long range among many short ones, whose workgroups would run on alone. Parts
+// are of 256 keys at least (fp32 FEW: 128), and ranges are cut from the length at which that saves more than
+// the join costs, 4 us of a replayed graph and 6 of an eager call: 2 parts, FEW 1024 keys (fp32, where
+// a tile takes 3.5 or 7 us: 512 or 384). us cut / whole, replayed: one token of 2 x 8 heads of 128 over 1024,
+// bf16 11.7 / 15.5 (of two parts), fp32 14.3 / 32.3; 1500 rows of 12 heads, 9 sequences over 6 to 963
+// keys, those under 12 rows, 15.2 / 27.8; 2500 rows of 8 heads over 356 (below two parts) 18.0 / 13.7; eager: 64
+// of 8 heads of 64 over 700 (below 1024) 18.0 / 12.6.
 static Plan cross_plan(const AttnProblem &p, const int32_t *kv_lens, const int32_t *kv_index) {
   Plan pl;
   int64_t row_tiles, most;
@@ -1540,7 +1543,8 @@ static Plan cross_plan(const AttnProblem &p, const int32_t *kv_lens, const int32
     pl.kind = Plan::FEW;
     pl.TR = 32;
     pl.KT = 128;
-    least = 4;
+    least = p.dtype == MTE_BF16 ? 2 : 1;
+    pl.cut.from = p.dtype == MTE_BF16 ? 8 : p.c.d > 64 ? 3 : 4;
   } else if (p.dtype == MTE_BF16 && p.near_rows && p.near_tiles) {
     pl.kind = Plan::COPIES;
     pl.KT = 32;
@@ -1556,13 +1560,13 @@ static Plan cross_plan(const AttnProblem &p, const int32_t *kv_lens, const int32
   };
   double work = 0;
   each([&](int rows, int keys) { work += (double)rows * keys; });
-  pl.per = (int)std::min(std::max((double)least, std::ceil(work * p.c.hkv / kFill)), 0x1p30);
+  pl.cut.per = (int)std::min(std::max((double)least, std::ceil(work * p.c.hkv / kFill)), 0x1p29);
   // no more parts than a join takes
-  each([&](int, int keys) { pl.per = std::max(pl.per, ceil_div(keys, kMaxParts - 1)); });
+  each([&](int, int keys) { pl.cut.per = std::max(pl.cut.per, ceil_div(keys, kMaxParts - 1)); });
   int64_t at = 0;
   int in = 0;
   each([&](int rows, int keys) {
-    const int used = parts_of(keys, pl.per);
+    const int used = parts_of(keys, pl.cut);
     pl.split |= used > 1;
     if (used > 1) at += (int64_t)rows * used;        // (place_units: the others have no partial results)
     pl.tiles = std::max(pl.tiles, at);
@@ -1617,14 +1621,14 @@ template <int DP> int join_grid(int parts, int rows) { return parts > kFewParts 
 static int place_units(CrossArgs &a, const Plan &pl) {
   const auto rank = [&](const CondSeq &q) {
     const int nt = ceil_div(q.k_len, pl.KT);
-    return parts_of(nt, pl.per) > 1 ? INT_MAX : nt;
+    return parts_of(nt, pl.cut) > 1 ? INT_MAX : nt;
   };
   std::stable_sort(a.seq, a.seq + a.n_seq, [&](const CondSeq &x, const CondSeq &y) { return rank(x) > rank(y); });
   int units = 0;
   for (int i = 0; i < a.n_seq; ++i) {
     CondSeq &q = a.seq[i];
     q.tile0 = units;
-    units += ceil_div((int64_t)q.q_len * a.rep, pl.TR) * parts_of(ceil_div(q.k_len, pl.KT), pl.per);
+    units += ceil_div((int64_t)q.q_len * a.rep, pl.TR) * parts_of(ceil_div(q.k_len, pl.KT), pl.cut);
   }
   return units;
 }
@@ -1648,7 +1652,7 @@ static hipError_t run_cross(CrossArgs &a, const Plan &pl, hipStream_t s) {
   int n = 0, tiles = 0, most = 0;
   for (int i = 0; i < a.n_seq; ++i) {
     CondSeq q = a.seq[i];
-    const int used = parts_of(ceil_div(q.k_len, pl.KT), pl.per);
+    const int used = parts_of(ceil_div(q.k_len, pl.KT), pl.cut);
     if (used == 1) continue;
     q.k0 = q.tile0;
     q.k_len = used;
@@ -1679,7 +1683,7 @@ hipError_t launch_cross(const AttnProblem &p, const void *k, const void *v, cons
   a.k_head = k_head;
   a.v_row = v_row;
   a.v_head = v_head;
-  a.per = pl.per;
+  a.cut = pl.cut;
   a.n_split = 1;
   a.ws_rows = pl.ws_rows;
   a.ws_ml = pl.ml(a.hkv, dp);

@@ -31,11 +31,14 @@ struct AttnCommon {
   int big;                           // out is more than the caches hold
 };
 
+// How key ranges are cut: key tiles of a part, and of the shortest range that is cut.
+struct KeyCut { int per, from; };
+
 struct CrossArgs : AttnCommon {
   const void *k, *v;
   const uint8_t *mask;
   int64_t k_row, k_head, v_row, v_head;
-  int per;                           // key tiles of a part
+  KeyCut cut;
   CondSeq seq[kCondSeqs];
 };
 
