@@ -151,6 +151,9 @@ int mte_kv8_read(const mte_kv8 *cache, const int32_t *table, int32_t table_width
  * 0 .. kv_lens[i] - q_lens[i] + u only (its own token last: append, then attend).
  * A query that sees nothing gets zeros. Formula, q, out and workspace as in
  * mte_cross_attention (workspace: mte_kv8_attention_workspace); q_lens: HOST int32[n].
+ * Rounding: a token's weight, its probability times the scale of its block's values, meets the codes with 11
+ * significant bits (MTE_F32: 22), and none below 2^-31 of the largest weight of its row; whatever
+ * scales the blocks of lesser weight have.
  * The work is split for sequences of up to 32 table_width tokens: a table that
  * is much wider than its sequences costs time.
  * Errors: MTE_E_INVALID, MTE_E_UNSUPPORTED (head_dim), MTE_E_CAPACITY

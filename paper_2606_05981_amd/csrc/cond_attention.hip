@@ -88,6 +88,9 @@ __device__ __forceinline__ Span split_span(int nt, int n_split, int split, int l
   return s;
 }
 
+// A reference of scores or sums as a finite number (nothing seen yet: 0, so that exp2(-inf - 0) = 0).
+__device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
+
 // Running softmax of one row per lane (both halves of the wave hold the same row).
 // m is a reference, not quite the maximum: it moves only when some row of the wave has a
 // score more than kSlack above it, so that O and l are rescaled in the first step and hardly
@@ -118,12 +121,12 @@ template <int ND> struct Rows {
     return ref();
   }
   __device__ __forceinline__ bool over(float mb) const { return __any(mb > m + kSlack); }   // wave-uniform
-  __device__ __forceinline__ float ref() const { return m == -INFINITY ? 0.f : m; }   // nothing seen yet: exp2(-inf - 0) = 0
+  __device__ __forceinline__ float ref() const { return finite_ref(m); }
   __device__ __forceinline__ void lift(float mb) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
     const float m_new = fmaxf(m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
     if (__any(m != -INFINITY)) {                        // else O and l are still zero
-      const float alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.f : m_new));
+      const float alpha = __builtin_amdgcn_exp2f(m - finite_ref(m_new));
       l *= alpha;
       scale(alpha);
     }
@@ -179,7 +182,7 @@ __device__ __forceinline__ void join_waves(Rows<ND> &st, float *red, int kw, int
   float mx = st.m;
 #pragma unroll
   for (int v = 0; v < KW - 1; ++v) mx = fmaxf(mx, red[v * NV * 64 + lane]);
-  const float mr = mx == -INFINITY ? 0.f : mx;
+  const float mr = finite_ref(mx);
   const float f0 = __builtin_amdgcn_exp2f(st.m - mr);
   st.l *= f0;
   st.scale(f0);
@@ -515,33 +518,6 @@ __device__ __forceinline__ uint32_t tile_words(const uint8_t *mask, int klen, in
   return words;
 }
 
-// One row tile over n steps of 32 keys, two at a time.
-//   scores(i, s): raw scores;  mask(i, s);  factor(i): what turns them into log2 units;
-//   probs(i, s, ref): their operand;  values(i, p): O += V^T P^T.
-template <int ND, typename P, typename SC, typename MA, typename FA, typename PR, typename VA>
-__device__ __forceinline__ void attend_steps(Rows<ND> &st, int n, SC scores, MA mask, FA factor, PR probs, VA values) {
-  int i = 0;
-  for (; i + 2 <= n; i += 2) {
-    f32x16 s0, s1;
-    scores(i, s0);
-    scores(i + 1, s1);
-    mask(i, s0);
-    mask(i + 1, s1);
-    const float ref = st.raise(fmaxf(max16(s0, -INFINITY) * factor(i), max16(s1, -INFINITY) * factor(i + 1)));
-    const P p0 = probs(i, s0, ref);                 // (may rescale O: before the block's values, after those before)
-    values(i, p0);
-    const P p1 = probs(i + 1, s1, ref);
-    values(i + 1, p1);
-  }
-  if (i < n) {
-    f32x16 s0;
-    scores(i, s0);
-    mask(i, s0);
-    const float ref = st.raise(max16(s0, -INFINITY) * factor(i));
-    values(i, probs(i, s0, ref));
-  }
-}
-
 constexpr int kBox = 4096;          // a wave's LDS for it
 // A store that leaves nothing in L2 (written out: as a branch of two stores of one value the
 // compiler makes one plain store of it).
@@ -770,14 +746,127 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
 // ---- keys and values as e4m3 codes --------------------------------------------------------------
 //
 // Codes widen exactly: keys to bf16 (the queries' type: their range is bf16's), values to
-// fp16, and the probabilities, at most 2^15 here (an offset in the exponent that
-// keeps small ones out of fp16's subnormals), to fp16. fp32 queries are three bf16
-// terms (24 bits) and fp32 probabilities two fp16 terms (22 bits), so that the products
-// keep fp32's precision on the 16-bit matrix cores.
-// Block scales: the key scale multiplies the scores; the value scale, relative to the
-// largest one so far (`vref`, a power of two, wave-uniform), multiplies the
-// probabilities, and O is in units of vref.
+// fp16. fp32 queries are three bf16 terms (24 bits).
+// Block scales: the key scale multiplies the scores, the value scale the probabilities. Their products,
+// weights p_j 2^lv (lv: log2 of the block's value scale), are the operand of the value product: fp16, once
+// rounded (2^-11), or for fp32 calls two fp16 terms (2^-22), so that the 16-bit matrix cores serve both. fp16's
+// range is short, so weights are relative to a running reference of their own for each row, u:
+// the largest is held in [2^7, 2^15], and fp16's smallest step is 2^-31 of it or less, whatever scales other
+// blocks have. (In units of the largest scale so far, a row whose weight lies in blocks of scales
+// 2^32 smaller, under keys that it hardly weighs, would come out as zero.)
 constexpr float kPOff = 15.f - kSlack;
+
+// log2 of a block's value scale: the exponent, exact, and the rest (0 for powers of two).
+__device__ __forceinline__ float scale_log(float vs) {
+  const uint32_t b = __float_as_uint(vs);
+  return (float)((int)(b >> 23) - 127) + __builtin_amdgcn_logf(__uint_as_float((b & 0x7FFFFF) | 0x3F800000));
+}
+
+// State of 32 rows over cached codes. With m the reference of the scores (Rows), O is in units of 2^(m + u); both
+// lag like m, and are whole numbers, so that rescaling is exact. l and the weights carry 2^kPOff more.
+template <int ND> struct CodeRows : Rows<ND> {
+  using Rows<ND>::o;
+  using Rows<ND>::m;
+  using Rows<ND>::l;
+  float u;
+  __device__ __forceinline__ void init() {
+    Rows<ND>::init();
+    u = -INFINITY;
+  }
+  // Takes the maxima mb (log2 units) of this lane's new scores in N blocks of value scales 2^lv.
+  template <int N> __device__ __forceinline__ void raise(const float (&mb)[N], const float (&lv)[N]) {
+    bool over = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) over |= mb[i] - m > fminf(kSlack, u + kSlack - lv[i]);   // (NaN where nothing is seen yet)
+    if (__any(over)) lift<N>(mb, lv);
+  }
+  template <int N> __device__ __forceinline__ void lift(const float (&mb)[N], const float (&lv)[N]) {
+    float top[N], m_new = m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb[i]), __float_as_uint(mb[i]), false, false);
+      top[i] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+      m_new = fmaxf(m_new, floorf(top[i]));
+    }
+    const float mr = finite_ref(m_new), kept = m - mr + u;
+    float u_new = kept;
+#pragma unroll
+    for (int i = 0; i < N; ++i) u_new = fmaxf(u_new, floorf(top[i] - mr + lv[i]));
+    if (__any(m != -INFINITY)) {                        // else O and l are still zero
+      l *= __builtin_amdgcn_exp2f(m - mr);
+      Rows<ND>::scale(__builtin_amdgcn_exp2f(kept - finite_ref(u_new)));
+    }
+    m = m_new;
+    u = u_new;
+  }
+  // For the block of value scale 2^lv: a weight is 2^(score + c), w what its sum counts in l. Weights too far
+  // below the row's largest (2^-60, nothing in fp16) are kept from fp32's own limit, for l.
+  struct Ref { float c, w; };
+  __device__ __forceinline__ Ref ref(float lv) const {
+    const float x = fminf(finite_ref(u) - lv, 60.f);
+    return Ref{kPOff - finite_ref(m) - x, __builtin_amdgcn_exp2f(x)};
+  }
+  // What O is still to be multiplied by, 2^u: here in part where that is far from 1.
+  __device__ __forceinline__ float unit() {
+    const float e = finite_ref(u);
+    float half = 0.f;
+    if (__any(fabsf(e) > 64.f)) {
+      half = truncf(0.5f * e);
+      Rows<ND>::scale(__builtin_amdgcn_exp2f(half));
+    }
+    return __builtin_amdgcn_exp2f(e - half);
+  }
+};
+
+// Brings the KW waves' states of the same rows to one pair of references. red: 2 KW x 64 floats.
+template <int ND, int KW>
+__device__ __forceinline__ void match_waves(CodeRows<ND> &st, float *red, int wave, int lane) {
+  red[wave * 64 + lane] = st.m;
+  red[(KW + wave) * 64 + lane] = st.u;
+  __syncthreads();
+  float m = -INFINITY, u = -INFINITY;
+#pragma unroll
+  for (int v = 0; v < KW; ++v) m = fmaxf(m, red[v * 64 + lane]);
+  const float mr = finite_ref(m);
+#pragma unroll
+  for (int v = 0; v < KW; ++v) u = fmaxf(u, red[v * 64 + lane] - mr + red[(KW + v) * 64 + lane]);
+  st.l *= __builtin_amdgcn_exp2f(st.m - mr);
+  st.scale(__builtin_amdgcn_exp2f(st.m - mr + st.u - finite_ref(u)));
+  st.m = m;
+  st.u = u;
+  __syncthreads();
+}
+
+// One row tile over n blocks, two at a time.
+//   scores(i, s): raw scores;  mask(i, s);  factor(i): what turns them into log2 units;  lv(i): log2 of the value
+//   scale;  probs(i, s): the weights' operand;  values(i, p): O += V^T P^T.
+template <int ND, typename P, typename SC, typename MA, typename FA, typename LV, typename PR, typename VA>
+__device__ __forceinline__ void attend_blocks(CodeRows<ND> &st, int n, SC scores, MA mask, FA factor, LV lv, PR probs,
+                                              VA values) {
+  int i = 0;
+  for (; i + 2 <= n; i += 2) {
+    f32x16 s0, s1;
+    scores(i, s0);
+    scores(i + 1, s1);
+    mask(i, s0);
+    mask(i + 1, s1);
+    const float mb[2] = {max16(s0, -INFINITY) * factor(i), max16(s1, -INFINITY) * factor(i + 1)};
+    const float at[2] = {lv(i), lv(i + 1)};
+    st.template raise<2>(mb, at);
+    const P p0 = probs(i, s0);
+    values(i, p0);
+    const P p1 = probs(i + 1, s1);
+    values(i + 1, p1);
+  }
+  if (i < n) {
+    f32x16 s0;
+    scores(i, s0);
+    mask(i, s0);
+    const float mb[1] = {max16(s0, -INFINITY) * factor(i)}, at[1] = {lv(i)};
+    st.template raise<1>(mb, at);
+    values(i, probs(i, s0));
+  }
+}
 
 template <typename T, int NK> struct QCodes {      // query operands: NQ bf16 terms
   static constexpr int NQ = sizeof(T) == 4 ? 3 : 1;
@@ -864,35 +953,20 @@ __device__ __forceinline__ void kv8_scores(f32x16 &s, const QCodes<T, NK> &q, co
   }
 }
 
-// Probabilities of one block, p = 2^(ksc s - ref), as fp16 (fp32 calls: two terms), times `ratio`: the
-// block's value scale over vref, a power of two at most 1.
+// Weights of one block, 2^(ksc s + c), as fp16 (fp32 calls: two terms); their sum, times w, joins l.
 template <typename T> struct CodeProbs { f16x8 f[2], lo[sizeof(T) == 4 ? 2 : 1]; };
 template <typename T>
-__device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, float ref, float ratio, float &l) {
-  float p[16];
+__device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, float c, float w, float &l) {
+  CodeProbs<T> o;
+  float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], ksc, -ref));
-    l += p[i];
+    const float p = __builtin_amdgcn_exp2f(fmaf(s[i], ksc, c));
+    sum += p;
+    o.f[i >> 3][i & 7] = (f16)p;
+    if constexpr (sizeof(T) == 4) o.lo[i >> 3][i & 7] = (f16)(p - (float)o.f[i >> 3][i & 7]);
   }
-  CodeProbs<T> o;
-#pragma unroll
-  for (int f = 0; f < 2; ++f) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (sizeof(T) == 4) {
-        const float x = p[8 * f + e] * ratio;
-        o.f[f][e] = (f16)x;
-        o.lo[f][e] = (f16)(x - (float)o.f[f][e]);
-      } else {
-        o.f[f][e] = (f16)p[8 * f + e];
-      }
-    }
-    if constexpr (sizeof(T) == 2) {
-      const f16 rt = (f16)ratio;
-      o.f[f] *= f16x8{rt, rt, rt, rt, rt, rt, rt, rt};
-    }
-  }
+  l = fmaf(sum, w, l);
   return o;
 }
 // O += V^T P^T; vf(n, f): value operand of d block n, keys 16 f ..
@@ -907,19 +981,6 @@ __device__ __forceinline__ void code_values(f32x16 (&o)[ND], const CodeProbs<T> 
       if constexpr (sizeof(T) == 4) mfma32(o[n], v, p.lo[f]);
     }
 }
-
-// The largest value scale so far: O is in its units.
-struct VRef {
-  float top = 0.f, inv = 0.f;
-  template <int ND> __device__ __forceinline__ float ratio(Rows<ND> &st, float vsc) {
-    if (vsc > top) {                                // wave-uniform
-      st.scale(top / vsc);                          // 0 at the first block, where O is 0
-      top = vsc;
-      inv = 1.f / vsc;
-    }
-    return vsc * inv;
-  }
-};
 
 // What the rows of a tile see of a sequence: its length; the keys of the tile's first and last row,
 // and of this lane's row.
@@ -1048,9 +1109,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
     for (int i = 0; i < NL; ++i) x.v[i] = vp[64 * i];
   };
   QCodes<T, NK> q;
-  Rows<ND> st;
+  CodeRows<ND> st;
   st.init();
-  VRef vr;
   Block cur, nxt;
   const int b0 = span.lo + wave;
   int id = id_at(b0 + 4);
@@ -1078,26 +1138,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
         }
       }
       const float ksc = key_factor(cur.ref.ks, a.sc);
-      const float ref = st.raise(max16(s, -INFINITY) * ksc) - kPOff;
-      const float ratio = vr.ratio(st, cur.ref.vs);
-      code_values<T, ND>(st.o, code_probs<T>(s, ksc, ref, ratio, st.l),
+      const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur.ref.vs)};
+      st.template raise<1>(mb, lv);
+      const auto rf = st.ref(lv[0]);
+      code_values<T, ND>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
                          [&](int n, int f) { return widen_f16(cur.v[n][2 * f], cur.v[n][2 * f + 1]); });
     }
     cur = nxt;
   }
-  // the waves' O in one unit before they are joined
   float *red = (float *)lds;
-  if (lane == 0) red[wave] = vr.top;
-  __syncthreads();
-  const float top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  if (top > 0.f) st.scale(vr.top / top);
-  __syncthreads();
+  match_waves<ND, 4>(st, red, wave, lane);
   join_waves<ND, 4>(st, red, wave, lane);
   if (wave > 0) return;
+  const float unit = st.unit();
   if (span.used == 1)
-    store_rows<T, ND>(a, st, top, live, sq.q0 + qi, head, lane);
+    store_rows<T, ND>(a, st, unit, live, sq.q0 + qi, head, lane);
   else
-    store_part<ND>(a, st, top, live, part, g, 0, lrow, lane);
+    store_part<ND>(a, st, unit, live, part, g, 0, lrow, lane);
 }
 
 // Many rows: four waves of 32 rows; two blocks of codes a step are widened once per
@@ -1157,9 +1214,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
   }
   QCodes<T, NK> q;
   q.load((const T *)a.q + (int64_t)(sq.q0 + qi) * a.q_row + (int64_t)head * a.q_head, live, h);
-  Rows<ND> st;
+  CodeRows<ND> st;
   st.init();
-  VRef vr;
   for (int b = span.lo; b < span.hi; b += 2) {
     __syncthreads();
     lstore();
@@ -1180,9 +1236,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
           kv8_scores<T, NK>(s, q, fr);
           if ((b + u) * 32 + 32 > seen.tile_lo) mask_below(s, seen.row_hi - (b + u) * 32, lane);
           const float ksc = key_factor(cur[u].ks, a.sc);
-          const float ref = st.raise(max16(s, -INFINITY) * ksc) - kPOff;
-          const float ratio = vr.ratio(st, cur[u].vs);
-          code_values<T, ND>(st.o, code_probs<T>(s, ksc, ref, ratio, st.l),
+          const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur[u].vs)};
+          st.template raise<1>(mb, lv);
+          const auto rf = st.ref(lv[0]);
+          code_values<T, ND>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
                              [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(NK + 2 * n + f) * 64]); });
         }
       }
@@ -1191,16 +1248,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
     for (int u = 0; u < 2; ++u) cur[u] = nxt[u];
   }
   if (r0 >= rows) return;
+  const float unit = st.unit();
   if (span.used == 1)
-    store_rows<T, ND>(a, st, vr.top, live, sq.q0 + qi, head, lane);
+    store_rows<T, ND>(a, st, unit, live, sq.q0 + qi, head, lane);
   else
-    store_part<ND>(a, st, vr.top, live, tile, g, split, wave * 32 + lrow, lane);
+    store_part<ND>(a, st, unit, live, tile, g, split, wave * 32 + lrow, lane);
 }
 
 // Many rows over a cache that fits LDS whole once widened. Lane j holds block j's scales and how many of
-// its tokens count (none: no such block). O is in units of the largest value scale so far, as in the
-// other kernels: one for all blocks, of which a causal row sees the first, would push that row's
-// probabilities below fp16. A wave takes several row tiles over codes widened once.
+// its tokens count (none: no such block). A wave takes several row tiles over codes widened once.
 // Bound by the matrix instructions and the softmax between them, and by the one pass of staging that a
 // workgroup waits for (16 x 1024 of 2 x 8 heads of 128 over 320: 61.5 us, 700 TFLOP/s, 2.4 TB/s).
 template <typename T, int D, int NW, bool BOX>
@@ -1237,14 +1293,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
     else load_own(r0, q);
   }
 
-  float ks = 1.f, vs = 0.f;
+  float ks = 1.f, lv = 0.f;
   int count = 0;
   if (lane < nk) {
     const int id = tab[lane];
     if (id >= 0 && id < a.c.n_blocks) {
       const int64_t at = (int64_t)id * a.c.hkv + g;
       ks = key_factor(a.c.scales[at * 2], a.sc);
-      vs = a.c.scales[at * 2 + 1];
+      lv = scale_log(a.c.scales[at * 2 + 1]);
       count = min(all.kv - lane * 32, 32);
     }
   }
@@ -1288,29 +1344,30 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
       load_own(r0 + NW * 32, qn);
     }
     const Seen seen = seen_of(a, sq, r0 / a.rep, (min(r0 + 32, rows) - 1) / a.rep, r / a.rep);
-    Rows<ND> st;
+    CodeRows<ND> st;
     st.init();
-    VRef vr;
     auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
-    attend_steps<ND, CodeProbs<T>>(
+    attend_blocks<ND, CodeProbs<T>>(
         st, (seen.tile_hi + 31) >> 5,
         [&](int i, f32x16 &s) { kv8_scores<T, NK>(s, q.f, codes + i * NF * 64 + lane); },
         [&](int i, f32x16 &s) {
           const int n = __builtin_amdgcn_readlane(count, i), at = i * 32;
           if (n < 32 || at + 32 > seen.tile_lo) mask_below(s, min(seen.row_hi - at, n), lane);
         },
-        [&](int i) { return lane_of(ks, i); },
-        [&](int i, const f32x16 &s, float ref) {
-          return code_probs<T>(s, lane_of(ks, i), ref - kPOff, vr.ratio(st, lane_of(vs, i)), st.l);
+        [&](int i) { return lane_of(ks, i); }, [&](int i) { return lane_of(lv, i); },
+        [&](int i, const f32x16 &s) {
+          const auto rf = st.ref(lane_of(lv, i));
+          return code_probs<T>(s, lane_of(ks, i), rf.c, rf.w, st.l);
         },
         [&](int i, const CodeProbs<T> &p) {
           const u32x4 *fr = codes + (i * NF + NK) * 64 + lane;
           code_values<T, ND>(st.o, p, [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(2 * n + f) * 64]); });
         });
+    const float unit = st.unit();
     if constexpr (BOX) {
-      store_tile<T, ND>(a, st, vr.top, TileRows(a, sq, r0, rows), g, box, lane);
+      store_tile<T, ND>(a, st, unit, TileRows(a, sq, r0, rows), g, box, lane);
     } else {
-      store_rows<T, ND>(a, st, vr.top, q.live, q.tok, q.head, lane);
+      store_rows<T, ND>(a, st, unit, q.live, q.tok, q.head, lane);
       if (sizeof(T) == 2) q = qn;
       else if (more) load_own(r0 + NW * 32, q);
     }

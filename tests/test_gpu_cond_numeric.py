@@ -1,0 +1,77 @@
+"""The operators over cached codes and conditioning rows (include/mte_cond.h) where magnitudes part: value
+scales of one block far above another's, NaN that only some rows see, scores past fp32's whole
+numbers, factors at the ends of the range; against the float64 oracle."""
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import cond_oracle as O
+from tests.test_gpu_cond import U, U16, _f64, _fill, _held, _i32, _randn
+
+pytestmark = pytest.mark.gpu
+
+
+def _say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "no GPU"
+    return torch
+
+
+@pytest.fixture(scope="module")
+def C():
+    from paper_2606_05981_amd import conditioning
+    return conditioning
+
+
+# q_len, kv_len, table width, Hq, Hkv: one token, few rows of a long cache, chunks of them, rows over tables that
+# fit LDS twice and once, and over one that does not (heads of 64)
+CACHED = [(1, 200, None, 4, 2), (3, 2500, None, 4, 2), (40, 300, None, 4, 2), (130, 140, None, 32, 4),
+          (300, 310, None, 32, 4), (300, 310, 40, 32, 4)]
+
+
+def _sees(q_len, kv_len, causal):
+    return np.arange(kv_len)[None] <= kv_len - q_len + np.arange(q_len)[:, None] if causal else np.ones((q_len, kv_len), bool)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("spread,away", [(20, 16), (25, 64), (40, 64), (40, 28), (60, 44), (100, 64), (-60, 0)])
+@pytest.mark.parametrize("ql,kl,width,hq,h", CACHED)
+def test_kv8_values_of_unlike_magnitude(torch, C, ql, kl, width, hq, h, spread, away, dtype):
+    """The first or the last block's values are 2^spread times the others', its keys `away` (natural log)
+    below: precision goes by what weight and scale come to together in the row, not by the largest scale.
+
+    Bound: as in tests/test_gpu_cond.py, but what fp16 cannot hold of a term, at most half its smallest step, 2^-25 of
+    operands whose largest in the row is 2^7 or more, is 2^-32 of the row's largest p_j scale_j, times codes of at
+    most 448, for each of n keys."""
+    d = 64
+    for first in (True, False):
+        _say(f"cached values 2^{spread} apart, away {away}, {ql} x {kl}, width {width}, {dtype}, first {first}")
+        big = slice(0, 32) if first else slice((kl - 1) // 32 * 32, kl)
+        cache, table, kv, k, v = _fill(torch, C, [kl], h, d, width=width, spread=False)
+        k[..., 0] = 0
+        k[big, :, 0] = -away
+        v[big] *= 2.0 ** spread
+        C.kv8_append(cache, table, kv, k, v, [kl])
+        q = _randn(torch, 110, ql, hq, d, dtype=dtype)
+        q[..., 0] = 8
+        got = _f64(C.kv8_attention(q, cache, table, kv, [ql]))
+        (kk, vv), = _held(torch, cache, table, [kl])
+        ref, mag, reach = O.attend(_f64(q), kk, vv, _sees(ql, kl, False), 1 / 8)
+        vs = cache.scales[table[0, :(kl + 31) // 32].long(), :, 1].double().cpu().numpy().repeat(32, 0)[:kl]
+        s = np.einsum("ihd,jhd->hij", _f64(q), kk.repeat(hq // h, 1)) / 8
+        p = np.exp(s - s.max(-1, keepdims=True))
+        p /= p.sum(-1, keepdims=True)
+        top = (p * vs.repeat(hq // h, 1).T[:, None]).max(-1).T[..., None]           # [ql, hq, 1]
+        D = (d + 4) * U * reach[..., None] + 2 * U
+        t = 4 * D * mag + 2 * (kl + 16) * U * mag + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * mag
+        t = t + kl * 2.0 ** -32 * 448 * top
+        t = t + (U16 if dtype == "bf16" else U) * (np.abs(ref) + t) + 1e-30
+        worst = float((np.abs(got - ref) / t).max())
+        _say(f"  worst error / bound {worst:.3f}")
+        assert worst <= 1.0
