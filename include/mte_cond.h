@@ -153,7 +153,8 @@ int mte_kv8_read(const mte_kv8 *cache, const int32_t *table, int32_t table_width
  * mte_cross_attention (workspace: mte_kv8_attention_workspace); q_lens: HOST int32[n].
  * Rounding: a token's weight, its probability times the scale of its block's values, meets the codes with 11
  * significant bits (MTE_F32: 22), and none below 2^-31 of the largest weight of its row; whatever
- * scales the blocks of lesser weight have.
+ * scales the blocks of lesser weight have. What tokens that a query does not see hold does not reach it; a
+ * cached NaN reaches the queries that see its token: a value in its channel, a key everywhere.
  * The work is split for sequences of up to 32 table_width tokens: a table that
  * is much wider than its sequences costs time.
  * Errors: MTE_E_INVALID, MTE_E_UNSUPPORTED (head_dim), MTE_E_CAPACITY

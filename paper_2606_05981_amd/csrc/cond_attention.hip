@@ -970,21 +970,37 @@ __device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, f
   return o;
 }
 // O += V^T P^T; vf(n, f): value operand of d block n, keys 16 f ..
-template <typename T, int ND, typename VF>
+// 0 x NaN is NaN: a NaN value reaches the rows that do not see its token, too. Where a tile's rows see different
+// tokens and its O holds NaN (some_nan), the tile is done again with FINITE, which takes NaN as -448, and
+// spread_nan brings NaN to the rows that see them.
+template <typename T, int ND, bool FINITE, typename VF>
 __device__ __forceinline__ void code_values(f32x16 (&o)[ND], const CodeProbs<T> &p, VF vf) {
 #pragma unroll
   for (int f = 0; f < 2; ++f)
 #pragma unroll
     for (int n = 0; n < ND; ++n) {
-      const f16x8 v = vf(n, f);
+      f16x8 v = vf(n, f);
+      if constexpr (FINITE) v = __builtin_elementwise_max(v, f16x8{} - (f16)448.f);   // (of a number and NaN, the number)
       mfma32(o[n], v, p.f[f]);
       if constexpr (sizeof(T) == 4) mfma32(o[n], v, p.lo[f]);
     }
 }
+template <int ND> __device__ __forceinline__ bool some_nan(const f32x16 (&o)[ND]) {   // of the wave (or infinities of both signs)
+  float sum = 0.f;
+#pragma unroll
+  for (int n = 0; n < ND; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum += o[n][r];
+  return __any(sum != sum);
+}
+template <bool X> struct Finite { static constexpr bool value = X; };
 
 // What the rows of a tile see of a sequence: its length; the keys of the tile's first and last row,
 // and of this lane's row.
-struct Seen { int kv, tile_lo, tile_hi, row_hi; };
+struct Seen {
+  int kv, tile_lo, tile_hi, row_hi;
+  __device__ __forceinline__ bool uneven(int blocks) const { return tile_lo < min(blocks * 32, kv); }   // some of the first blocks
+};
 __device__ __forceinline__ Seen seen_of(const Kv8AttnArgs &a, const CondSeq &sq, int first_tok, int last_tok, int tok) {
   Seen v;
   v.kv = min(max(uniform_at(a.c.kv_lens, sq.k0), 0), a.c.width * 32);
@@ -1007,6 +1023,36 @@ __device__ __forceinline__ BlockRef block_ref(const Kv8View &c, int id, int g) {
   b.ks = uniform_at(c.scales, b.at * 2);
   b.vs = ok ? uniform_at(c.scales, b.at * 2 + 1) : -1.f;
   return b;
+}
+
+// Rows that see a NaN value of block b get NaN in its channel: a product of where they are (1, else 0) and which
+// of the block's tokens a row sees, those below `left`.
+template <int D>
+__device__ __forceinline__ void spread_nan(f32x16 (&o)[D / 32], const Kv8View &c, const int32_t *tab, int b, int g, int left,
+                                           int lane) {
+  const BlockRef ref = block_ref(c, uniform_at(tab, b), g);
+  if (!(ref.vs > 0.f)) return;
+  const u32x4 *vp = (const u32x4 *)(c.v_codes + ref.at * (32 * D)) + (lane & 31) * 2 + (lane >> 5);
+  f16x8 sees[2];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = 8 * (i >> 2) + (i & 3) < left - 4 * (lane >> 5) ? (f16)1.f : (f16)0.f;
+#pragma unroll
+  for (int n = 0; n < D / 32; ++n) {
+    const u32x4 x = vp[64 * n];
+    f32x16 hits;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) hits[i] = 0.f;
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      f16x8 at;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) at[e] = ((x[2 * f + (e >> 2)] >> (8 * (e & 3))) & 0x7F) == 0x7F ? (f16)1.f : (f16)0.f;
+      mfma32(hits, at, sees[f]);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[n][i] = hits[i] > 0.f ? NAN : o[n][i];
+    __builtin_amdgcn_sched_barrier(0);                  // one d block's registers at a time
+  }
 }
 
 // Least blocks of a split: below that a partial result costs more than its keys.
@@ -1110,41 +1156,49 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
   };
   QCodes<T, NK> q;
   CodeRows<ND> st;
-  st.init();
-  Block cur, nxt;
   const int b0 = span.lo + wave;
-  int id = id_at(b0 + 4);
-  if (b0 < span.hi) load(id_at(b0), cur);
-  q.load((const T *)a.q + (int64_t)(sq.q0 + qi) * a.q_row + (int64_t)head * a.q_head, live, h);
-  for (int b = b0; b < span.hi; b += 4) {
-    if (b + 4 < span.hi) load(id, nxt);
-    id = id_at(b + 8);
-    if (cur.ref.vs > 0.f) {
-      f32x16 s;
+  auto pass = [&](auto finite) {
+    typedef decltype(finite) F;
+    st.init();
+    Block cur, nxt;
+    int id = id_at(b0 + 4);
+    if (b0 < span.hi) load(id_at(b0), cur);
+    if constexpr (!F::value) q.load((const T *)a.q + (int64_t)(sq.q0 + qi) * a.q_row + (int64_t)head * a.q_head, live, h);
+    for (int b = b0; b < span.hi; b += 4) {
+      if (b + 4 < span.hi) load(id, nxt);
+      id = id_at(b + 8);
+      if (cur.ref.vs > 0.f) {
+        f32x16 s;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        const bf16x8 kf = widen_bf16(cur.k[kk >> 1][2 * (kk & 1)], cur.k[kk >> 1][2 * (kk & 1) + 1]);
+        for (int kk = 0; kk < NK; ++kk) {
+          const bf16x8 kf = widen_bf16(cur.k[kk >> 1][2 * (kk & 1)], cur.k[kk >> 1][2 * (kk & 1) + 1]);
 #pragma unroll
-        for (int t = q.NQ - 1; t >= 0; --t) mfma32(s, kf, q.f[t][kk]);   // small terms first
-      }
-      const int left = seen.kv - b * 32;
-      if (left < 32 || b * 32 + 32 > seen.tile_lo) {  // wave-uniform
-        mask_below(s, seen.row_hi - b * 32, lane);
-        if (left < 32) {
-#pragma unroll
-          for (int i = 0; i < NL; ++i) cur.v[i] = keep_tokens(cur.v[i], left, h);
+          for (int t = q.NQ - 1; t >= 0; --t) mfma32(s, kf, q.f[t][kk]);   // small terms first
         }
+        const int left = seen.kv - b * 32;
+        if (left < 32 || b * 32 + 32 > seen.tile_lo) {  // wave-uniform
+          mask_below(s, seen.row_hi - b * 32, lane);
+          if (left < 32) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) cur.v[i] = keep_tokens(cur.v[i], left, h);
+          }
+        }
+        const float ksc = key_factor(cur.ref.ks, a.sc);
+        const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur.ref.vs)};
+        st.template raise<1>(mb, lv);
+        const auto rf = st.ref(lv[0]);
+        code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
+                                     [&](int n, int f) { return widen_f16(cur.v[n][2 * f], cur.v[n][2 * f + 1]); });
       }
-      const float ksc = key_factor(cur.ref.ks, a.sc);
-      const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur.ref.vs)};
-      st.template raise<1>(mb, lv);
-      const auto rf = st.ref(lv[0]);
-      code_values<T, ND>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
-                         [&](int n, int f) { return widen_f16(cur.v[n][2 * f], cur.v[n][2 * f + 1]); });
+      cur = nxt;
     }
-    cur = nxt;
+  };
+  pass(Finite<false>{});
+  if (seen.uneven(span.hi) && some_nan<ND>(st.o)) {
+    pass(Finite<true>{});
+    for (int b = b0; b < span.hi; b += 4) spread_nan<D>(st.o, a.c, tab, b, g, seen.row_hi - b * 32, lane);
   }
   float *red = (float *)lds;
   match_waves<ND, 4>(st, red, wave, lane);
@@ -1168,6 +1222,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
   constexpr int PIECES = 4 * NL;                    // 1 KB loads of a step: 2 blocks x (k, v) x NL
   constexpr int PPW = PIECES / 4;
   extern __shared__ u32x4 lds[];                    // [block][NK key + 2 ND value fragments][64 lanes]
+  __shared__ int again[4];                          // waves whose O holds NaN
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
   const Unit un = unit_of(a.hkv);
@@ -1205,47 +1260,60 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
       widen_to<NL>(lds + blk * 4 * NL * 64, sub, x[i], lane);
     }
   };
-  BlockRef cur[2], nxt[2];
-  int id[2] = {id_at(span.lo + 2), id_at(span.lo + 3)};
-  if (span.lo < span.hi) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) cur[u] = block_ref(a.c, id_at(span.lo + u), g);
-    gload(span.lo, cur);
-  }
   QCodes<T, NK> q;
-  q.load((const T *)a.q + (int64_t)(sq.q0 + qi) * a.q_row + (int64_t)head * a.q_head, live, h);
   CodeRows<ND> st;
-  st.init();
-  for (int b = span.lo; b < span.hi; b += 2) {
-    __syncthreads();
-    lstore();
-    __syncthreads();
-    if (b + 2 < span.hi) {
+  auto pass = [&](auto finite) {
+    typedef decltype(finite) F;
+    BlockRef cur[2], nxt[2];
+    int id[2] = {id_at(span.lo + 2), id_at(span.lo + 3)};
+    if (span.lo < span.hi) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) nxt[u] = block_ref(a.c, id[u], g);
-      gload(b + 2, nxt);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) id[u] = id_at(b + 4 + u);
+      for (int u = 0; u < 2; ++u) cur[u] = block_ref(a.c, id_at(span.lo + u), g);
+      gload(span.lo, cur);
     }
-    if (r0 < rows) {                                // wave-uniform: others still load and meet the barriers
+    if constexpr (!F::value) q.load((const T *)a.q + (int64_t)(sq.q0 + qi) * a.q_row + (int64_t)head * a.q_head, live, h);
+    st.init();
+    for (int b = span.lo; b < span.hi; b += 2) {
+      __syncthreads();
+      lstore();
+      __syncthreads();
+      if (b + 2 < span.hi) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (cur[u].vs > 0.f) {
-          const u32x4 *fr = lds + u * 4 * NL * 64 + lane;
-          f32x16 s;
-          kv8_scores<T, NK>(s, q, fr);
-          if ((b + u) * 32 + 32 > seen.tile_lo) mask_below(s, seen.row_hi - (b + u) * 32, lane);
-          const float ksc = key_factor(cur[u].ks, a.sc);
-          const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur[u].vs)};
-          st.template raise<1>(mb, lv);
-          const auto rf = st.ref(lv[0]);
-          code_values<T, ND>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
-                             [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(NK + 2 * n + f) * 64]); });
+        for (int u = 0; u < 2; ++u) nxt[u] = block_ref(a.c, id[u], g);
+        gload(b + 2, nxt);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) id[u] = id_at(b + 4 + u);
+      }
+      if (r0 < rows) {                              // wave-uniform: others still load and meet the barriers
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (cur[u].vs > 0.f) {
+            const u32x4 *fr = lds + u * 4 * NL * 64 + lane;
+            f32x16 s;
+            kv8_scores<T, NK>(s, q, fr);
+            if ((b + u) * 32 + 32 > seen.tile_lo) mask_below(s, seen.row_hi - (b + u) * 32, lane);
+            const float ksc = key_factor(cur[u].ks, a.sc);
+            const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur[u].vs)};
+            st.template raise<1>(mb, lv);
+            const auto rf = st.ref(lv[0]);
+            code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
+                                         [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(NK + 2 * n + f) * 64]); });
+          }
         }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) cur[u] = nxt[u];
+      for (int u = 0; u < 2; ++u) cur[u] = nxt[u];
+    }
+  };
+  pass(Finite<false>{});
+  if (a.causal) {                                   // uniform
+    const bool mine = r0 < rows && seen.uneven(span.hi) && some_nan<ND>(st.o);
+    if (lane == 0) again[wave] = mine;
+    __syncthreads();
+    if (again[0] | again[1] | again[2] | again[3]) {
+      pass(Finite<true>{});
+      for (int b = span.lo; r0 < rows && b < span.hi; ++b) spread_nan<D>(st.o, a.c, tab, b, g, seen.row_hi - b * 32, lane);
+    }
   }
   if (r0 >= rows) return;
   const float unit = st.unit();
@@ -1345,24 +1413,33 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
     }
     const Seen seen = seen_of(a, sq, r0 / a.rep, (min(r0 + 32, rows) - 1) / a.rep, r / a.rep);
     CodeRows<ND> st;
-    st.init();
     auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
-    attend_blocks<ND, CodeProbs<T>>(
-        st, (seen.tile_hi + 31) >> 5,
-        [&](int i, f32x16 &s) { kv8_scores<T, NK>(s, q.f, codes + i * NF * 64 + lane); },
-        [&](int i, f32x16 &s) {
-          const int n = __builtin_amdgcn_readlane(count, i), at = i * 32;
-          if (n < 32 || at + 32 > seen.tile_lo) mask_below(s, min(seen.row_hi - at, n), lane);
-        },
-        [&](int i) { return lane_of(ks, i); }, [&](int i) { return lane_of(lv, i); },
-        [&](int i, const f32x16 &s) {
-          const auto rf = st.ref(lane_of(lv, i));
-          return code_probs<T>(s, lane_of(ks, i), rf.c, rf.w, st.l);
-        },
-        [&](int i, const CodeProbs<T> &p) {
-          const u32x4 *fr = codes + (i * NF + NK) * 64 + lane;
-          code_values<T, ND>(st.o, p, [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(2 * n + f) * 64]); });
-        });
+    auto pass = [&](auto finite) {
+      typedef decltype(finite) F;
+      st.init();
+      attend_blocks<ND, CodeProbs<T>>(
+          st, (seen.tile_hi + 31) >> 5,
+          [&](int i, f32x16 &s) { kv8_scores<T, NK>(s, q.f, codes + i * NF * 64 + lane); },
+          [&](int i, f32x16 &s) {
+            const int n = __builtin_amdgcn_readlane(count, i), at = i * 32;
+            if (n < 32 || at + 32 > seen.tile_lo) mask_below(s, min(seen.row_hi - at, n), lane);
+          },
+          [&](int i) { return lane_of(ks, i); }, [&](int i) { return lane_of(lv, i); },
+          [&](int i, const f32x16 &s) {
+            const auto rf = st.ref(lane_of(lv, i));
+            return code_probs<T>(s, lane_of(ks, i), rf.c, rf.w, st.l);
+          },
+          [&](int i, const CodeProbs<T> &p) {
+            const u32x4 *fr = codes + (i * NF + NK) * 64 + lane;
+            code_values<T, ND, F::value>(st.o, p,
+                                         [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(2 * n + f) * 64]); });
+          });
+    };
+    pass(Finite<false>{});
+    if (seen.uneven(nk) && some_nan<ND>(st.o)) {
+      pass(Finite<true>{});
+      for (int b = 0; b * 32 < seen.tile_hi; ++b) spread_nan<D>(st.o, a.c, tab, b, g, seen.row_hi - b * 32, lane);
+    }
     const float unit = st.unit();
     if constexpr (BOX) {
       store_tile<T, ND>(a, st, unit, TileRows(a, sq, r0, rows), g, box, lane);

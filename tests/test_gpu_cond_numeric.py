@@ -75,3 +75,47 @@ def test_kv8_values_of_unlike_magnitude(torch, C, ql, kl, width, hq, h, spread, 
         worst = float((np.abs(got - ref) / t).max())
         _say(f"  worst error / bound {worst:.3f}")
         assert worst <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ql,kl,width,hq,h", [(4, 100, None, 4, 2), (4, 2500, None, 4, 2), (40, 64, None, 4, 2), (130, 140, None, 32, 4),
+                                              (300, 310, None, 32, 4), (300, 310, 40, 32, 4)])
+def test_kv8_unseen_nan(torch, C, ql, kl, width, hq, h, d, dtype):
+    """A causal row's result does not depend on NaN that it does not see: a cached NaN value reaches the rows that
+    see its token, in its channel; a NaN key the rows that see it, whole."""
+    _say(f"cached NaN, {ql} x {kl} of {d}, width {width}, {dtype}")
+    cache, table, kv, k, v = _fill(torch, C, [kl], h, d, width=width)
+    q = _randn(torch, 111, ql, hq, d, dtype=dtype)
+    seen_by = lambda tok: torch.arange(ql, device="cuda") >= tok - (kl - ql)     # rows that see a token
+    for tok, chan in ((kl - ql + 1, 5), (kl - 1, d - 1), (kl - (ql + 1) // 2, 0)):
+        bad = v.clone()
+        bad[tok, 0, chan] = 0                      # (no scale hangs on it)
+        C.kv8_append(cache, table, kv, k, bad, [kl])
+        clean = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
+        every = C.kv8_attention(q, cache, table, kv, [ql])
+        bad[tok, 0, chan] = float("nan")
+        C.kv8_append(cache, table, kv, k, bad, [kl])
+        want = clean.clone()
+        rows = seen_by(tok)
+        want[:, :hq // h, chan] = torch.where(rows[:, None], torch.full_like(want[:, :hq // h, chan], float("nan")),
+                                              want[:, :hq // h, chan])
+        got = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
+        assert bool(rows.any()) and not bool(rows.all())
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+        got = C.kv8_attention(q, cache, table, kv, [ql])                        # seen by all
+        assert bool(torch.isnan(got[:, :hq // h, chan]).all())
+        got[:, :hq // h, chan] = every[:, :hq // h, chan]
+        assert torch.equal(got, every)
+    bad = k.clone()
+    bad[kl - 2, 0, 3] = 0
+    C.kv8_append(cache, table, kv, bad, v, [kl])
+    clean = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
+    bad[kl - 2, 0, 3] = float("nan")
+    C.kv8_append(cache, table, kv, bad, v, [kl])
+    got = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
+    rows = seen_by(kl - 2)
+    assert bool(torch.isnan(got[rows][:, :hq // h]).all())
+    got[rows, :hq // h] = clean[rows, :hq // h]
+    assert torch.equal(got, clean)
