@@ -97,10 +97,18 @@ __device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0
 // ever after (with random scores every step raises some row's maximum a little, and the 64
 // multiplications of a rescaled O of 128 were a fifth of the step's vector work).
 // Probabilities are then at most 2^kSlack, and relative precision is what it was.
-constexpr float kSlack = 8.f;
+// Far out, where fp32's step at m is more than 2^-8, m is off the largest product of score and factor by as much, and
+// fma(score, factor, -m) with it, up to infinity: there the product is rounded, like m, before m is subtracted.
+constexpr float kSlack = 8.f, kFar = 0x1p16f;
+__device__ __forceinline__ void far_scores(f32x16 &s, float factor, float m) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = s[i] * factor - m;
+}
 template <int ND> struct Rows {
   f32x16 o[ND];
   float m, l;      // m in log2 units; l over this lane's keys only
+  bool far;        // wave-uniform: some row's m is beyond kFar
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int n = 0; n < ND; ++n)
@@ -108,6 +116,11 @@ template <int ND> struct Rows {
       for (int r = 0; r < 16; ++r) o[n][r] = 0.f;
     m = -INFINITY;
     l = 0.f;
+    far = false;
+  }
+  __device__ __forceinline__ void set(float m_new) {
+    m = m_new;
+    far = __any(fabsf(finite_ref(m)) >= kFar);
   }
   __device__ __forceinline__ void scale(float f) {
 #pragma unroll
@@ -130,7 +143,7 @@ template <int ND> struct Rows {
       l *= alpha;
       scale(alpha);
     }
-    m = m_new;
+    set(m_new);
   }
 };
 
@@ -298,13 +311,18 @@ __device__ __forceinline__ void set_probs(Probs<float> &o, const float *p) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) o.p[e] = p[e];
 }
-template <typename T>
-__device__ __forceinline__ Probs<T> probs_of(const f32x16 &s, float sc, float ref, float &l) {
+template <typename T, int ND>
+__device__ __forceinline__ Probs<T> probs_of(f32x16 &s, float sc, float ref, Rows<ND> &st) {
   float p[16];
+  if (st.far) {
+    far_scores(s, sc, ref);
+    sc = 1.f;
+    ref = 0.f;
+  }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -ref));
-    l += p[i];
+    st.l += p[i];
   }
   Probs<T> o;
   set_probs(o, p);
@@ -462,7 +480,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
     const float ref = st.raise(mb * a.sc);
 #pragma unroll
     for (int u = 0; u < NS; ++u)
-      add_values<T, DP>(st.o, probs_of<T>(s[u], a.sc, ref, st.l), sv, kw * NS + u, lane);
+      add_values<T, DP>(st.o, probs_of<T>(s[u], a.sc, ref, st), sv, kw * NS + u, lane);
   };
 
   for (int kt = span.lo; kt < span.hi; ++kt) {
@@ -728,7 +746,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
         mfma32(s, __builtin_bit_cast(bf16x8, sk[lrow * NCH + key_swz<NCH>(lrow, 2 * kk + h)]), qf[kk]);
       if (word != 0xFFFFFFFFu) mask_word(s, word);
       const float ref = st.raise(max16(s, -INFINITY) * a.sc);
-      add_values<bf16, DP>(st.o, probs_of<bf16>(s, a.sc, ref, st.l), (const char *)sv, 0, lane);
+      add_values<bf16, DP>(st.o, probs_of<bf16>(s, a.sc, ref, st), (const char *)sv, 0, lane);
     }
   }
   if (r0 >= rows) return;
@@ -768,6 +786,7 @@ template <int ND> struct CodeRows : Rows<ND> {
   using Rows<ND>::o;
   using Rows<ND>::m;
   using Rows<ND>::l;
+  using Rows<ND>::far;
   float u;
   __device__ __forceinline__ void init() {
     Rows<ND>::init();
@@ -796,15 +815,15 @@ template <int ND> struct CodeRows : Rows<ND> {
       l *= __builtin_amdgcn_exp2f(m - mr);
       Rows<ND>::scale(__builtin_amdgcn_exp2f(kept - finite_ref(u_new)));
     }
-    m = m_new;
+    Rows<ND>::set(m_new);
     u = u_new;
   }
-  // For the block of value scale 2^lv: a weight is 2^(score + c), w what its sum counts in l. Weights too far
+  // For the block of value scale 2^lv: a weight is 2^(score - m + c), w what its sum counts in l. Weights too far
   // below the row's largest (2^-60, nothing in fp16) are kept from fp32's own limit, for l.
-  struct Ref { float c, w; };
+  struct Ref { float m, c, w; };
   __device__ __forceinline__ Ref ref(float lv) const {
     const float x = fminf(finite_ref(u) - lv, 60.f);
-    return Ref{kPOff - finite_ref(m) - x, __builtin_amdgcn_exp2f(x)};
+    return Ref{finite_ref(m), kPOff - x, __builtin_amdgcn_exp2f(x)};
   }
   // What O is still to be multiplied by, 2^u: here in part where that is far from 1.
   __device__ __forceinline__ float unit() {
@@ -853,6 +872,10 @@ __device__ __forceinline__ void attend_blocks(CodeRows<ND> &st, int n, SC scores
     const float mb[2] = {max16(s0, -INFINITY) * factor(i), max16(s1, -INFINITY) * factor(i + 1)};
     const float at[2] = {lv(i), lv(i + 1)};
     st.template raise<2>(mb, at);
+    if (st.far) {
+      far_scores(s0, factor(i), finite_ref(st.m));
+      far_scores(s1, factor(i + 1), finite_ref(st.m));
+    }
     const P p0 = probs(i, s0);
     values(i, p0);
     const P p1 = probs(i + 1, s1);
@@ -864,6 +887,7 @@ __device__ __forceinline__ void attend_blocks(CodeRows<ND> &st, int n, SC scores
     mask(i, s0);
     const float mb[1] = {max16(s0, -INFINITY) * factor(i)}, at[1] = {lv(i)};
     st.template raise<1>(mb, at);
+    if (st.far) far_scores(s0, factor(i), finite_ref(st.m));
     values(i, probs(i, s0));
   }
 }
@@ -953,12 +977,16 @@ __device__ __forceinline__ void kv8_scores(f32x16 &s, const QCodes<T, NK> &q, co
   }
 }
 
-// Weights of one block, 2^(ksc s + c), as fp16 (fp32 calls: two terms); their sum, times w, joins l.
+// Weights of one block, 2^(ksc s - m + c), as fp16 (fp32 calls: two terms); their sum, times w, joins l. (st.far:
+// s has been through far_scores.)
 template <typename T> struct CodeProbs { f16x8 f[2], lo[sizeof(T) == 4 ? 2 : 1]; };
-template <typename T>
-__device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, float c, float w, float &l) {
+template <typename T, int ND>
+__device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, float lv, CodeRows<ND> &st) {
+  const auto rf = st.ref(lv);
   CodeProbs<T> o;
   float sum = 0.f;
+  const float c = st.far ? rf.c : rf.c - rf.m;
+  if (st.far) ksc = 1.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float p = __builtin_amdgcn_exp2f(fmaf(s[i], ksc, c));
@@ -966,7 +994,7 @@ __device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, f
     o.f[i >> 3][i & 7] = (f16)p;
     if constexpr (sizeof(T) == 4) o.lo[i >> 3][i & 7] = (f16)(p - (float)o.f[i >> 3][i & 7]);
   }
-  l = fmaf(sum, w, l);
+  st.l = fmaf(sum, rf.w, st.l);
   return o;
 }
 // O += V^T P^T; vf(n, f): value operand of d block n, keys 16 f ..
@@ -1188,8 +1216,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
         const float ksc = key_factor(cur.ref.ks, a.sc);
         const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur.ref.vs)};
         st.template raise<1>(mb, lv);
-        const auto rf = st.ref(lv[0]);
-        code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
+        if (st.far) far_scores(s, ksc, finite_ref(st.m));
+        code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, lv[0], st),
                                      [&](int n, int f) { return widen_f16(cur.v[n][2 * f], cur.v[n][2 * f + 1]); });
       }
       cur = nxt;
@@ -1295,8 +1323,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
             const float ksc = key_factor(cur[u].ks, a.sc);
             const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur[u].vs)};
             st.template raise<1>(mb, lv);
-            const auto rf = st.ref(lv[0]);
-            code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, rf.c, rf.w, st.l),
+            if (st.far) far_scores(s, ksc, finite_ref(st.m));
+            code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, lv[0], st),
                                          [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(NK + 2 * n + f) * 64]); });
           }
         }
@@ -1425,10 +1453,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
             if (n < 32 || at + 32 > seen.tile_lo) mask_below(s, min(seen.row_hi - at, n), lane);
           },
           [&](int i) { return lane_of(ks, i); }, [&](int i) { return lane_of(lv, i); },
-          [&](int i, const f32x16 &s) {
-            const auto rf = st.ref(lane_of(lv, i));
-            return code_probs<T>(s, lane_of(ks, i), rf.c, rf.w, st.l);
-          },
+          [&](int i, const f32x16 &s) { return code_probs<T>(s, lane_of(ks, i), lane_of(lv, i), st); },
           [&](int i, const CodeProbs<T> &p) {
             const u32x4 *fr = codes + (i * NF + NK) * 64 + lane;
             code_values<T, ND, F::value>(st.o, p,

@@ -119,3 +119,46 @@ def test_kv8_unseen_nan(torch, C, ql, kl, width, hq, h, d, dtype):
     assert bool(torch.isnan(got[rows][:, :hq // h]).all())
     got[rows, :hq // h] = clean[rows, :hq // h]
     assert torch.equal(got, clean)
+
+
+def _far(torch, q_len, kv_len, hq, h, d, sign, dtype):
+    """One channel: queries of 165 * 2^10, keys of 9 * 2^14, the heaviest 9 * 2^15 (sign -1: -9 * 2^15 and -9 * 2^14): scores of
+    1485 * 2^24 and twice that, exact, in units of which any scale takes fp32 past its whole numbers."""
+    win = kv_len * 2 // 3
+    q = torch.zeros(q_len, hq, d)
+    k = torch.zeros(kv_len, h, d)
+    q[..., 3] = 165 * 2.0 ** 10
+    k[..., 3] = 9 * 2.0 ** 14 * (1 if sign > 0 else -2)
+    k[win, :, 3] = 9 * 2.0 ** 14 * (2 if sign > 0 else -1)
+    return q.to(dtype).cuda(), k.to(dtype).cuda(), win
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,hq,h,d", [(1, 96, 4, 2, 64), (33, 130, 4, 2, 128), (2, 2500, 4, 2, 64), (2100, 96, 8, 8, 64),
+                                          (2100, 96, 4, 2, 128), (600, 2500, 16, 16, 64)])
+def test_cross_scores_far_out(torch, C, ql, kl, hq, h, d, dtype):
+    """Scores past fp32's whole numbers: the heaviest key takes all, exactly."""
+    _say(f"cross, scores of 2^34, {ql} x {kl}, {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    v = _randn(torch, 112, kl, h, d, dtype=dtype)
+    for sign in (1, -1):
+        q, k, win = _far(torch, ql, kl, hq, h, d, sign, dt)
+        for scale in (1.0, 1.3, 0.9, 0.071):
+            got = C.cross_attention(q, k, v, [ql], [kl], scale=scale)
+            assert torch.equal(got, v[win].repeat_interleave(hq // h, 0)[None].expand(ql, -1, -1)), (sign, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ql,kl,width,hq,h", CACHED)
+def test_kv8_scores_far_out(torch, C, ql, kl, width, hq, h, d, dtype):
+    _say(f"cached, scores of 2^34, {ql} x {kl} of {d}, width {width}, {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    cache, table, kv, _, v = _fill(torch, C, [kl], h, d, width=width)
+    for sign in (1, -1):
+        q, k, win = _far(torch, ql, kl, hq, h, d, sign, dt)
+        C.kv8_append(cache, table, kv, k.to(v.dtype), v, [kl])
+        _, rv = C.kv8_read(cache, table, kv, [kl], dtype=dt)
+        for scale in (1.0, 1.3, 0.9, 0.071):
+            got = C.kv8_attention(q, cache, table, kv, [ql], scale=scale)
+            assert torch.equal(got, rv[win].repeat_interleave(hq // h, 0)[None].expand(ql, -1, -1)), (sign, scale)
