@@ -1039,8 +1039,9 @@ __device__ __forceinline__ Seen seen_of(const Kv8AttnArgs &a, const CondSeq &sq,
   return v;
 }
 
-// What scores of a block's key codes are multiplied by; never 0, so that a masked score stays -inf.
-__device__ __forceinline__ float key_factor(float ks, float sc) { return fmaxf(ks * sc, 0x1p-149f); }
+// What scores of a block's key codes are multiplied by; never 0 or infinite, so that a masked score stays -inf
+// and one of 0 stays 0. (Beyond either end no query that is not 0 has a score within fp32.)
+__device__ __forceinline__ float key_factor(float ks, float sc) { return fminf(fmaxf(ks * sc, 0x1p-149f), 0x1.fffffep127f); }
 
 // A block of the pool, or none: its number times heads + g, and its scales (vs < 0: none).
 struct BlockRef { int64_t at; float ks, vs; };

@@ -162,3 +162,23 @@ def test_kv8_scores_far_out(torch, C, ql, kl, width, hq, h, d, dtype):
         for scale in (1.0, 1.3, 0.9, 0.071):
             got = C.kv8_attention(q, cache, table, kv, [ql], scale=scale)
             assert torch.equal(got, rv[win].repeat_interleave(hq // h, 0)[None].expand(ql, -1, -1)), (sign, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,width,hq,h", CACHED)
+def test_kv8_largest_keys_under_zero_queries(torch, C, ql, kl, width, hq, h, dtype):
+    """Keys at the largest block scale and a large factor: their product is beyond fp32, a score of 0 is 0 all
+    the same, and all tokens weigh alike."""
+    _say(f"cached, zero queries over the largest keys, {ql} x {kl}, width {width}, {dtype}")
+    d = 64
+    cache, table, kv, k, v = _fill(torch, C, [kl], h, d, width=width, spread=False)
+    k[:] = 3.2e38
+    C.kv8_append(cache, table, kv, k, v, [kl])
+    assert bool((cache.scales[table[0, :(kl + 31) // 32].long(), :, 0] == 2.0 ** 120).all())
+    q = torch.zeros((ql, hq, d), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    got = _f64(C.kv8_attention(q, cache, table, kv, [ql], scale=512.0))
+    (_, vv), = _held(torch, cache, table, [kl])
+    ref, mag = vv.mean(0).repeat(hq // h, 0)[None], np.abs(vv).mean(0).repeat(hq // h, 0)[None]
+    # p = 1 exactly: sums of kl terms, their quotient, the result
+    t = 2 * (kl + 16) * U * mag + (U16 if dtype == "bf16" else U) * np.abs(ref)
+    assert (np.abs(got - ref) <= t).all()
