@@ -43,7 +43,7 @@ extern "C" {
  *  h / (Hq/Hkv)), head_dim = d.
  *  dtype: mte_dtype of q, k, v and out. Scores, softmax and sums are fp32; with
  *  MTE_BF16 the probabilities are rounded to 16 bits before they meet the values.
- *  scale: multiplies q.k; finite and > 0.
+ *  scale: multiplies q.k; > 0, and finite also times log2(e).
  *  *_row / *_head: elements from one token's row to the next, and from one head
  *  to the next within a row (the d elements of a head are contiguous). The
  *  halves of a fused key/value projection are row strides of 2 Hkv d; a

@@ -16,6 +16,7 @@ constexpr int64_t kMaxRows = 0x7FFFFFFF;
 constexpr int64_t kMaxStride = (int64_t)1 << 40;     // row * stride stays inside 64 bits
 constexpr int32_t kMaxWidth = (1 << 26) - 1;         // 32 * table_width stays inside 31 bits
 constexpr int32_t kMaxGrid = 65535;
+constexpr float kLog2e = 1.4426950408889634f;
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 bool stride_ok(int64_t s) { return s >= 0 && s <= kMaxStride && s % 8 == 0; }
@@ -39,7 +40,7 @@ int shape_status(const mte_attn_shape *s, bool (*built)(int32_t)) {
   if (s->n_q_heads <= 0 || s->n_kv_heads <= 0 || s->head_dim <= 0 || s->n_q_heads % s->n_kv_heads) return MTE_E_INVALID;
   if (s->n_kv_heads > kMaxGrid) return MTE_E_INVALID;
   if (s->dtype != MTE_F32 && s->dtype != MTE_BF16) return MTE_E_INVALID;
-  if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return MTE_E_INVALID;
+  if (!(s->scale > 0.f) || !std::isfinite(s->scale * kLog2e)) return MTE_E_INVALID;
   if (!built(s->head_dim)) return MTE_E_UNSUPPORTED;
   if (!stride_ok(s->q_row) || !stride_ok(s->q_head) || !stride_ok(s->o_row) || !stride_ok(s->o_head))
     return MTE_E_INVALID;
@@ -62,7 +63,7 @@ AttnProblem problem(const mte_attn_shape &s, const int32_t *q_lens, int32_t n) {
   p.c.q_head = s.q_head;
   p.c.o_row = s.o_row;
   p.c.o_head = s.o_head;
-  p.c.sc = s.scale * 1.4426950408889634f;
+  p.c.sc = s.scale * kLog2e;
   p.c.d = s.head_dim;
   p.c.hkv = s.n_kv_heads;
   p.c.rep = s.n_q_heads / s.n_kv_heads;
