@@ -24,7 +24,7 @@
  * that share no written buffer may overlap in time. A workspace needs no
  * initial value, carries nothing from one call to the next, and may be shared
  * by calls that run one after the other; not by calls (or replays of captured
- * graphs) that overlap in time.
+ * graphs) that overlap in time. Everything is forward: results carry no gradient.
  */
 #ifndef MTE_COND_H
 #define MTE_COND_H
@@ -49,7 +49,8 @@ extern "C" {
  *  halves of a fused key/value projection are row strides of 2 Hkv d; a
  *  head-major tensor [H, T, d] is row d, head T d. A stride is 0 or more and a
  *  multiple of 8; every base address is aligned to 16 bytes. k_* and v_* are not
- *  read by mte_kv8_attention. out's rows and heads must not overlap. */
+ *  read by mte_kv8_attention. out's rows and heads must not overlap. out may be q (the same
+ *  address and strides: every row is read before it is written), else it overlaps no input. */
 typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
   int32_t dtype;
@@ -66,7 +67,7 @@ typedef struct {
  *  q, out:   device, sum(q_lens) rows, sequences back to back in q_lens order.
  *  k, v:     device, sum(kv_lens) rows, back to back in kv_lens order.
  *  key_mask: device uint8[sum(kv_lens)], or NULL (all tokens count).
- *  q_lens:   HOST int32[n_q], each >= 0; kv_lens: HOST int32[n_kv], each >= 0.
+ *  q_lens:   HOST int32[n_q], each >= 0; kv_lens: HOST int32[n_kv], each >= 0; n_q and n_kv at least 1.
  *  kv_index: HOST int32[n_q], the kv sequence of each query sequence (several may
  *            name the same one: one frame's conditioning for all); NULL: b
  *            itself, n_q == n_kv.
@@ -130,7 +131,7 @@ typedef struct {
  * subnormal, which move by at most 2^-10 of the new scale). Code: nearest to x / 2^e,
  * ties to the even one; NaN stays NaN; at the largest scale, 2^120, magnitudes end at
  * 240 * 2^120 (infinities become that), so that every stored value is finite in fp32. Places of a touched block past the length are set to zero.
- * new_lens: HOST int32[n], each >= 0. Errors: MTE_E_INVALID, MTE_E_UNSUPPORTED
+ * new_lens: HOST int32[n], each >= 0; n >= 1. Errors: MTE_E_INVALID, MTE_E_UNSUPPORTED
  * (head_dim), MTE_E_HIP. */
 int mte_kv8_append(const mte_kv8 *cache, const int32_t *table, int32_t table_width, int64_t table_row,
                    const int32_t *kv_lens, const void *k, int64_t k_row, int64_t k_head, const void *v,
@@ -141,7 +142,7 @@ int mte_kv8_append(const mte_kv8 *cache, const int32_t *table, int32_t table_wid
  * contiguous [sum(counts), Hkv, d], aligned to 16 bytes) receive code * scale (exact,
  * but for bf16 magnitudes below 2^-126: they are rounded to its multiples of 2^-133) of tokens kv_lens[i] - counts[i] .. kv_lens[i] - 1, packed back to
  * back (rows of tokens before the first or beyond the table: zeros). counts: HOST
- * int32[n], each >= 0. Errors as mte_kv8_append. */
+ * int32[n], each >= 0; n >= 1. Errors as mte_kv8_append. */
 int mte_kv8_read(const mte_kv8 *cache, const int32_t *table, int32_t table_width, int64_t table_row,
                  const int32_t *kv_lens, const int32_t *counts, int32_t n, void *k, void *v, int32_t dtype,
                  hipStream_t stream);
@@ -150,7 +151,7 @@ int mte_kv8_read(const mte_kv8 *cache, const int32_t *table, int32_t table_width
  * attend to its kv_lens[i] cached tokens; with causal = 1 its query u sees tokens
  * 0 .. kv_lens[i] - q_lens[i] + u only (its own token last: append, then attend).
  * A query that sees nothing gets zeros. Formula, q, out and workspace as in
- * mte_cross_attention (workspace: mte_kv8_attention_workspace); q_lens: HOST int32[n].
+ * mte_cross_attention (workspace: mte_kv8_attention_workspace); q_lens: HOST int32[n], n >= 1.
  * Rounding: a token's weight, its probability times the scale of its block's values, meets the codes with 11
  * significant bits (MTE_F32: 22), and none below 2^-31 of the largest weight of its row; whatever
  * scales the blocks of lesser weight have. What tokens that a query does not see hold does not reach it; a
@@ -177,7 +178,7 @@ int64_t mte_kv8_attention_workspace(const mte_attn_shape *shape, const int32_t *
  *     (>= 0; rows of a wider buffer may be normalised in place of a copy). y alike;
  *     y may be x (same strides), else they must not overlap.
  *  gamma, beta: device, dtype, [channels], or NULL (1 / 0).
- *  groups divides channels. eps >= 0 and finite.
+ *  groups divides channels; n and groups are at most 65535. eps >= 0 and finite.
  *  workspace: device, at least mte_group_norm_workspace(...) bytes, aligned to 16; NULL
  *     where that is 0.
  * Buffers need only be aligned like one element (16 bytes and strides that are

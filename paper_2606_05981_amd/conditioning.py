@@ -2,7 +2,8 @@
 read the encoder's conditioning (cross attention, an 8-bit key/value cache, group norm).
 
 Tensors in, tensors out, as in ``encoder``: PyTorch provides memory and streams, every step
-runs in libmte's HIP kernels, nothing falls back. Workspaces are taken from torch's
+runs in libmte's HIP kernels, nothing falls back. Forward only: results carry no gradient, also where
+inputs require one. Workspaces are taken from torch's
 allocator call by call, on the stream the call runs on, so calls on several streams and
 captured graphs share none. A call given a `stream` other than the current one orders
 nothing by itself: the caller makes that stream wait for the inputs, and the current
@@ -121,7 +122,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: S
     of each query sequence (default: its own), so that one frame's conditioning can serve all
     ([0] * len(q_lens), as with TECache's batch_one); key_mask: uint8 or bool [Tk], 0 hides a
     token from every query; scale: default 1 / sqrt(d). A query that sees no token gets
-    zeros. q, k, v (bf16 or fp32) may be strided over tokens and heads."""
+    zeros. q, k, v (bf16 or fp32) may be strided over tokens and heads; out may be q."""
     hq, d, dtype, dev = _query(q)
     hkv = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
     sq = _rows("q", q, dtype, hq, d, dev)
@@ -232,7 +233,8 @@ def kv8_append(cache, table: torch.Tensor, kv_lens: torch.Tensor, k: torch.Tenso
 def kv8_read(cache, table: torch.Tensor, kv_lens: torch.Tensor, counts: Sequence[int],
              dtype: torch.dtype = torch.bfloat16, stream: Optional[torch.cuda.Stream] = None):
     """mte_kv8_read: the newest counts[i] tokens of each sequence -> (k, v), each
-    [sum(counts), Hkv, d] of `dtype` (bf16 or fp32, both exact)."""
+    [sum(counts), Hkv, d] of `dtype` (bf16 or fp32, both exact, but for bf16 magnitudes below 2^-126: rounded to
+    multiples of 2^-133)."""
     if dtype not in _DTYPE:
         raise ValueError("dtype: expected torch.bfloat16 or torch.float32")
     dev = cache[0].device
@@ -258,7 +260,7 @@ def kv8_attention(q: torch.Tensor, cache, table: torch.Tensor, kv_lens: torch.Te
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """mte_kv8_attention: packed queries q [Tq, Hq, d] attend to their sequence's cached tokens ->
     [Tq, Hq, d]. causal: query u of q_lens[i] sees the tokens up to kv_lens[i] - q_lens[i] + u
-    (append its own token first). The work is split for sequences as long as the table is wide:
+    (append its own token first). out may be q. The work is split for sequences as long as the table is wide:
     a narrower view table[:, :m] serves shorter ones better."""
     hq, d, dtype, dev = _query(q)
     keep, lens, n = _lens("q_lens", q_lens, q.shape[0])

@@ -182,3 +182,80 @@ def test_kv8_largest_keys_under_zero_queries(torch, C, ql, kl, width, hq, h, dty
     # p = 1 exactly: sums of kl terms, their quotient, the result
     t = 2 * (kl + 16) * U * mag + (U16 if dtype == "bf16" else U) * np.abs(ref)
     assert (np.abs(got - ref) <= t).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_kv8_append_beside_refused_sequences(torch, C, d):
+    """A length that does not fit leaves its own sequence's blocks as they were; the sequences beside it are
+    written, from their own rows."""
+    _say(f"append beside refused sequences, d {d}")
+    h, new = 2, [20, 0, 35, 20]
+    k, v = _randn(torch, 113, sum(new), h, d), _randn(torch, 114, sum(new), h, d)
+    start = [0, 20, 20, 55, 75]
+    for lens in ([20, 0, 34, 20], [19, 5, 40, 20], [20, 0, 35, 65], [-5, 0, 64, 2**31 - 1], [64, -1, 36, -2**31]):
+        cache = C.kv8_cache(8, h, d)
+        table = _i32(torch, [[7, 2], [3, 5], [0, 6], [4, 1]])
+        C.kv8_append(cache, table, _i32(torch, lens), k, v, new)
+        for i, (n, m) in enumerate(zip(lens, new)):
+            blocks = table[i].long()
+            if m == 0 or n < m or n > 64:
+                assert not bool(cache.k_codes[blocks].any()) and not bool(cache.v_codes[blocks].any())
+                assert bool((cache.scales[blocks] == 2.0 ** -126).all())
+                continue
+            one = C.kv8_cache(8, h, d)               # the same rows alone
+            C.kv8_append(one, table[i:i + 1], _i32(torch, [n]), k[start[i]:start[i + 1]], v[start[i]:start[i + 1]], [m])
+            assert bool(one.k_codes[blocks].any())
+            for a, b in zip(cache, one):
+                assert torch.equal(a[blocks], b[blocks])
+            (kk, vv), = _held(torch, cache, table[i:i + 1], [n])
+            for rows, got in ((k, kk), (v, vv)):
+                ref = O.Cache(h, d)
+                if n > m:
+                    ref.append(np.zeros((n - m, h, d)))
+                ref.append(_f64(rows[start[i]:start[i + 1]]))
+                np.testing.assert_array_equal(got, ref.values())
+
+
+def test_kv8_read_smallest_values(torch, C):
+    """Values at the smallest scale, 2^-126: fp32 holds them all, bf16 those that are multiples of 2^-133; the others
+    are rounded to one, ties to even."""
+    _say("read, smallest values")
+    h, d = 1, 64
+    codes = torch.tensor([c for c in range(256) if c & 0x7F != 0x7F], dtype=torch.int64)   # all but NaN
+    rows = torch.cat([codes, codes[:2]]).reshape(4, 1, 64)
+    cache = C.kv8_cache(1, h, d)
+    lut = torch.from_numpy(O.Q.decode_table()).double()
+    x = (lut[rows] * 2.0 ** -126).float()            # exact
+    C.kv8_append(cache, _i32(torch, [[0]]), _i32(torch, [4]), x.cuda(), x.cuda(), [4])
+    assert bool((cache.scales == 2.0 ** -126).all())
+    for got in C.kv8_read(cache, _i32(torch, [[0]]), _i32(torch, [4]), [4], dtype=torch.float32):
+        assert torch.equal(got.cpu(), x)
+    steps = torch.round(x.double() * 2.0 ** 133) * 2.0 ** -133                  # ties to even
+    want = torch.where(x.double().abs() < 2.0 ** -126, steps, x.double())
+    for got in C.kv8_read(cache, _i32(torch, [[0]]), _i32(torch, [4]), [4]):
+        assert torch.equal(got.double().cpu(), want)
+    assert not torch.equal(want, x.double())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,hq,h,d", [([40, 3], [96, 7], 4, 2, 64), ([3, 2], [2500, 40], 4, 2, 64), ([2100], [96], 16, 8, 128),
+                                          ([1300, 9], [130, 70], 8, 8, 40), ([600], [2500], 16, 16, 64)])
+def test_cross_in_place_of_the_queries(torch, C, ql, kl, hq, h, d, dtype):
+    _say(f"cross, out = q, {ql} x {kl} {dtype}")
+    q = _randn(torch, 116, sum(ql), hq, d, dtype=dtype)
+    k, v = _randn(torch, 117, sum(kl), h, d, dtype=dtype), _randn(torch, 118, sum(kl), h, d, dtype=dtype)
+    want = C.cross_attention(q, k, v, ql, kl)
+    got = C.cross_attention(q, k, v, ql, kl, out=q)
+    assert got is q and torch.equal(q, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ql,kl,width,hq,h", CACHED)
+def test_kv8_in_place_of_the_queries(torch, C, ql, kl, width, hq, h, d, dtype):
+    _say(f"cached, out = q, {ql} x {kl} of {d}, width {width}, {dtype}")
+    cache, table, kv, _, _ = _fill(torch, C, [kl], h, d, width=width)
+    q = _randn(torch, 119, ql, hq, d, dtype=dtype)
+    want = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
+    got = C.kv8_attention(q, cache, table, kv, [ql], causal=True, out=q)
+    assert got is q and torch.equal(q, want)
