@@ -271,7 +271,7 @@ __global__ __launch_bounds__(TH) void k_gn_stats(GnArgs a) {
     for (int e = 0; e < V; ++e) {
       const float d = s[e] - mean[e];
       mean[e] = fmaf(d, share, mean[e]);
-      sq[e] += fmaf(d * d, cross, q[e]);
+      sq[e] += fmaf(d * cross, d, q[e]);            // (the first batch: cross = 0, and d the mean, whose square may overflow)
     }
     n = all;
   }

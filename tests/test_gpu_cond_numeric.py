@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from oracle import cond_oracle as O
-from tests.test_gpu_cond import U, U16, _f64, _fill, _held, _i32, _randn
+from tests.test_gpu_cond import U, U16, _check_norm, _f64, _fill, _held, _i32, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -259,3 +259,14 @@ def test_kv8_in_place_of_the_queries(torch, C, ql, kl, width, hq, h, d, dtype):
     want = C.kv8_attention(q, cache, table, kv, [ql], causal=True)
     got = C.kv8_attention(q, cache, table, kv, [ql], causal=True, out=q)
     assert got is q and torch.equal(q, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,px,c,groups", [(1, 4096, 5, 5), (1, 9, 64, 8), (2, 2048, 6, 3)])
+def test_group_norm_mean_whose_square_overflows(torch, C, n, px, c, groups, dtype):
+    """A mean of 1.5 * 2^64, beyond fp32 when squared, under a spread of 2^57.6: only differences are squared."""
+    _say(f"group norm, mean of 2^64.6, {n} x {px} x {c} / {groups}, {dtype}")
+    g = torch.Generator().manual_seed(125)
+    x = 1.5 * (1 + 2.0 ** -7 * torch.randint(-1, 2, (n, px, c), generator=g)) * 2.0 ** 64   # (8 bits: exact in bf16)
+    x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+    _check_norm(torch, C.group_norm(x, groups), x, groups, None, None, 1e-5, None, dtype)
