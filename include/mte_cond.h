@@ -77,7 +77,7 @@ typedef struct {
  * runs. Which kernel takes the rows and how a long key range is split goes by the
  * whole call, so that other sequences may change the last bits of a result.
  * Errors: MTE_E_INVALID (null, negative length, bad index, heads, dtype, scale,
- * strides or alignment, a sum of lengths beyond 2^31 - 1), MTE_E_UNSUPPORTED
+ * strides or alignment, a sum of kv_lens, or of q_lens times heads, beyond 2^31 - 4097), MTE_E_UNSUPPORTED
  * (head_dim), MTE_E_CAPACITY (workspace_bytes), MTE_E_HIP. No query rows at all
  * is MTE_OK and enqueues nothing (then q and out may be NULL, and k and v where
  * there are no key rows). */
@@ -159,7 +159,7 @@ int mte_kv8_read(const mte_kv8 *cache, const int32_t *table, int32_t table_width
  * The work is split for sequences of up to 32 table_width tokens: a table that
  * is much wider than its sequences costs time.
  * Errors: MTE_E_INVALID, MTE_E_UNSUPPORTED (head_dim), MTE_E_CAPACITY
- * (workspace_bytes), MTE_E_HIP. */
+ * (workspace_bytes), MTE_E_HIP, sizes as in mte_cross_attention. */
 int mte_kv8_attention(const mte_attn_shape *shape, const mte_kv8 *cache, const int32_t *table,
                       int32_t table_width, int64_t table_row, const int32_t *kv_lens, const void *q,
                       const int32_t *q_lens, int32_t n, int32_t causal, void *out, void *workspace,

@@ -12,7 +12,7 @@ using namespace mte;
 
 namespace {
 
-constexpr int64_t kMaxRows = 0x7FFFFFFF;
+constexpr int64_t kMaxRows = 0x7FFFFFFF - 4096;      // a last tile's end, up to 4096 rows on, stays inside 31 bits
 constexpr int64_t kMaxStride = (int64_t)1 << 40;     // row * stride stays inside 64 bits
 constexpr int32_t kMaxWidth = (1 << 26) - 1;         // 32 * table_width stays inside 31 bits
 constexpr int32_t kMaxGrid = 65535;
