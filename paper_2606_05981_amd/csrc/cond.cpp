@@ -74,8 +74,9 @@ AttnProblem problem(const mte_attn_shape &s, const int32_t *q_lens, int32_t n) {
   p.c.big = 0;
   p.dtype = s.dtype;
   p.near_rows = s.k_row < (1 << 24) && s.v_row < (1 << 24);
-  const auto near = [&](int64_t row, int64_t head) {   // 31 rows and rep heads: 2^29 + 2^30 elements
-    return row < (1 << 24) && head < ((int64_t)1 << 30) && (p.c.rep - 1) * head < ((int64_t)1 << 30);
+  // 31 rows and rep heads: 2^29 + 2^30 elements; rep: what the tiles divide by in fp32 (exact below 2^22)
+  const auto near = [&](int64_t row, int64_t head) {
+    return p.c.rep <= (1 << 16) && row < (1 << 24) && head < ((int64_t)1 << 30) && (p.c.rep - 1) * head < ((int64_t)1 << 30);
   };
   p.near_tiles = near(s.q_row, s.q_head) && near(s.o_row, s.o_head);
   p.q_lens = q_lens;

@@ -570,7 +570,7 @@ struct TileRows {
   // elements from the base to row r0 + i
   __device__ __forceinline__ uint32_t offset(int i, int64_t row, int64_t head, int rep) const {
     if (rep == 1) return __umul24(i, (uint32_t)row);
-    const int x = rem0 + i, t = (int)(((float)x + 0.5f) * inv);   // small numbers: exact in fp32
+    const int x = rem0 + i, t = (int)(((float)x + 0.5f) * inv);   // exact: rep is 2^16 at most
     return __umul24(t, (uint32_t)row) + (uint32_t)(x - t * rep) * (uint32_t)head;
   }
 };

@@ -270,3 +270,22 @@ def test_group_norm_mean_whose_square_overflows(torch, C, n, px, c, groups, dtyp
     x = 1.5 * (1 + 2.0 ** -7 * torch.randint(-1, 2, (n, px, c), generator=g)) * 2.0 ** 64   # (8 bits: exact in bf16)
     x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
     _check_norm(torch, C.group_norm(x, groups), x, groups, None, None, 1e-5, None, dtype)
+
+
+def test_cross_more_heads_than_fp32_counts(torch, C):
+    """2^24 query heads on one kv head, rows of a wider buffer: rows are found by whole numbers, not in fp32."""
+    _say("cross, 2^24 heads")
+    hq, d = 1 << 24, 8
+    wide = [torch.full((2, hq * d + 64), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    q, out = (w.as_strided((2, hq, d), (hq * d + 64, d, 1)) for w in wide)
+    q.copy_(torch.randn(2, hq, d, generator=torch.Generator("cuda").manual_seed(126), device="cuda"))
+    k, v = _randn(torch, 127, 3, 1, d), _randn(torch, 128, 3, 1, d)
+    C.cross_attention(q, k, v, [2], [3], out=out)
+    kf, vf = k[:, 0].float(), v[:, 0].float()
+    for i in range(2):
+        p = torch.softmax(torch.stack([(q[i].float() * x).sum(-1) for x in kf], -1) / d ** 0.5, -1)
+        ref = sum(p[:, j:j + 1] * vf[j] for j in range(3))
+        mag = sum(p[:, j:j + 1] * vf[j].abs() for j in range(3))
+        # the probabilities' and the result's rounding; fp32 on both sides: (d + 16) u each of the scores, |s| < 40
+        assert bool(((out[i].float() - ref).abs() <= U16 * (mag + ref.abs()) * 1.01 + 4 * 40 * (d + 16) * U * mag).all())
+    assert all(bool((w[:, -64:] == 7.0).all()) for w in wide)
