@@ -98,7 +98,8 @@ __device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0
 // multiplications of a rescaled O of 128 were a fifth of the step's vector work).
 // Probabilities are then at most 2^kSlack, and relative precision is what it was.
 // Far out, where fp32's step at m is more than 2^-8, m is off the largest product of score and factor by as much, and
-// fma(score, factor, -m) with it, up to infinity: there the product is rounded, like m, before m is subtracted.
+// fma(score, factor, -m) with it, up to infinity: there the product is rounded, like m, before m is subtracted, in
+// the branch that moves m, which far rows always take (as a branch of its own: 1 to 2% of a call).
 constexpr float kSlack = 8.f, kFar = 0x1p16f;
 __device__ __forceinline__ void far_scores(f32x16 &s, float factor, float m) {
 #pragma clang fp contract(off)
@@ -108,7 +109,7 @@ __device__ __forceinline__ void far_scores(f32x16 &s, float factor, float m) {
 template <int ND> struct Rows {
   f32x16 o[ND];
   float m, l;      // m in log2 units; l over this lane's keys only
-  bool far;        // wave-uniform: some row's m is beyond kFar
+  float slack;     // kSlack, -inf where some row's m is beyond kFar; wave-uniform
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int n = 0; n < ND; ++n)
@@ -116,11 +117,14 @@ template <int ND> struct Rows {
       for (int r = 0; r < 16; ++r) o[n][r] = 0.f;
     m = -INFINITY;
     l = 0.f;
-    far = false;
+    slack = kSlack;
   }
-  __device__ __forceinline__ void set(float m_new) {
+  // Sets m; whether it is far out.
+  __device__ __forceinline__ bool set(float m_new) {
     m = m_new;
-    far = __any(fabsf(finite_ref(m)) >= kFar);
+    const bool far = __any(fabsf(finite_ref(m)) >= kFar);
+    slack = far ? -INFINITY : kSlack;
+    return far;
   }
   __device__ __forceinline__ void scale(float f) {
 #pragma unroll
@@ -128,14 +132,21 @@ template <int ND> struct Rows {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[n][r] *= f;
   }
-  // Takes the maximum mb (log2 units) of this lane's new scores and returns what to subtract from them.
-  __device__ __forceinline__ float raise(float mb) {
-    if (over(mb)) lift(mb);
-    return ref();
+  // Takes new scores, their maximum mb (log2 units) and their factor; a probability is then 2^(s factor - ref).
+  template <int N> __device__ __forceinline__ void raise(f32x16 (&s)[N], float mb, float &factor, float &ref) {
+    ref = finite_ref(m);
+    if (__any(mb > m + slack)) {
+      const bool far = lift(mb);
+      ref = finite_ref(m);
+      if (far) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) far_scores(s[i], factor, ref);
+        factor = 1.f;
+        ref = 0.f;
+      }
+    }
   }
-  __device__ __forceinline__ bool over(float mb) const { return __any(mb > m + kSlack); }   // wave-uniform
-  __device__ __forceinline__ float ref() const { return finite_ref(m); }
-  __device__ __forceinline__ void lift(float mb) {
+  __device__ __forceinline__ bool lift(float mb) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
     const float m_new = fmaxf(m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
     if (__any(m != -INFINITY)) {                        // else O and l are still zero
@@ -143,7 +154,7 @@ template <int ND> struct Rows {
       l *= alpha;
       scale(alpha);
     }
-    set(m_new);
+    return set(m_new);
   }
 };
 
@@ -311,18 +322,13 @@ __device__ __forceinline__ void set_probs(Probs<float> &o, const float *p) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) o.p[e] = p[e];
 }
-template <typename T, int ND>
-__device__ __forceinline__ Probs<T> probs_of(f32x16 &s, float sc, float ref, Rows<ND> &st) {
+template <typename T>
+__device__ __forceinline__ Probs<T> probs_of(const f32x16 &s, float sc, float ref, float &l) {
   float p[16];
-  if (st.far) {
-    far_scores(s, sc, ref);
-    sc = 1.f;
-    ref = 0.f;
-  }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -ref));
-    st.l += p[i];
+    l += p[i];
   }
   Probs<T> o;
   set_probs(o, p);
@@ -477,10 +483,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
       if (word != 0xFFFFFFFFu) mask_word(s[u], word);
       mb = max16(s[u], mb);
     }
-    const float ref = st.raise(mb * a.sc);
+    float sc = a.sc, ref;
+    st.raise(s, mb * sc, sc, ref);
 #pragma unroll
     for (int u = 0; u < NS; ++u)
-      add_values<T, DP>(st.o, probs_of<T>(s[u], a.sc, ref, st), sv, kw * NS + u, lane);
+      add_values<T, DP>(st.o, probs_of<T>(s[u], sc, ref, st.l), sv, kw * NS + u, lane);
   };
 
   for (int kt = span.lo; kt < span.hi; ++kt) {
@@ -738,15 +745,16 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
     __syncthreads();                                // the tile is whole, and the one before it read
     if (t + 2 < t1) copy_tile(t + 2);
     if (r0 < rows) {                                // wave-uniform
-      f32x16 s;
+      f32x16 s[1];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+      for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk)
-        mfma32(s, __builtin_bit_cast(bf16x8, sk[lrow * NCH + key_swz<NCH>(lrow, 2 * kk + h)]), qf[kk]);
-      if (word != 0xFFFFFFFFu) mask_word(s, word);
-      const float ref = st.raise(max16(s, -INFINITY) * a.sc);
-      add_values<bf16, DP>(st.o, probs_of<bf16>(s, a.sc, ref, st), (const char *)sv, 0, lane);
+        mfma32(s[0], __builtin_bit_cast(bf16x8, sk[lrow * NCH + key_swz<NCH>(lrow, 2 * kk + h)]), qf[kk]);
+      if (word != 0xFFFFFFFFu) mask_word(s[0], word);
+      float sc = a.sc, ref;
+      st.raise(s, max16(s[0], -INFINITY) * sc, sc, ref);
+      add_values<bf16, DP>(st.o, probs_of<bf16>(s[0], sc, ref, st.l), (const char *)sv, 0, lane);
     }
   }
   if (r0 >= rows) return;
@@ -786,20 +794,37 @@ template <int ND> struct CodeRows : Rows<ND> {
   using Rows<ND>::o;
   using Rows<ND>::m;
   using Rows<ND>::l;
-  using Rows<ND>::far;
+  using Rows<ND>::slack;
   float u;
   __device__ __forceinline__ void init() {
     Rows<ND>::init();
     u = -INFINITY;
   }
-  // Takes the maxima mb (log2 units) of this lane's new scores in N blocks of value scales 2^lv.
-  template <int N> __device__ __forceinline__ void raise(const float (&mb)[N], const float (&lv)[N]) {
+  // Takes the scores of N blocks of value scales 2^lv, and their factors; a probability is then 2^(s factor - ref).
+  template <int N>
+  __device__ __forceinline__ void raise(f32x16 (&s)[N], float (&factor)[N], const float (&lv)[N], float &ref) {
+    float mb[N];
     bool over = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) over |= mb[i] - m > fminf(kSlack, u + kSlack - lv[i]);   // (NaN where nothing is seen yet)
-    if (__any(over)) lift<N>(mb, lv);
+    for (int i = 0; i < N; ++i) {
+      mb[i] = max16(s[i], -INFINITY) * factor[i];
+      over |= mb[i] - m > fminf(slack, u + kSlack - lv[i]);   // (NaN where nothing is seen yet)
+    }
+    ref = finite_ref(m);
+    if (__any(over)) {
+      const bool far = lift<N>(mb, lv);
+      ref = finite_ref(m);
+      if (far) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          far_scores(s[i], factor[i], ref);
+          factor[i] = 1.f;
+        }
+        ref = 0.f;
+      }
+    }
   }
-  template <int N> __device__ __forceinline__ void lift(const float (&mb)[N], const float (&lv)[N]) {
+  template <int N> __device__ __forceinline__ bool lift(const float (&mb)[N], const float (&lv)[N]) {
     float top[N], m_new = m;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -815,15 +840,15 @@ template <int ND> struct CodeRows : Rows<ND> {
       l *= __builtin_amdgcn_exp2f(m - mr);
       Rows<ND>::scale(__builtin_amdgcn_exp2f(kept - finite_ref(u_new)));
     }
-    Rows<ND>::set(m_new);
     u = u_new;
+    return Rows<ND>::set(m_new);
   }
-  // For the block of value scale 2^lv: a weight is 2^(score - m + c), w what its sum counts in l. Weights too far
-  // below the row's largest (2^-60, nothing in fp16) are kept from fp32's own limit, for l.
-  struct Ref { float m, c, w; };
-  __device__ __forceinline__ Ref ref(float lv) const {
+  // For the block of value scale 2^lv: a weight is a probability times 2^c, w what their sum counts in l. Weights too
+  // far below the row's largest (2^-60, nothing in fp16) are kept from fp32's own limit, for l.
+  struct Share { float c, w; };
+  __device__ __forceinline__ Share share(float lv) const {
     const float x = fminf(finite_ref(u) - lv, 60.f);
-    return Ref{finite_ref(m), kPOff - x, __builtin_amdgcn_exp2f(x)};
+    return Share{kPOff - x, __builtin_amdgcn_exp2f(x)};
   }
   // What O is still to be multiplied by, 2^u: here in part where that is far from 1.
   __device__ __forceinline__ float unit() {
@@ -858,37 +883,34 @@ __device__ __forceinline__ void match_waves(CodeRows<ND> &st, float *red, int wa
 
 // One row tile over n blocks, two at a time.
 //   scores(i, s): raw scores;  mask(i, s);  factor(i): what turns them into log2 units;  lv(i): log2 of the value
-//   scale;  probs(i, s): the weights' operand;  values(i, p): O += V^T P^T.
+//   scale;  probs(s, factor, ref, lv): the weights' operand;  values(i, p): O += V^T P^T.
 template <int ND, typename P, typename SC, typename MA, typename FA, typename LV, typename PR, typename VA>
 __device__ __forceinline__ void attend_blocks(CodeRows<ND> &st, int n, SC scores, MA mask, FA factor, LV lv, PR probs,
                                               VA values) {
   int i = 0;
+  float ref;
   for (; i + 2 <= n; i += 2) {
-    f32x16 s0, s1;
-    scores(i, s0);
-    scores(i + 1, s1);
-    mask(i, s0);
-    mask(i + 1, s1);
-    const float mb[2] = {max16(s0, -INFINITY) * factor(i), max16(s1, -INFINITY) * factor(i + 1)};
+    f32x16 s[2];
+    scores(i, s[0]);
+    scores(i + 1, s[1]);
+    mask(i, s[0]);
+    mask(i + 1, s[1]);
+    float f[2] = {factor(i), factor(i + 1)};
     const float at[2] = {lv(i), lv(i + 1)};
-    st.template raise<2>(mb, at);
-    if (st.far) {
-      far_scores(s0, factor(i), finite_ref(st.m));
-      far_scores(s1, factor(i + 1), finite_ref(st.m));
-    }
-    const P p0 = probs(i, s0);
+    st.raise(s, f, at, ref);
+    const P p0 = probs(s[0], f[0], ref, at[0]);
     values(i, p0);
-    const P p1 = probs(i + 1, s1);
+    const P p1 = probs(s[1], f[1], ref, at[1]);
     values(i + 1, p1);
   }
   if (i < n) {
-    f32x16 s0;
-    scores(i, s0);
-    mask(i, s0);
-    const float mb[1] = {max16(s0, -INFINITY) * factor(i)}, at[1] = {lv(i)};
-    st.template raise<1>(mb, at);
-    if (st.far) far_scores(s0, factor(i), finite_ref(st.m));
-    values(i, probs(i, s0));
+    f32x16 s[1];
+    scores(i, s[0]);
+    mask(i, s[0]);
+    float f[1] = {factor(i)};
+    const float at[1] = {lv(i)};
+    st.raise(s, f, at, ref);
+    values(i, probs(s[0], f[0], ref, at[0]));
   }
 }
 
@@ -977,16 +999,14 @@ __device__ __forceinline__ void kv8_scores(f32x16 &s, const QCodes<T, NK> &q, co
   }
 }
 
-// Weights of one block, 2^(ksc s - m + c), as fp16 (fp32 calls: two terms); their sum, times w, joins l. (st.far:
-// s has been through far_scores.)
+// Weights of one block, 2^(ksc s - ref + c), as fp16 (fp32 calls: two terms); their sum, times w, joins l.
 template <typename T> struct CodeProbs { f16x8 f[2], lo[sizeof(T) == 4 ? 2 : 1]; };
 template <typename T, int ND>
-__device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, float lv, CodeRows<ND> &st) {
-  const auto rf = st.ref(lv);
+__device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, float ref, float lv, CodeRows<ND> &st) {
+  const auto sh = st.share(lv);
   CodeProbs<T> o;
   float sum = 0.f;
-  const float c = st.far ? rf.c : rf.c - rf.m;
-  if (st.far) ksc = 1.f;
+  const float c = sh.c - ref;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float p = __builtin_amdgcn_exp2f(fmaf(s[i], ksc, c));
@@ -994,7 +1014,7 @@ __device__ __forceinline__ CodeProbs<T> code_probs(const f32x16 &s, float ksc, f
     o.f[i >> 3][i & 7] = (f16)p;
     if constexpr (sizeof(T) == 4) o.lo[i >> 3][i & 7] = (f16)(p - (float)o.f[i >> 3][i & 7]);
   }
-  st.l = fmaf(sum, rf.w, st.l);
+  st.l = fmaf(sum, sh.w, st.l);
   return o;
 }
 // O += V^T P^T; vf(n, f): value operand of d block n, keys 16 f ..
@@ -1197,28 +1217,27 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
       if (b + 4 < span.hi) load(id, nxt);
       id = id_at(b + 8);
       if (cur.ref.vs > 0.f) {
-        f32x16 s;
+        f32x16 s[1];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
           const bf16x8 kf = widen_bf16(cur.k[kk >> 1][2 * (kk & 1)], cur.k[kk >> 1][2 * (kk & 1) + 1]);
 #pragma unroll
-          for (int t = q.NQ - 1; t >= 0; --t) mfma32(s, kf, q.f[t][kk]);   // small terms first
+          for (int t = q.NQ - 1; t >= 0; --t) mfma32(s[0], kf, q.f[t][kk]);   // small terms first
         }
         const int left = seen.kv - b * 32;
         if (left < 32 || b * 32 + 32 > seen.tile_lo) {  // wave-uniform
-          mask_below(s, seen.row_hi - b * 32, lane);
+          mask_below(s[0], seen.row_hi - b * 32, lane);
           if (left < 32) {
 #pragma unroll
             for (int i = 0; i < NL; ++i) cur.v[i] = keep_tokens(cur.v[i], left, h);
           }
         }
-        const float ksc = key_factor(cur.ref.ks, a.sc);
-        const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur.ref.vs)};
-        st.template raise<1>(mb, lv);
-        if (st.far) far_scores(s, ksc, finite_ref(st.m));
-        code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, lv[0], st),
+        float ksc[1] = {key_factor(cur.ref.ks, a.sc)}, ref;
+        const float lv[1] = {scale_log(cur.ref.vs)};
+        st.raise(s, ksc, lv, ref);
+        code_values<T, ND, F::value>(st.o, code_probs<T>(s[0], ksc[0], ref, lv[0], st),
                                      [&](int n, int f) { return widen_f16(cur.v[n][2 * f], cur.v[n][2 * f + 1]); });
       }
       cur = nxt;
@@ -1318,14 +1337,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
         for (int u = 0; u < 2; ++u) {
           if (cur[u].vs > 0.f) {
             const u32x4 *fr = lds + u * 4 * NL * 64 + lane;
-            f32x16 s;
-            kv8_scores<T, NK>(s, q, fr);
-            if ((b + u) * 32 + 32 > seen.tile_lo) mask_below(s, seen.row_hi - (b + u) * 32, lane);
-            const float ksc = key_factor(cur[u].ks, a.sc);
-            const float mb[1] = {max16(s, -INFINITY) * ksc}, lv[1] = {scale_log(cur[u].vs)};
-            st.template raise<1>(mb, lv);
-            if (st.far) far_scores(s, ksc, finite_ref(st.m));
-            code_values<T, ND, F::value>(st.o, code_probs<T>(s, ksc, lv[0], st),
+            f32x16 s[1];
+            kv8_scores<T, NK>(s[0], q, fr);
+            if ((b + u) * 32 + 32 > seen.tile_lo) mask_below(s[0], seen.row_hi - (b + u) * 32, lane);
+            float ksc[1] = {key_factor(cur[u].ks, a.sc)}, ref;
+            const float lv[1] = {scale_log(cur[u].vs)};
+            st.raise(s, ksc, lv, ref);
+            code_values<T, ND, F::value>(st.o, code_probs<T>(s[0], ksc[0], ref, lv[0], st),
                                          [&](int n, int f) { return __builtin_bit_cast(f16x8, fr[(NK + 2 * n + f) * 64]); });
           }
         }
@@ -1454,7 +1472,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
             if (n < 32 || at + 32 > seen.tile_lo) mask_below(s, min(seen.row_hi - at, n), lane);
           },
           [&](int i) { return lane_of(ks, i); }, [&](int i) { return lane_of(lv, i); },
-          [&](int i, const f32x16 &s) { return code_probs<T>(s, lane_of(ks, i), lane_of(lv, i), st); },
+          [&](const f32x16 &s, float f, float ref, float at) { return code_probs<T>(s, f, ref, at, st); },
           [&](int i, const CodeProbs<T> &p) {
             const u32x4 *fr = codes + (i * NF + NK) * 64 + lane;
             code_values<T, ND, F::value>(st.o, p,
