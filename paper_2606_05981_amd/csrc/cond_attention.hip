@@ -299,11 +299,12 @@ __device__ __forceinline__ void store_part(const AttnCommon &a, Rows<ND> &st, fl
 //
 // k_cross: a workgroup of four waves serves 32 RW rows of one sequence and kv head; the other 4 / RW ways of
 // its waves split the keys of a tile (few rows: RW = 1). Key tiles go global -> registers -> LDS, the
-// next tile's loads in flight while one is computed (where the registers hold them: not fp32 tiles of
-// 128 keys of 128); rows past the end and masked value rows become zeros on the way.
-// Bound by latency: launch, sequence table, first loads, softmax, store, one after the other (16 x 1
-// tokens of 2 x 8 heads of 128 over 96: 7.5 us for 6.4 MB); fp32 by its matrix instructions, an eighth of
-// bf16's rate (12 x 918 rows of 8 heads over 3 to 287 keys: 59.6 us, 50 TFLOP/s).
+// next tile's loads issued before one is computed (where the registers hold them: not fp32 tiles of
+// 128 keys of 128); rows past the end and masked value rows become zeros as they arrive, so that the loads are
+// waited for before that computation, not after it, and with a mask its bytes before the rows.
+// Bound by latency: launch, sequence table, each tile's loads, softmax, store, one after the other (16 x 1
+// tokens of 2 x 8 heads of 128 over 96: 7.5 us for 6.4 MB); fp32 by the loads and the matrix instructions, a
+// ninth of bf16's rate, in turn (12 x 918 rows of 8 heads of 64 over 1610 keys in all: 46 us, 66 of 137 TFLOP/s).
 // LDS: keys as 16-byte chunks in the order of the MFMA operand ([32 keys][chunk c]:
 // lane = key), the key index xored with the chunk so that neither the row-wise
 // writes nor the operand reads meet in a bank; values as rows, chunks xored so that the
@@ -1173,8 +1174,8 @@ __device__ __forceinline__ Cut cut_of(const Kv8AttnArgs &a, int target, int at, 
 // Few rows (at most 32 a sequence, or chunk of one): bound by the codes that stream in. Each of the four waves
 // takes every fourth block of the split's range and loads its codes straight into MFMA operand
 // order, 16 bytes a lane and 1 KB a load, the next block's while one is computed. One token of 2 x 8 heads
-// of 128 over 131071: 59.5 us with the join, 4.5 TB/s; 32 over 96 to 8192: 56.3 us, 4.1 TB/s (parts of
-// equal tables instead of equal work: 115).
+// of 128 over 131071: 58.6 us with the join, 4.6 TB/s; 32 over 96 to 8192: 55.8 us, 4.1 TB/s (parts of
+// equal tables instead of equal work: 115); in fp32 queries, one wave a SIMD, 70 us.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(Kv8AttnArgs a, int target) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32;
@@ -1261,9 +1262,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_rows(K
 
 // Many rows: four waves of 32 rows; two blocks of codes a step are widened once per
 // workgroup on their way into LDS, in MFMA operand order (1 KB of lanes a fragment,
-// free of bank conflicts), the next step's codes in flight in registers. Bound by the matrix instructions
-// and the softmax between them, at one or two waves a SIMD (1000 of 2 x 8 heads of 128 over 1000,
-// causal, in four parts: 31.5 us, 130 TFLOP/s).
+// free of bank conflicts). The next step's codes are loaded into registers before a step is computed, but arrive
+// before its products: which block a wave loads goes by its number, so that the block references are kept in
+// scratch (80 bytes a lane), and what is read back from there waits for all loads before it. Bound by those
+// waits, at one to three waves a SIMD (1000 of 2 x 8 heads of 128 over 1000, causal, in four parts: 31.2 us,
+// 131 TFLOP/s; 512 over 4096, causal, 47 us, 342 TFLOP/s).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(Kv8AttnArgs a) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32;
@@ -1372,8 +1375,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
 
 // Many rows over a cache that fits LDS whole once widened. Lane j holds block j's scales and how many of
 // its tokens count (none: no such block). A wave takes several row tiles over codes widened once.
-// Bound by the matrix instructions and the softmax between them, and by the one pass of staging that a
-// workgroup waits for (16 x 1024 of 2 x 8 heads of 128 over 320: 61.5 us, 700 TFLOP/s, 2.4 TB/s).
+// 16 x 1024 of 2 x 8 heads of 128 over 320: 61 to 63 us, 690 TFLOP/s, 2.3 TB/s. Of that the matrix cores are busy 17,
+// vector instructions about 23 (4900 a wave, two waves a SIMD; an exponential takes four times as long); the rest
+// is the staging that a workgroup waits for, and the next rows' queries, issued ahead but waited for before a
+// tile's first product.
 template <typename T, int D, int NW, bool BOX>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void k_kv8_res(Kv8AttnArgs a, int chunk) {
   constexpr int ND = D / 32, NK = D / 16, NL = D / 32, NF = D / 8;
@@ -1951,7 +1956,7 @@ static Plan kv8_plan(const AttnProblem &p, int width, bool few) {
     pl.lds = (int)res + (pl.box ? pl.nw * room : 0);
     // Row tiles a wave takes one after the other: the keys are staged once for all of them. Whole
     // rounds of the workgroups that the chip holds, a staging at the cost of a tile (16 x 1024
-    // queries over 320 tokens: 4 tiles in one round 61.5 us, 2 in two rounds 67).
+    // queries over 320 tokens, us: 4 tiles in one round 61.5, 2 in two rounds 67).
     const int64_t slots = 256 * std::max(1, std::min(kLds / pl.lds, 4 * simd / pl.nw));
     int64_t best = INT64_MAX;
     int iters = 1;

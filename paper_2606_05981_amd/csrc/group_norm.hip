@@ -93,7 +93,9 @@ __device__ __forceinline__ float team_sum(float s, int lanes) {   // within a wa
 template <int V, int TH>
 __device__ __forceinline__ void group_sums(const GnArgs &a, const float (&v)[V], const Place &w, float *part, float *gs) {
   const int tid = threadIdx.x;
-  const int pitch = a.ppi | 1;                      // odd: columns in different banks
+  // odd: entries of neighbouring lanes in different banks, where a column is one entry (`same`); else they are V
+  // pitches apart and V of them meet in a bank (16 x 64 x 64 x 320: two thirds of k_gn_stats's LDS cycles)
+  const int pitch = a.ppi | 1;
   const int ng = a.gb;
   int per;                                          // entries of a group, in a run
   __syncthreads();                                  // part and gs are free
