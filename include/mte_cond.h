@@ -98,7 +98,8 @@ int64_t mte_cross_attention_workspace(const mte_attn_shape *shape, const int32_t
  *  k_codes uint8 [n_blocks][Hkv][d / 16][32 tokens][16]
  *  v_codes uint8 [n_blocks][Hkv][d][32], token 16 t + 8 a + 4 h + i (t, a, h < 2, i < 4)
  *          of the block at position 16 h + 8 t + 4 a + i
- *  scales  float [n_blocks][Hkv][2] (key, value)
+ *  scales  float [n_blocks][Hkv][2] (key, value); a program that fills blocks itself may use
+ *          any normal positive ones, but mte_kv8_append continues only blocks with powers of two
  * (the orders in which the matrix cores take them: a wave's 64 lanes load 1 KB
  * of consecutive codes at a time.) head_dim: 64 or 128.
  *

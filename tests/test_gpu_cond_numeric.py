@@ -289,3 +289,73 @@ def test_cross_more_heads_than_fp32_counts(torch, C):
         # the probabilities' and the result's rounding; fp32 on both sides: (d + 16) u each of the scores, |s| < 40
         assert bool(((out[i].float() - ref).abs() <= U16 * (mag + ref.abs()) * 1.01 + 4 * 40 * (d + 16) * U * mag).all())
     assert all(bool((w[:, -64:] == 7.0).all()) for w in wide)
+
+
+def _alike(torch, got, ref, mag, n, dtype):
+    """Equal weights: sums of n terms, their quotient, and the result's rounding."""
+    t = 2 * (n + 16) * U * mag + (U16 if dtype == "bf16" else U) * np.abs(ref)
+    assert (np.abs(_f64(got) - ref) <= t + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,hq,h,d", [(3, 96, 4, 2, 64), (2, 2500, 4, 2, 64), (2100, 96, 8, 8, 64), (2100, 130, 4, 2, 128)])
+def test_cross_scores_far_out_masked(torch, C, ql, kl, hq, h, d, dtype):
+    """The heaviest key masked: the others, of one score, weigh alike; and a sequence beside it that sees nothing."""
+    _say(f"cross, far scores, heaviest masked, {ql} x {kl} {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    v = _randn(torch, 129, kl, h, d, dtype=dtype)
+    for sign in (1, -1):
+        q, k, win = _far(torch, ql, kl, hq, h, d, sign, dt)
+        mask = torch.ones(2 * kl, dtype=torch.bool)
+        mask[win], mask[kl:] = False, False
+        got = C.cross_attention(torch.cat([q, q]), torch.cat([k, k]), torch.cat([v, v]), [ql, ql], [kl, kl],
+                                key_mask=mask.cuda(), scale=1.3)
+        vv = np.delete(_f64(v), win, 0).repeat(hq // h, 1)
+        _alike(torch, got[:ql], vv.mean(0)[None], np.abs(vv).mean(0)[None], kl, dtype)
+        assert not bool(got[ql:].any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,width,hq,h", CACHED)
+def test_kv8_scores_far_out_causal(torch, C, ql, kl, width, hq, h, dtype):
+    """Rows from the heaviest key on are its value, those before it the mean of what they see."""
+    _say(f"cached, far scores, causal, {ql} x {kl}, width {width}, {dtype}")
+    d, dt = 64, torch.bfloat16 if dtype == "bf16" else torch.float32
+    cache, table, kv, _, v = _fill(torch, C, [kl], h, d, width=width)
+    for sign in (1, -1):
+        q, k, _ = _far(torch, ql, kl, hq, h, d, sign, dt)
+        win, rest = kl - (ql + 1) // 2, k[:1].clone()
+        k[:] = rest
+        k[win] *= 2.0 if sign > 0 else 0.5
+        C.kv8_append(cache, table, kv, k.to(v.dtype), v, [kl])
+        got = C.kv8_attention(q, cache, table, kv, [ql], causal=True, scale=1.3)
+        (_, vv), = _held(torch, cache, table, [kl])
+        vv = vv.repeat(hq // h, 1)
+        for u in range(ql):
+            n = kl - ql + u + 1
+            if n > win:
+                assert np.array_equal(_f64(got[u]), _f64(torch.from_numpy(vv[win]).to(dt)))
+            else:
+                _alike(torch, got[u], vv[:n].mean(0), np.abs(vv[:n]).mean(0), n, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ql,kl,width,hq,h", CACHED)
+def test_kv8_scales_that_are_no_powers_of_two(torch, C, ql, kl, width, hq, h, dtype):
+    """A cache that another program filled, its scales between powers of two: attention takes them as they are. (The
+    logarithm of a value scale is within 2^-21 here, |log2| < 8: its weights move by less.)"""
+    _say(f"cached, scales of any value, {ql} x {kl}, width {width}, {dtype}")
+    d = 64
+    cache, table, kv, _, _ = _fill(torch, C, [kl], h, d, width=width, spread=False)
+    cache.scales.mul_(1 + torch.rand(cache.scales.shape, generator=torch.Generator().manual_seed(130)).cuda() * 0.99)
+    q = _randn(torch, 131, ql, hq, d, dtype=dtype)
+    got = _f64(C.kv8_attention(q, cache, table, kv, [ql]))
+    (kk, vv), = _held(torch, cache, table, [kl])
+    ref, mag, reach = O.attend(_f64(q), kk, vv, _sees(ql, kl, False), 1 / 8)
+    D = (d + 4) * U * reach[..., None] + 2 * U
+    t = 4 * D * mag + 2 * (kl + 16) * U * mag + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) * mag + 2.0 ** -21 * mag
+    t = t + kl * 2.0 ** -32 * 448 * float(cache.scales[..., 1].max())
+    t = t + (U16 if dtype == "bf16" else U) * (np.abs(ref) + t) + 1e-30
+    worst = float((np.abs(got - ref) / t).max())
+    _say(f"  worst error / bound {worst:.3f}")
+    assert worst <= 1.0
