@@ -108,7 +108,7 @@ int64_t mte_cross_attention_workspace(const mte_attn_shape *shape, const int32_t
  * kv_lens[i] (device int32, so that a captured step can be replayed as the
  * sequence grows). Blocks may appear in several rows (a shared prefix, one
  * frame's conditioning for all) as long as no call appends to a block that
- * another of its sequences appends to or reads. Device values are checked on the
+ * another of its sequences appends to or reads, or that the same row names twice. Device values are checked on the
  * device: a length below 0 counts as 0, one beyond 32 table_width as that (attention; append
  * and read: see there), and a block number outside [0, n_blocks) as a block whose
  * tokens are all masked (read: zeros; append: not written). table_width is at most
