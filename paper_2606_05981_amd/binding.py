@@ -1,4 +1,4 @@
-"""ctypes binding of libmte (include/mte.h, mte_vision.h, mte_cond.h): argument marshalling only.
+"""ctypes binding of libmte (include/mte.h, mte_vision.h, mte_cond.h, mte_proj.h): argument marshalling only.
 
 Every function keeps the C name and returns what the C call returns, except
 that a negative status raises MteError. Device buffers are passed as integer
@@ -24,6 +24,7 @@ STATUS = {0: "MTE_OK", -1: "MTE_E_INVALID", -2: "MTE_E_CAPACITY", -3: "MTE_E_HIP
           -4: "MTE_E_OOM", -5: "MTE_E_UNSUPPORTED"}
 MTE_ACT_NONE, MTE_ACT_SILU = 0, 1
 MTE_KV8_BLOCK = 32
+MTE_I8_CODES, MTE_I8_COLS = 2, 131071
 KERNEL_CLASSES = {"qkv_gemm": 0, "attention": 1, "o_gemm": 2, "gate_up_gemm": 3, "down_gemm": 4}
 
 
@@ -94,6 +95,14 @@ class mte_kv8(C.Structure):
                 ("n_blocks", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
 
 
+class mte_rotary_shape(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_k_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32),
+                ("dtype", C.c_int32), ("interleaved", C.c_int32), ("inverse", C.c_int32), ("n_axes", C.c_int32),
+                ("section", C.c_int32 * 4), ("factor", C.c_float),
+                ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+                ("qo_row", C.c_int64), ("qo_head", C.c_int64), ("ko_row", C.c_int64), ("ko_head", C.c_int64)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2606_05981_amd.build`")
 lib = C.CDLL(LIB_PATH)
@@ -137,6 +146,12 @@ _sig = {
     "mte_group_norm": (C.c_int, [_P, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P,
                                  C.c_float, C.c_int32, C.c_int32, _P, C.c_int64, C.c_int64, _P, C.c_int64, _P]),
     "mte_group_norm_workspace": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "mte_i8_pitch": (C.c_int64, [C.c_int32]),
+    "mte_i8_quantize_rows": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
+    "mte_i8_linear": (C.c_int, [_P, C.c_int64, _P, C.c_int32, C.c_int32, C.c_int32, _P, _P, C.c_int32, _P, C.c_int32, _P,
+                                C.c_int64, C.c_int32, _P, C.c_int64, _P]),
+    "mte_i8_linear_workspace": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "mte_rotary": (C.c_int, [_P, _P, _P, _P, C.c_int64, _P, C.c_int32, _P, _P, _P]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(lib, _name)
@@ -363,3 +378,33 @@ def mte_group_norm(x: int, x_row: int, x_image: int, n: int, pixels: int, channe
                    y_image: int, workspace: Optional[int], workspace_bytes: int, stream: int) -> int:
     return _check(lib.mte_group_norm(x, x_row, x_image, n, pixels, channels, groups, gamma, beta, eps, act, dtype, y,
                                      y_row, y_image, workspace, workspace_bytes, stream), "mte_group_norm")
+
+
+# mte_proj.h; ROTARY_SHAPE: mte_rotary_shape as bytes.
+ROTARY_SHAPE = struct.Struct("@8i4if4x8q")
+assert ROTARY_SHAPE.size == C.sizeof(mte_rotary_shape)
+
+
+def mte_i8_pitch(cols: int) -> int:
+    return _check(lib.mte_i8_pitch(cols), "mte_i8_pitch")
+
+
+def mte_i8_quantize_rows(x: int, x_row: int, rows: int, cols: int, dtype: int, codes: int, scales: int,
+                         stream: int) -> int:
+    return _check(lib.mte_i8_quantize_rows(x, x_row, rows, cols, dtype, codes, scales, stream), "mte_i8_quantize_rows")
+
+
+def mte_i8_linear_workspace(x_type: int, m: int, k: int, n: int) -> int:
+    return _check(lib.mte_i8_linear_workspace(x_type, m, k, n), "mte_i8_linear_workspace")
+
+
+def mte_i8_linear(x: int, x_row: int, x_scales: Optional[int], x_type: int, m: int, k: int, w: int, w_scales: int, n: int,
+                  bias: Optional[int], act: int, out: int, out_row: int, dtype: int, workspace: Optional[int],
+                  workspace_bytes: int, stream: int) -> int:
+    return _check(lib.mte_i8_linear(x, x_row, x_scales, x_type, m, k, w, w_scales, n, bias, act, out, out_row, dtype,
+                                    workspace, workspace_bytes, stream), "mte_i8_linear")
+
+
+def mte_rotary(shape, q: int, k: Optional[int], positions: int, axis_stride: int, freq: int, tokens: int, q_out: int,
+               k_out: Optional[int], stream: int) -> int:
+    return _check(lib.mte_rotary(shape, q, k, positions, axis_stride, freq, tokens, q_out, k_out, stream), "mte_rotary")

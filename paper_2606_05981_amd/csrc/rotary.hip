@@ -1,0 +1,136 @@
+// Rotary positions on queries and keys, one launch for both.
+//
+//   y1 = f (x1 cos a - x2 sin a), y2 = f (x2 cos a + x1 sin a), a = p freq[i] for pair i
+//
+// Bound by bytes: every channel is read and written once, 3 operations each. A workgroup takes some
+// tokens: first the sines and cosines of their pairs (fp64 angle, reduced by whole turns in fp64:
+// at position 2^30 an fp32 angle is off by up to 32 radians), which all heads share, into LDS; then
+// the heads, V channels of either member of V pairs a thread (interleaved: 2 V channels in a row).
+#include "common.h"
+#include "proj_launch.h"
+
+namespace mte {
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kTableMax = 2048;      // (sin, cos) pairs of a workgroup's tokens in LDS: 16 KB
+
+template <typename T, int V> struct Vec { typedef T type __attribute__((ext_vector_type(V))); };
+template <typename T> struct Vec<T, 1> { typedef T type __attribute__((ext_vector_type(1))); };
+
+// V consecutive channels at p (aligned to V elements, 16 bytes at most).
+template <typename T, int V> __device__ __forceinline__ void load(float (&x)[V], const T *p) {
+  typedef typename Vec<T, V>::type vec;
+  const vec v = *(const vec *)p;
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = to_f32((T)v[i]);
+}
+template <typename T, int V> __device__ __forceinline__ void store(T *p, const float (&x)[V]) {
+  typedef typename Vec<T, V>::type vec;
+  vec v;
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = from_f32<T>(x[i]);
+  *(vec *)p = v;
+}
+
+// V: channels of a load. tb: tokens of a workgroup.
+template <typename T, int V, bool INTER>
+__global__ __launch_bounds__(kRotThreads) void k_rotary(RotaryArgs a, int tb) {
+  __shared__ float2 turn[kTableMax];
+  const int tid = threadIdx.x, pairs = a.rot >> 1;
+  const int t0 = blockIdx.x * tb, nt = min(tb, a.tokens - t0);
+  for (int i = tid; i < nt * pairs; i += kRotThreads) {
+    const int t = i / pairs, p = i - t * pairs;
+    const int axis = (p >= a.end[0]) + (p >= a.end[1]) + (p >= a.end[2]);
+    const double w = (double)a.pos[axis * a.axis_stride + t0 + t] * a.freq[p];
+    // whole turns taken off: 2 pi as the sum of two doubles, so that the rest is exact to 2^-53 of itself or so
+    const double n = rint(w * 0.15915494309189535);
+    const double r = fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, w));
+    float s, c;
+    sincosf((float)r, &s, &c);
+    turn[i] = float2{s * a.sign, c};
+  }
+  __syncthreads();
+  // units of a head: of the rotated channels, then of the rest where that is copied
+  constexpr int W = INTER ? V : 2 * V;                 // channels of a rotating unit
+  const int heads = a.hq + a.hk, spin = a.rot / W, rest = a.q_tail | a.k_tail ? (a.d - a.rot) / V : 0, units = spin + rest;
+  const int per = heads * units;
+  for (int i = tid; i < nt * per; i += kRotThreads) {
+    const int t = i / per, x = i - t * per, hh = x / units, u = x - hh * units;
+    const bool isk = hh >= a.hq;
+    const int h = isk ? hh - a.hq : hh;
+    const T *in = isk ? (const T *)a.k + (t0 + t) * a.k_row + h * a.k_head : (const T *)a.q + (t0 + t) * a.q_row + h * a.q_head;
+    T *out = isk ? (T *)a.ko + (t0 + t) * a.ko_row + h * a.ko_head : (T *)a.qo + (t0 + t) * a.qo_row + h * a.qo_head;
+    if (u >= spin) {
+      if (isk ? a.k_tail : a.q_tail) {
+        typedef typename Vec<T, V>::type vec;
+        const int c = a.rot + (u - spin) * V;
+        *(vec *)(out + c) = *(const vec *)(in + c);
+      }
+      continue;
+    }
+    const float2 *tr = turn + t * pairs;
+    if constexpr (INTER) {
+      float y[V];
+      load<T, V>(y, in + u * V);
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        const float2 sc = tr[u * (V / 2) + e / 2];
+        const float x1 = y[e], x2 = y[e + 1];
+        y[e] = a.factor * (x1 * sc.y - x2 * sc.x);
+        y[e + 1] = a.factor * (x2 * sc.y + x1 * sc.x);
+      }
+      store<T, V>(out + u * V, y);
+    } else {
+      float y1[V], y2[V];
+      load<T, V>(y1, in + u * V);
+      load<T, V>(y2, in + pairs + u * V);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float2 sc = tr[u * V + e];
+        const float x1 = y1[e], x2 = y2[e];
+        y1[e] = a.factor * (x1 * sc.y - x2 * sc.x);
+        y2[e] = a.factor * (x2 * sc.y + x1 * sc.x);
+      }
+      store<T, V>(out + u * V, y1);
+      store<T, V>(out + pairs + u * V, y2);
+    }
+  }
+}
+
+template <typename T, int V>
+hipError_t run(const RotaryArgs &a, int tb, hipStream_t s) {
+  const dim3 grid((a.tokens + tb - 1) / tb);
+  if (a.inter) {
+    if constexpr (V > 1) hipLaunchKernelGGL((k_rotary<T, V, true>), grid, dim3(kRotThreads), 0, s, a, tb);
+  } else {
+    hipLaunchKernelGGL((k_rotary<T, V, false>), grid, dim3(kRotThreads), 0, s, a, tb);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs &a, int dtype, hipStream_t s) {
+  // the widest load that the members of a pair allow: strides and bases are multiples of 8 channels
+  const int apart = a.inter ? a.rot : a.rot / 2, most = dtype == MTE_BF16 ? 8 : 4;
+  int v = a.inter ? 2 : 1;
+  while (v < most && apart % (2 * v) == 0) v *= 2;
+  const int units = (a.hq + a.hk) * ((a.inter ? a.rot / v : a.rot / 2 / v) + (a.q_tail | a.k_tail ? (a.d - a.rot) / v : 0));
+  // tokens of a workgroup: about four units a thread, 512 workgroups at least
+  int tb = (4 * kRotThreads + units - 1) / units;
+  tb = tb < a.tokens / 512 ? tb : a.tokens / 512;
+  tb = tb < kTableMax / (a.rot / 2) ? tb : kTableMax / (a.rot / 2);
+  tb = tb < 1 ? 1 : tb;
+  if (dtype == MTE_BF16) {
+    if (v == 8) return run<bf16, 8>(a, tb, s);
+    if (v == 4) return run<bf16, 4>(a, tb, s);
+    if (v == 2) return run<bf16, 2>(a, tb, s);
+    return run<bf16, 1>(a, tb, s);
+  }
+  if (v == 4) return run<float, 4>(a, tb, s);
+  if (v == 2) return run<float, 2>(a, tb, s);
+  return run<float, 1>(a, tb, s);
+}
+
+}  // namespace mte
