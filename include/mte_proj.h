@@ -4,11 +4,14 @@
  *
  * The encoder (mte.h) ends at its hidden states, and the attentions of mte_cond.h
  * begin at queries, keys and values. Between the two lie the denoiser's projections
- * and, where its heads have one, a rotary embedding:
+ * and, where its heads have one, a rotary embedding; and where all streams of a batch
+ * share a long context (an instruction, a history; Sec. III-B's one encode for every frame of a
+ * batch) beside each one's own tokens, an attention that reads the shared part once:
  *
  *   mte_i8_quantize_rows   rows as 8-bit integers with a scale each
  *   mte_i8_linear          their product with an 8-bit weight, bias and activation
  *   mte_rotary             rotary positions on queries and keys
+ *   mte_prefix_attention   keys shared by all sequences, then each one's own
  *
  * Conventions as in mte_cond.h: device / host pointers, negative mte_status codes,
  * host-side checks before any HIP call, every call only enqueues work on `stream`
@@ -95,6 +98,25 @@ typedef struct {
  * MTE_E_HIP. tokens == 0 is MTE_OK. */
 int mte_rotary(const mte_rotary_shape *shape, const void *q, const void *k, const int32_t *positions,
                int64_t axis_stride, const double *freq, int32_t tokens, void *q_out, void *k_out, hipStream_t stream);
+
+/* Attention of packed sequences that share a prefix: sequence i's q_lens[i] queries attend to the
+ * prefix_len tokens that all of them share and then to its own kv_lens[i] tokens, in one softmax.
+ * causal = 1: query u sees own tokens 0 .. kv_lens[i] - q_lens[i] + u only (the whole prefix in any
+ * case). A query that sees nothing gets zeros. What tokens that a query does not see hold (infinities,
+ * NaN) does not reach it.
+ *  shape:      heads, types and strides as in mte_cross_attention (k_*, v_*: of the own tokens).
+ *  prefix_k/v: device, prefix_len rows at the strides pk_row, pk_head, pv_row, pv_head.
+ *  k, v:       device, sum(kv_lens) rows back to back; q, out, workspace as in mte_cross_attention.
+ *  q_lens, kv_lens: HOST int32[n], each >= 0; n >= 1.
+ * Few rows a sequence: the rows of all sequences are read as one tile over the prefix, which is
+ * read once for all of them; many: a tile reads the prefix and its sequence's tokens in one pass.
+ * Other sequences may change the last bits of a result. Errors and limits as in mte_cross_attention. */
+int mte_prefix_attention(const mte_attn_shape *shape, const void *q, const void *prefix_k, const void *prefix_v,
+                         int64_t pk_row, int64_t pk_head, int64_t pv_row, int64_t pv_head, int32_t prefix_len,
+                         const void *k, const void *v, const int32_t *q_lens, const int32_t *kv_lens, int32_t n,
+                         int32_t causal, void *out, void *workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t mte_prefix_attention_workspace(const mte_attn_shape *shape, int32_t prefix_len, const int32_t *q_lens,
+                                       const int32_t *kv_lens, int32_t n);
 
 #ifdef __cplusplus
 }

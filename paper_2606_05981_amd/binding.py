@@ -151,6 +151,9 @@ _sig = {
     "mte_i8_linear": (C.c_int, [_P, C.c_int64, _P, C.c_int32, C.c_int32, C.c_int32, _P, _P, C.c_int32, _P, C.c_int32, _P,
                                 C.c_int64, C.c_int32, _P, C.c_int64, _P]),
     "mte_i8_linear_workspace": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "mte_prefix_attention": (C.c_int, [_P, _P, _P, _P, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, _P, _P, _P, _P,
+                                       C.c_int32, C.c_int32, _P, _P, C.c_int64, _P]),
+    "mte_prefix_attention_workspace": (C.c_int64, [_P, C.c_int32, _P, _P, C.c_int32]),
     "mte_rotary": (C.c_int, [_P, _P, _P, _P, C.c_int64, _P, C.c_int32, _P, _P, _P]),
 }
 for _name, (_res, _args) in _sig.items():
@@ -408,3 +411,17 @@ def mte_i8_linear(x: int, x_row: int, x_scales: Optional[int], x_type: int, m: i
 def mte_rotary(shape, q: int, k: Optional[int], positions: int, axis_stride: int, freq: int, tokens: int, q_out: int,
                k_out: Optional[int], stream: int) -> int:
     return _check(lib.mte_rotary(shape, q, k, positions, axis_stride, freq, tokens, q_out, k_out, stream), "mte_rotary")
+
+
+def mte_prefix_attention_workspace(shape, prefix_len: int, q_lens, kv_lens, n: int) -> int:
+    return _check(lib.mte_prefix_attention_workspace(shape, prefix_len, q_lens, kv_lens, n),
+                  "mte_prefix_attention_workspace")
+
+
+def mte_prefix_attention(shape, q: int, prefix_k: Optional[int], prefix_v: Optional[int], pk_row: int, pk_head: int,
+                         pv_row: int, pv_head: int, prefix_len: int, k: Optional[int], v: Optional[int], q_lens, kv_lens,
+                         n: int, causal: int, out: int, workspace: Optional[int], workspace_bytes: int,
+                         stream: int) -> int:
+    return _check(lib.mte_prefix_attention(shape, q, prefix_k, prefix_v, pk_row, pk_head, pv_row, pv_head, prefix_len, k, v,
+                                           q_lens, kv_lens, n, causal, out, workspace, workspace_bytes, stream),
+                  "mte_prefix_attention")

@@ -21,7 +21,7 @@ PROBE_OUT = os.path.join(HERE, "libmte_probe.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["gemm.hip", "gemm_f8.hip", "attention.hip", "norm_rope.hip", "vision_kernels.hip",
            "cond_attention.hip", "kv8.hip", "group_norm.hip",
-           "rotary.hip", "i8_quantize.hip", "i8_linear.hip", "api.cpp", "vision.cpp", "cond.cpp", "proj.cpp"]
+           "prefix_attention.hip", "rotary.hip", "i8_quantize.hip", "i8_linear.hip", "api.cpp", "vision.cpp", "cond.cpp", "proj.cpp"]
 PROBE_SOURCES = ["probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,5 +1,6 @@
-"""Torch-facing wrappers of include/mte_cond.h: the operators with which a denoiser's layers
-read the encoder's conditioning (cross attention, an 8-bit key/value cache, group norm).
+"""Torch-facing wrappers of include/mte_cond.h, and of mte_proj.h's attention: the operators with which a
+denoiser's layers read the encoder's conditioning (cross attention, also over a prefix that all
+sequences share, an 8-bit key/value cache, group norm).
 
 Tensors in, tensors out, as in ``encoder``: PyTorch provides memory and streams, every step
 runs in libmte's HIP kernels, nothing falls back. Forward only: results carry no gradient, also where
@@ -154,6 +155,50 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: S
                     ql, n_q, kl, n_kv, idx, o.data_ptr(), ws, n, st))
         return o
     return _on(dev, stream, (q, k, v, key_mask, out), call)
+
+
+def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                     q_lens: Sequence[int], kv_lens: Sequence[int], causal: bool = True, scale: Optional[float] = None,
+                     out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """mte_prefix_attention: packed queries q [Tq, Hq, d] attend to the tokens that all sequences share,
+    prefix_k, prefix_v [P, Hkv, d], and to their own, k, v [Tk, Hkv, d] -> [Tq, Hq, d].
+
+    q_lens / kv_lens: query rows and own tokens of each sequence (0 allowed); causal: query u of q_lens[i] sees
+    own tokens up to kv_lens[i] - q_lens[i] + u (all of the prefix in any case); scale: default
+    1 / sqrt(d). A query that sees no token gets zeros. All but out (which may be q) may be strided over tokens and
+    heads. Streams of single queries over a long prefix read it once between them."""
+    hq, d, dtype, dev = _query(q)
+    hkv = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
+    sq = _rows("q", q, dtype, hq, d, dev)
+    sk, sv = _rows("k", k, dtype, hkv, d, dev), _rows("v", v, dtype, hkv, d, dev)
+    spk, spv = _rows("prefix_k", prefix_k, dtype, hkv, d, dev), _rows("prefix_v", prefix_v, dtype, hkv, d, dev)
+    p_len = prefix_k.shape[0]
+    if v.shape[0] != k.shape[0]:
+        raise ValueError(f"v: expected {k.shape[0]} rows, got {v.shape[0]}")
+    if prefix_v.shape[0] != p_len:
+        raise ValueError(f"prefix_v: expected {p_len} rows, got {prefix_v.shape[0]}")
+    q_keep, ql, n = _lens("q_lens", q_lens, q.shape[0])
+    kv_keep, kl, n_kv = _lens("kv_lens", kv_lens, k.shape[0])
+    if n_kv != n:
+        raise ValueError(f"kv_lens: expected {n} lengths, got {n_kv}")
+    if p_len >= 1 << 31:
+        raise ValueError(f"prefix_k: expected fewer than 2^31 rows, got {p_len}")
+    so = None
+    if out is not None:
+        so = _rows("out", out, dtype, hq, d, dev)
+        _out_rows(out, q, so)
+    sc = 1.0 / math.sqrt(d) if scale is None else float(scale)
+
+    def call(st):
+        o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
+        shape = B.ATTN_SHAPE.pack(hq, hkv, d, _DTYPE[dtype], sc, *sq, *sk, *sv, *((hq * d, d) if so is None else so))
+        _spaced(dev, "mte_prefix_attention", p_len >= 1024,
+                lambda: B.mte_prefix_attention_workspace(shape, p_len, ql, kl, n),
+                lambda ws, nb: B.lib.mte_prefix_attention(
+                    shape, q.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(), *spk, *spv, p_len, k.data_ptr(),
+                    v.data_ptr(), ql, kl, n, 1 if causal else 0, o.data_ptr(), ws, nb, st))
+        return o
+    return _on(dev, stream, (q, prefix_k, prefix_v, k, v, out), call)
 
 
 class KV8Cache(NamedTuple):

@@ -6,26 +6,38 @@
 #include <cstdint>
 
 #include "../../include/mte_proj.h"
+#include "cond_checks.h"
 #include "proj_launch.h"
 
 using namespace mte;
 
 namespace {
 
-constexpr int64_t kMaxRows = 0x7FFFFFFF - 4096;      // a last tile's end stays inside 31 bits
-constexpr int64_t kMaxStride = (int64_t)1 << 40;     // row * stride stays inside 64 bits
 constexpr int32_t kMaxHeads = 65535;
 
 bool aligned(const void *p, uintptr_t n) { return (uintptr_t)p % n == 0; }
 bool type_ok(int32_t t) { return t == MTE_F32 || t == MTE_BF16; }
 uintptr_t size_of(int32_t t) { return t == MTE_BF16 ? 2 : 4; }
-bool stride_ok(int64_t s) { return s >= 0 && s <= kMaxStride && s % 8 == 0; }
 int hip(hipError_t e) { return e == hipSuccess ? MTE_OK : MTE_E_HIP; }
 
 int linear_status(int32_t x_type, int32_t m, int32_t k, int32_t n) {
   if (x_type != MTE_I8_CODES && !type_ok(x_type)) return MTE_E_INVALID;
   if (m < 0 || m > kMaxRows || n <= 0 || n > kMaxRows || k <= 0 || k > MTE_I8_COLS) return MTE_E_INVALID;
   return MTE_OK;
+}
+
+// MTE_OK or an error for everything of a prefix attention but its buffers and the prefix's strides.
+int prefix_status(const mte_attn_shape *s, int32_t prefix_len, const int32_t *q_lens, const int32_t *kv_lens, int32_t n,
+                  int64_t *q_rows, int64_t *kv_rows) {
+  const int st = shape_status(s, rows_dim);
+  if (st != MTE_OK) return st;
+  if (!stride_ok(s->k_row) || !stride_ok(s->k_head) || !stride_ok(s->v_row) || !stride_ok(s->v_head))
+    return MTE_E_INVALID;
+  *q_rows = query_rows(*s, q_lens, n);
+  if (*q_rows < 0) return (int)*q_rows;
+  if (!kv_lens || prefix_len < 0) return MTE_E_INVALID;
+  *kv_rows = total(kv_lens, n);
+  return *kv_rows < 0 || *kv_rows + prefix_len > kMaxRows ? MTE_E_INVALID : MTE_OK;
 }
 
 }  // namespace
@@ -145,6 +157,39 @@ int mte_rotary(const mte_rotary_shape *s, const void *q, const void *k, const in
   a.q_tail = q != q_out && s->rot_dim < s->head_dim;
   a.k_tail = s->n_k_heads > 0 && k != k_out && s->rot_dim < s->head_dim;
   return hip(launch_rotary(a, s->dtype, stream));
+}
+
+int64_t mte_prefix_attention_workspace(const mte_attn_shape *shape, int32_t prefix_len, const int32_t *q_lens,
+                                       const int32_t *kv_lens, int32_t n) {
+  int64_t nq, nk;
+  const int st = prefix_status(shape, prefix_len, q_lens, kv_lens, n, &nq, &nk);
+  return st != MTE_OK ? (int64_t)st : prefix_workspace(problem(*shape, q_lens, n), prefix_len, kv_lens);
+}
+
+int mte_prefix_attention(const mte_attn_shape *shape, const void *q, const void *prefix_k, const void *prefix_v,
+                         int64_t pk_row, int64_t pk_head, int64_t pv_row, int64_t pv_head, int32_t prefix_len,
+                         const void *k, const void *v, const int32_t *q_lens, const int32_t *kv_lens, int32_t n,
+                         int32_t causal, void *out, void *workspace, int64_t workspace_bytes, hipStream_t stream) {
+  int64_t nq, nk;
+  const int st = prefix_status(shape, prefix_len, q_lens, kv_lens, n, &nq, &nk);
+  if (st != MTE_OK) return st;
+  if (causal != 0 && causal != 1) return MTE_E_INVALID;
+  if (!stride_ok(pk_row) || !stride_ok(pk_head) || !stride_ok(pv_row) || !stride_ok(pv_head)) return MTE_E_INVALID;
+  if (nq == 0) return MTE_OK;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return MTE_E_INVALID;
+  if (prefix_len > 0 && (!prefix_k || !prefix_v || !aligned16(prefix_k) || !aligned16(prefix_v))) return MTE_E_INVALID;
+  if (nk > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return MTE_E_INVALID;
+  AttnProblem p = problem(*shape, q_lens, n);
+  p.near_rows = p.near_rows && pk_row < (1 << 24) && pv_row < (1 << 24);
+  const int64_t need = prefix_workspace(p, prefix_len, kv_lens);
+  if (workspace_bytes < need) return MTE_E_CAPACITY;
+  if (need > 0 && (!workspace || !aligned16(workspace))) return MTE_E_INVALID;
+  p.c.q = q;
+  p.c.out = out;
+  p.c.ws = (float *)workspace;
+  const PrefixRows x{prefix_k, prefix_v, k, v, pk_row, pk_head, pv_row, pv_head,
+                     shape->k_row, shape->k_head, shape->v_row, shape->v_head, prefix_len};
+  return hip(launch_prefix(p, x, kv_lens, causal, stream));
 }
 
 }  // extern "C"

@@ -47,4 +47,13 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(const RotaryArgs &a, int dtype, hipStream_t s);
 
+struct PrefixRows {
+  const void *pk, *pv, *k, *v;
+  int64_t pk_row, pk_head, pv_row, pv_head, k_row, k_head, v_row, v_head;
+  int p_len;
+};
+// p.near_rows: of all four sources.
+int64_t prefix_workspace(const AttnProblem &p, int p_len, const int32_t *kv_lens);
+hipError_t launch_prefix(const AttnProblem &p, const PrefixRows &x, const int32_t *kv_lens, int causal, hipStream_t s);
+
 }  // namespace mte

@@ -23,7 +23,8 @@ def test_header_and_library_agree(B):
     src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "mte_proj.h")).read(), flags=re.S)
     names = set(re.findall(r"^\s*(?:int|int64_t)\s+(mte_[a-z0-9_]+)\s*\(", src, flags=re.M))
     assert names == set(n for n in B._sig if n.startswith(("mte_i8_", "mte_rotary", "mte_prefix_")))
-    assert {"mte_i8_pitch", "mte_i8_quantize_rows", "mte_i8_linear", "mte_i8_linear_workspace", "mte_rotary"} <= names
+    assert names == {"mte_i8_pitch", "mte_i8_quantize_rows", "mte_i8_linear", "mte_i8_linear_workspace", "mte_rotary",
+                     "mte_prefix_attention", "mte_prefix_attention_workspace"}
     lib = ctypes.CDLL(B.LIB_PATH)
     assert not [n for n in names if not hasattr(lib, n)]
     assert ctypes.sizeof(B.mte_rotary_shape) == 120
@@ -107,6 +108,48 @@ def test_rotary(B, kw, status):
     assert _rot(B, **kw) == status
 
 
+def _pre(B, shape=None, q=P, pk=P, pv=P, ps=(1024, 128, 1024, 128), p_len=96, k=P, v=P, ql=(4, 5), kl=(7, 9), n=None,
+         causal=1, out=P, ws=P, nbytes=1 << 40, hq=16, hkv=8, d=128, dtype=1, scale=0.1, **kw):
+    s = B.make_attn_shape(hq, hkv, d, dtype, scale, q=(hq * d, d), k=(hkv * d, d), v=(hkv * d, d), out=(hq * d, d))
+    for name, value in kw.items():
+        setattr(s, name, value)
+    return B.lib.mte_prefix_attention(
+        None if shape is False else ctypes.byref(s), q, pk, pv, *ps, p_len, k, v, None if ql is None else B._i32(ql),
+        None if kl is None else B._i32(kl), len(ql or ()) if n is None else n, causal, out, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(shape=False), INVALID), (dict(q=None), INVALID), (dict(pk=None), INVALID), (dict(pv=None), INVALID),
+    (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(out=None), INVALID), (dict(ql=None), INVALID),
+    (dict(kl=None), INVALID), (dict(n=0), INVALID), (dict(n=-1), INVALID), (dict(ql=(4, -1)), INVALID),
+    (dict(kl=(-7, 9)), INVALID), (dict(p_len=-1), INVALID), (dict(causal=2), INVALID), (dict(causal=-1), INVALID),
+    (dict(hq=10, hkv=4), INVALID), (dict(hq=0), INVALID), (dict(hkv=-1), INVALID), (dict(d=0), INVALID),
+    (dict(dtype=2), INVALID), (dict(scale=0.0), INVALID), (dict(scale=NAN), INVALID), (dict(scale=2.4e38), INVALID),
+    (dict(q_row=2044), INVALID), (dict(k_head=-128), INVALID), (dict(v_row=1 << 41), INVALID), (dict(o_head=4), INVALID),
+    (dict(ps=(1020, 128, 1024, 128)), INVALID), (dict(ps=(1024, -8, 1024, 128)), INVALID),
+    (dict(ps=(1024, 128, 1 << 41, 128)), INVALID), (dict(ps=(1024, 128, 1024, 4)), INVALID),
+    (dict(q=P + 8), INVALID), (dict(pk=P + 2), INVALID), (dict(pv=P + 8), INVALID), (dict(k=P + 2), INVALID),
+    (dict(v=P + 4), INVALID), (dict(out=P + 1), INVALID), (dict(ql=(2**31 - 1, 0)), INVALID),
+    (dict(kl=(2**31 - 1, 1)), INVALID), (dict(kl=(TOP - 90, 0)), INVALID),            # with the prefix past 31 bits
+    (dict(d=136), UNSUPPORTED), (dict(d=20), UNSUPPORTED),
+    (dict(ql=(1, 1), kl=(1, 1), p_len=16384, nbytes=16), CAPACITY),
+    (dict(ql=(1, 1), kl=(1, 1), p_len=16384, ws=None), INVALID), (dict(ql=(1, 1), kl=(1, 1), p_len=16384, ws=P + 4), INVALID),
+    (dict(ql=(0, 0), q=None, out=None, ws=None, nbytes=0), 0), (dict(ql=(0, 0), causal=3), INVALID),
+])
+def test_prefix_attention(B, kw, status):
+    assert _pre(B, **kw) == status
+
+
+def test_prefix_workspace(B):
+    s = B.make_attn_shape(16, 8, 128, 1, 0.1, q=(2048, 128), k=(1024, 128), v=(1024, 128), out=(2048, 128))
+    w = lambda p, ql, kl, sh=s: B.lib.mte_prefix_attention_workspace(ctypes.byref(sh), p, B._i32(ql), B._i32(kl), len(ql))
+    assert w(96, (4096,) * 16, (96,) * 16) == 0 and w(96, (0, 0), (4, 5)) == 0
+    assert w(16384, (1,) * 64, (96,) * 64) > 0 and w(0, (1,), (9000,)) > 0
+    assert w(-1, (1,), (1,)) == INVALID and w(96, (-1,), (1,)) == INVALID and w(96, (1,), (-1,)) == INVALID
+    s.head_dim = 136
+    assert w(96, (1,), (1,)) == UNSUPPORTED
+
+
 def test_binding_raises(B):
     with pytest.raises(B.MteError) as e:
         B.mte_i8_linear(P, 320, None, 1, 4, 320, P, P, 640, None, 9, P, 640, 1, P, 1 << 40, 0)
@@ -121,12 +164,14 @@ def test_binding_raises(B):
 
 def test_wrappers_take_gpu_tensors_only(B):
     import torch
+    from paper_2606_05981_amd import conditioning as C
     from paper_2606_05981_amd import projections as J
     x = torch.zeros(4, 64)
     w = J.I8Rows(torch.zeros((8, 128), dtype=torch.int8), torch.ones(8), 64)
     for call in (lambda: J.quantize_rows(x), lambda: J.i8_linear(x, w), lambda: J.i8_linear(w, w),
                  lambda: J.rotary(torch.zeros(4, 2, 64), torch.zeros(4, dtype=torch.int32), torch.ones(32, dtype=torch.float64)),
-                 lambda: J.i8_linear(x, w, act="gelu")):
+                 lambda: J.i8_linear(x, w, act="gelu"),
+                 lambda: C.prefix_attention(*[torch.zeros(4, 2, 64)] * 5, [4], [4])):
         with pytest.raises(ValueError):
             call()
 
