@@ -16,7 +16,7 @@ def i8_rows(x):
     x = np.asarray(x, np.float64)
     bad = ~np.isfinite(x).all(1)
     top = np.abs(np.where(bad[:, None], 0.0, x)).max(1).astype(np.float32)
-    s = np.maximum(top / np.float32(127), np.float32(2.0 ** -126))
+    s = np.maximum(top * (np.float32(1) / np.float32(127)), np.float32(2.0 ** -126))
     codes = np.rint(np.where(bad[:, None], 0.0, x) / s.astype(np.float64)[:, None])   # ties to even
     return codes, np.where(bad, np.float32(np.nan), s)
 

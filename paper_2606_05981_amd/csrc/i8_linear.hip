@@ -4,7 +4,9 @@
 // rate of 16-bit floating point for the same bytes of operands. Codes are rows of a multiple of
 // 128 bytes, so that a K stage is 128 bytes of every row and there is no ragged end of K.
 // C^T = B A^T: a lane then holds four consecutive columns of one row of the result.
-#include "common.h"
+#include <cmath>
+
+#include "gemm_kernel.h"
 #include "proj_launch.h"
 
 namespace mte {
@@ -82,6 +84,245 @@ template <typename TO, bool ACT> hipError_t run_few(const I8Args &g, hipStream_t
   return hipGetLastError();
 }
 
+// ---- many rows ----------------------------------------------------------------------------------
+//
+// A workgroup takes a BM x BN tile of the result, a wave (BM / WM) x (BN / WN) of it. K goes by in stages of
+// 128 bytes a row through a ring of P slots that LDS-direct copies fill (as in the encoder's
+// projections, see gemm_kernel.h: swizzle, one barrier a stage, fragments of the longer side of a wave's tile used by
+// one row of products each and then replaced, those of the shorter side double-buffered). Rows past the
+// last are repeats of it and are not stored.
+// The result goes through LDS, 16 rows of a wave at a time, so that it is stored in whole lines and at any
+// alignment.
+struct I8Tile { int bm, bn, wm, wn, p, occ; double stage_us, tile_us; };
+
+template <typename TO, int BM, int BN, int WM, int WN, int P, int OCC, bool ACT>
+__global__ __launch_bounds__(64 * WM * WN, OCC) __attribute__((amdgpu_waves_per_eu((OCC * WM * WN + 3) / 4, (OCC * WM * WN + 3) / 4))) void k_i8_gemm(I8Args g) {
+  constexpr int CH = kStageBytes / 16;            // 16-byte chunks of a row and stage
+  constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
+  constexpr int NW = WM * WN;
+  constexpr int ACH = BM * CH, BCH = BN * CH, AG = ACH / 64, BG = BCH / 64;   // chunks, groups of 64 of them
+  constexpr int AR = (AG + NW - 1) / NW, BR = (BG + NW - 1) / NW, LOADS = AR + BR;   // copies of a wave a stage
+  constexpr int STAGE = ACH + BCH;
+  static_assert(LOADS * (P - 1) < 64 && P >= 2, "vmcnt range");
+  extern __shared__ u32x4 lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave / WN, wn = wave % WN, uwave = __builtin_amdgcn_readfirstlane(wave);
+  int tn, tm;
+  {
+    // XCD of this workgroup and its index there -> its place in the tile sequence (GemmArgs)
+    const int total = gridDim.x, xcd = blockIdx.x & 7;
+    const int t = xcd * (total >> 3) + min(xcd, total & 7) + ((int)blockIdx.x >> 3);
+    const int grp = t / (g.gh * g.gn), m1 = grp * g.gh, h = min(g.gh, g.gm - m1), v = t - m1 * g.gn;
+    tn = v / h;
+    tm = m1 + v - tn * h;
+  }
+  const int n0 = tn * BN, m0 = tm * BM, M = g.m, N = g.n;
+  const int8_t *ab = g.a + (int64_t)m0 * g.pitch, *bb = g.b + (int64_t)n0 * g.pitch;   // wave-uniform
+  const int nk = g.pitch / kStageBytes;
+  uint32_t pa[AR], pb[BR];                        // a tile's rows are under 2^26 bytes apart
+#pragma unroll
+  for (int c = 0; c < AR; ++c) {
+    const int q = min(c * NW + wave, AG - 1) * 64 + lane, r = q / CH;
+    pa[c] = (uint32_t)min(r, M - 1 - m0) * (uint32_t)g.pitch + swz<CH>(r, q % CH) * 16;
+  }
+#pragma unroll
+  for (int c = 0; c < BR; ++c) {
+    const int q = min(c * NW + wave, BG - 1) * 64 + lane, r = q / CH;
+    pb[c] = (uint32_t)min(r, N - 1 - n0) * (uint32_t)g.pitch + swz<CH>(r, q % CH) * 16;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  auto dma_one = [&](int ks, int slot, int x) {
+    const uint32_t st = lds0 + (uint32_t)(slot * STAGE) * 16u;
+    const int ko = ks * kStageBytes;
+    if (x < AR) dma16(ab + ko, pa[x], st + (uint32_t)(min(x * NW + uwave, AG - 1) * 64) * 16u);
+    else dma16(bb + ko, pb[x - AR], st + (uint32_t)(ACH + min((x - AR) * NW + uwave, BG - 1) * 64) * 16u);
+  };
+
+  i32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  constexpr int KK = 2;                           // k-steps of 64 a stage
+  constexpr bool RA = TM >= TN;                   // rows of products run over the fragments of a
+  constexpr int X = RA ? TM : TN, Y = RA ? TN : TM, NM = TM * TN;
+  i32x4 fx[X], fy[2][Y];
+  const int lc = lane & 15, rg = lane >> 4;
+  uint32_t oa[KK], ob[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    oa[kk] = (uint32_t)((wm * WTM + lc) * CH + swz<CH>(lc, 4 * kk + rg)) * 16u;
+    ob[kk] = (uint32_t)(ACH + (wn * WTN + lc) * CH + swz<CH>(lc, 4 * kk + rg)) * 16u;
+  }
+  const char *ldsb = (const char *)lds;
+  auto frag = [&](uint32_t st, uint32_t o, int t) { return *(const i32x4 *)(ldsb + (st + o) + t * 16 * CH * 16); };
+  auto read_x = [&](uint32_t st, int kk, int o) { fx[o] = frag(st, RA ? oa[kk] : ob[kk], o); };
+  auto read_y = [&](uint32_t st, int kk, int b, int y) { fy[b][y] = frag(st, RA ? ob[kk] : oa[kk], y); };
+  auto mfma_one = [&](int cur, int m) {
+    const int o = m / Y, y = m % Y;
+    if constexpr (RA) mfma_i8(acc[o][y], fy[cur][y], fx[o]);
+    else mfma_i8(acc[y][o], fx[o], fy[cur][y]);
+  };
+  constexpr int NPART = (P >= 3) ? KK : 1, PART = (LOADS + NPART - 1) / NPART;
+  auto kstep = [&](int cur, uint32_t rst, int rkk, int ks, int slot, int d0, int d1, bool bar) {
+    const int b0 = bar ? Y - 1 : 0, nd = d1 - d0;
+    auto upto = [&](int m, int n, int w) { return m <= b0 ? 0 : m >= b0 + w ? n : ((m - b0) * n + w - 1) / w; };
+    const int wy = (NM - b0 + 1) / 2, wd = NM - b0;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+      mfma_one(cur, m);
+      if (bar && m == b0) {
+        wait_vm_lds0<(P - 2) * LOADS>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+#pragma unroll
+      for (int y = upto(m, Y, wy); y < upto(m + 1, Y, wy); ++y) read_y(rst, rkk, cur ^ 1, y);
+      if (m % Y == Y - 1) read_x(rst, rkk, m / Y);
+#pragma unroll
+      for (int d = upto(m, nd, wd); d < upto(m + 1, nd, wd); ++d) dma_one(ks, slot, d0 + d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  constexpr int PRE_FULL = (NPART > 1) ? P - 1 : P, PRE_PART = (NPART > 1) ? (PART < LOADS ? PART : LOADS) : 0;
+#pragma unroll
+  for (int s = 0; s < PRE_FULL; ++s)
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) dma_one(min(s, nk - 1), s, x);
+#pragma unroll
+  for (int x = 0; x < PRE_PART; ++x) dma_one(min(P - 1, nk - 1), P - 1, x);
+  wait_vm<(PRE_FULL - 1) * LOADS + PRE_PART>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int y = 0; y < Y; ++y) read_y(0, 0, 0, y);
+#pragma unroll
+  for (int o = 0; o < X; ++o) read_x(0, 0, o);
+  for (int kt = 0; kt < nk; ++kt) {
+    const uint32_t st = (uint32_t)((kt % P) * STAGE) * 16u, nx = (uint32_t)(((kt + 1) % P) * STAGE) * 16u;
+    const int ksa = min(kt + P - 1, nk - 1), sla = (kt + P - 1) % P, ksb = min(kt + P, nk - 1), slb = kt % P;
+    kstep(0, st, 1, ksa, sla, NPART > 1 ? min(PART, LOADS) : 0, NPART > 1 ? LOADS : 0, false);
+    kstep(1, nx, 0, ksb, slb, 0, NPART > 1 ? min(PART, LOADS) : LOADS, true);
+  }
+  wait_vm<0>();
+  __syncthreads();                                // every copy has landed, every fragment is read
+
+  // row mw + 16 i + lc, columns cw + 16 j + 4 rg .. + 3
+  const int mw = m0 + uwave / WN * WTM, cw = n0 + uwave % WN * WTN;
+  if (mw >= M || cw >= N) return;
+  constexpr int PITCH = WTN * (int)sizeof(TO) + 32;
+  constexpr int CPR = WTN * (int)sizeof(TO) / 16; // 16-byte chunks of a row
+  char *box = (char *)lds + uwave * 16 * PITCH;
+  static_assert(NW * 16 * PITCH <= P * STAGE * 16, "room to turn the result");
+  f32x4 tc[TN], bs[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int n = min(cw + 16 * j + 4 * rg + e, N - 1);
+      tc[j][e] = col_scale(g.sb[n]);
+      bs[j][e] = g.bias ? to_f32(((const TO *)g.bias)[n]) : 0.f;
+    }
+  const bool vec = (((uintptr_t)g.out | (uint64_t)(g.out_row * (int64_t)sizeof(TO))) & 15) == 0 && cw + WTN <= N;   // uniform
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int mb = mw + 16 * i;
+    if (mb >= M) break;                           // uniform
+    const float sr = row_scale(g.sa[min(mb + lc, M - 1)]);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      typedef TO to4 __attribute__((ext_vector_type(4)));
+      to4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = from_f32<TO>(finish<ACT>(acc[i][j][e], sr, tc[j][e], bs[j][e]));
+      *(to4 *)(box + lc * PITCH + (16 * j + 4 * rg) * (int)sizeof(TO)) = y;
+    }
+    if (vec) {
+#pragma unroll
+      for (int x = 0; x < 16 * CPR / 64; ++x) {
+        const int q = x * 64 + lane, r = q / CPR, c = q % CPR;
+        const u32x4 v = *(const u32x4 *)(box + r * PITCH + c * 16);
+        if (mb + r < M) *(u32x4 *)((char *)g.out + ((int64_t)(mb + r) * g.out_row + cw) * (int)sizeof(TO) + c * 16) = v;
+      }
+    } else {
+      for (int q = lane; q < 16 * WTN; q += 64) {
+        const int r = q / WTN, c = q % WTN;
+        const TO v = *(const TO *)(box + r * PITCH + c * (int)sizeof(TO));
+        if (mb + r < M && cw + c < N) ((TO *)g.out)[(int64_t)(mb + r) * g.out_row + cw + c] = v;
+      }
+    }
+  }
+}
+
+template <typename TO, bool ACT, int BM, int BN, int WM, int WN, int P, int OCC>
+hipError_t run_tile(const I8Args &g, hipStream_t s) {
+  constexpr int bytes = P * (BM + BN) * kStageBytes;
+  auto kern = k_i8_gemm<TO, BM, BN, WM, WN, P, OCC, ACT>;
+  static const hipError_t attr =
+      hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL(kern, dim3(g.gm * g.gn), dim3(64 * WM * WN), bytes, s, g);
+  return hipGetLastError();
+}
+
+// bm, bn, waves, ring, workgroups a compute unit; us of a stage and of a tile.
+#define I8_TILES(X)                                     \
+  X(0, 256, 256, 4, 2, 2, 1, 1.335, 10.86)              \
+  X(1, 192, 384, 2, 4, 2, 1, 1.309, 15.45)              \
+  X(2, 128, 256, 4, 2, 3, 1, 0.754, 7.23)               \
+  X(3, 128, 128, 4, 2, 4, 1, 0.461, 4.42)               \
+  X(4, 96, 128, 2, 4, 4, 1, 0.385, 3.82)                \
+  X(5, 64, 128, 2, 4, 5, 1, 0.300, 3.30)                \
+  X(6, 64, 64, 2, 2, 6, 1, 0.211, 2.29)                 \
+  X(7, 32, 64, 2, 2, 6, 2, 0.196, 1.45)
+const I8Tile kTiles[] = {
+#define I8_INFO(id, bm, bn, wm, wn, p, occ, su, tu) {bm, bn, wm, wn, p, occ, su, tu},
+    I8_TILES(I8_INFO)
+#undef I8_INFO
+};
+
+// Tile times that a launch takes on 256 compute units (as the encoder's planner counts them).
+double rounds_of(int64_t wgs, int occ) {
+  const double f = (double)wgs / 256.0, full = std::floor(f / occ), rem = f - occ * full;
+  double r = full * (occ == 2 ? 1.5 : 1.0);
+  if (rem > 0) r += rem <= 1.0 ? 0.85 + 0.15 * rem : 1.0 + 0.5 * (0.5 + 0.5 * (rem - 1.0));
+  return r;
+}
+int pick_tile(int m, int n, int pitch) {
+  int best = 0;
+  double least = 1e30;
+  for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
+    const I8Tile &t = kTiles[i];
+    const int64_t wgs = (int64_t)((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn);
+    const double us = rounds_of(wgs, t.occ) * (pitch / kStageBytes * t.stage_us + t.tile_us);
+    if (us < least) {
+      least = us;
+      best = i;
+    }
+  }
+  return best;
+}
+
+template <typename TO, bool ACT> hipError_t run_many(I8Args g, hipStream_t s) {
+  const int id = pick_tile(g.m, g.n, g.pitch);
+  g.gm = (g.m + kTiles[id].bm - 1) / kTiles[id].bm;
+  g.gn = (g.n + kTiles[id].bn - 1) / kTiles[id].bn;
+  // an XCD's 32 tiles at a time as a block: about as many rows of a as of b
+  g.gh = 1;
+  while (g.gh < g.gm && g.gh * kTiles[id].bm < 6 * kTiles[id].bn) ++g.gh;
+  switch (id) {
+#define I8_CASE(idv, bm, bn, wm, wn, p, occ, su, tu) \
+  case idv: return run_tile<TO, ACT, bm, bn, wm, wn, p, occ>(g, s);
+    I8_TILES(I8_CASE)
+#undef I8_CASE
+  }
+  return hipErrorInvalidValue;
+}
+
+template <typename TO, bool ACT> hipError_t run(const I8Args &g, hipStream_t s) {
+  return g.m <= 64 ? run_few<TO, ACT>(g, s) : run_many<TO, ACT>(g, s);
+}
+
 }  // namespace
 
 // Codes and scales of rows that the call quantises itself.
@@ -98,8 +339,8 @@ hipError_t launch_i8_linear(I8Args a, int x_type, int dtype, void *ws, hipStream
     a.a = codes;
     a.sa = scales;
   }
-  if (dtype == MTE_BF16) return a.act ? run_few<bf16, true>(a, s) : run_few<bf16, false>(a, s);
-  return a.act ? run_few<float, true>(a, s) : run_few<float, false>(a, s);
+  if (dtype == MTE_BF16) return a.act ? run<bf16, true>(a, s) : run<bf16, false>(a, s);
+  return a.act ? run<float, true>(a, s) : run<float, false>(a, s);
 }
 
 }  // namespace mte

@@ -1,4 +1,4 @@
-// Rows as 8-bit integers with a scale each: s = max |x| / 127, c = x / s to the nearest whole number.
+// Rows as 8-bit integers with a scale each: s = max |x| (1/127), c = x / s to the nearest whole number.
 //
 // Codes are those of the exact quotient: c0 = rint(x * (1/s)) is off by at most one, r = x - c0 s is
 // exact in one fma (a multiple of the finer ulp of x and s, and no more than s), and c0 moves by
@@ -54,7 +54,7 @@ struct Scale {
   bool bad;
   __device__ __forceinline__ explicit Scale(uint32_t top) {
     bad = top >= 0x7F800000u;
-    s = fmaxf(__uint_as_float(bad ? 0u : top) / 127.f, 0x1p-126f);
+    s = fmaxf(__uint_as_float(bad ? 0u : top) * (1.f / 127.f), 0x1p-126f);
     inv = 1.f / s;
   }
   __device__ __forceinline__ float stored() const { return bad ? __uint_as_float(0x7FC00000u) : s; }
