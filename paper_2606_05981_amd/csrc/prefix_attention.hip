@@ -63,66 +63,51 @@ __device__ __forceinline__ Part part_in(const PrefixArgs &a, const CondSeq &sq, 
   return p;
 }
 
-// Values of 32 keys of which the rows see different ones, infinities or NaN among them: key by key, for the
-// rows that see it (0 times infinity in the matrix product would reach the others). n: keys that this lane's row sees.
-template <typename T, int DP>
-__device__ __forceinline__ bool wild_values(const char *sv, int sub, int lane) {
-  constexpr int NCH = DP * sizeof(T) / 16;
+// Infinities and NaN among the values of a tile whose rows see different keys: 0 times infinity in the matrix
+// product would reach the rows that do not see them. Such values become zeros on their way to LDS, and rows that
+// see them have them added after the last tile (add_wild; whatever its weight, an infinity stays one). In
+// the loop itself a second path to O would cost a second copy of it, and its registers.
+template <typename T> __device__ __forceinline__ bool tame(u32x4 &x) {
   bool wild = false;
-#pragma unroll 4
-  for (int i = lane; i < 32 * NCH; i += 64) {
-    const u32x4 x = ((const u32x4 *)sv)[sub * 32 * NCH + i];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if constexpr (sizeof(T) == 4) wild |= (x[w] & 0x7F800000u) == 0x7F800000u;
-      else wild |= (x[w] & 0x7F800000u) == 0x7F800000u || (x[w] & 0x7F80u) == 0x7F80u;
+  for (int w = 0; w < 4; ++w) {
+    if constexpr (sizeof(T) == 4) {
+      const bool b = (x[w] & 0x7F800000u) == 0x7F800000u;
+      x[w] = b ? 0u : x[w];
+      wild |= b;
+    } else {
+      const bool hi = (x[w] & 0x7F800000u) == 0x7F800000u, lo = (x[w] & 0x7F80u) == 0x7F80u;
+      x[w] &= (hi ? 0u : 0xFFFF0000u) | (lo ? 0u : 0xFFFFu);
+      wild |= hi || lo;
     }
   }
-  return __any(wild);
+  return wild;
 }
-template <typename T, int DP>
-__device__ __forceinline__ void add_values_seen(f32x16 (&o)[DP / 32], const float (&p)[16], const char *sv, int sub, int n,
-                                                int lane) {
-  constexpr int NCH = DP * sizeof(T) / 16, ND = DP / 32, E = 16 / sizeof(T);
+// Adds the infinities and NaN among the values of own keys [from, to) to O of the rows that see them; n: keys that
+// this lane's row sees.
+template <typename T, int ND>
+__device__ __forceinline__ void add_wild(f32x16 (&o)[ND], const T *vg, int64_t v_row, int d_all, int from, int to, int n,
+                                         int lane) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
   const int h = lane >> 5;
 #pragma unroll 1
-  for (int j = 0; j < 32; ++j) {
-    const int from = 4 * (j >> 3) + (j & 3);         // of the half (j >> 2) & 1
-    float pj = p[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) pj = i == from ? p[i] : pj;
-    pj = __shfl(pj, (lane & 31) + 32 * ((j >> 2) & 1), kWave);
-    if constexpr (sizeof(T) == 2) pj = (float)(bf16)pj;
-    const int row = sub * 32 + j;
+  for (int j = from; j < to; ++j) {
+    const T *row = vg + (int64_t)j * v_row;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        int c;
-        if constexpr (sizeof(T) == 4) c = 32 * (d ^ ((row >> 2) & 1)) + 8 * (r >> 2) + 4 * h + (r & 3);
-        else c = 32 * d + 8 * (r >> 2) + 4 * h + (r & 3);
-        float v;
-        if constexpr (sizeof(T) == 4) v = ((const float *)sv)[row * DP + c];
-        else v = (float)((const bf16 *)(sv + (row * NCH + value_chunk<NCH, true>(row, c / E)) * 16))[c % E];
-        o[d][r] = j < n ? fmaf(pj, v, o[d][r]) : o[d][r];
+      for (int b = 0; b < 4; ++b) {
+        const int c = 32 * d + 8 * b + 4 * h;
+        if (c < d_all) {
+          const t4 x = *(const t4 *)(row + c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = to_f32((T)x[e]);
+            o[d][4 * b + e] += j < n && (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u ? v : 0.f;
+          }
+        }
       }
   }
-}
-
-template <typename T, int DP>
-__device__ __forceinline__ void take_values(f32x16 (&o)[DP / 32], const f32x16 &s, float sc, float ref, float &l,
-                                            const char *sv, int sub, bool differ, int n, int lane) {
-  if (differ && wild_values<T, DP>(sv, sub, lane)) { // wave-uniform
-    float p[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -ref));
-      l += p[i];
-    }
-    add_values_seen<T, DP>(o, p, sv, sub, n, lane);
-    return;
-  }
-  add_values<T, DP>(o, probs_of<T>(s, sc, ref, l), sv, sub, lane);
 }
 
 // As k_cross: four waves, 32 RW rows, 4 / RW ways over the keys of a tile.
@@ -154,6 +139,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
   const int64_t tok = sq.q0 + (live ? r / a.rep : 0);
   const int head = g * a.rep + (live ? r % a.rep : 0);
   const int mine = ks.seen(live ? r / a.rep : sq.q_len - 1), least = ks.seen(r0 / a.rep);
+  const int all_see = ks.cross ? ks.seen(span.row_tile * 32 * RW / a.rep) : INT_MAX;   // every row of the tile does
+  uint32_t *wild = (uint32_t *)(sv + KT * NCH * 16);   // a word a wave: it found some
 
   const T *pk = (const T *)a.pk + (int64_t)g * a.pk_head, *pv = (const T *)a.pv + (int64_t)g * a.pv_head;
   const int64_t k0 = max(sq.k0, 0);
@@ -180,7 +167,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
       }
     }
   };
-  auto lstore = [&](int t0) {
+  auto lstore = [&](int kt, int t0) {
+    if (kt >= ks.np && (kt - ks.np + 1) * KT > all_see) {      // workgroup-uniform
+      bool any = false;
+#pragma unroll
+      for (int t = 0; t < STEP; ++t) any |= tame<T>(vx[t]);
+      if (any) wild[wave] = 1;
+    }
 #pragma unroll
     for (int t = 0; t < STEP; ++t) {
       const int idx = tid + (t0 + t) * kThreads, row = idx / NCH, c = idx % NCH;
@@ -189,6 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
     }
   };
 
+  if (lane == 0) wild[wave] = 0;
   if constexpr (AHEAD)
     if (span.lo < span.hi) gload(span.lo, 0);       // workgroup-uniform
   frag_t qf[NK];
@@ -211,23 +205,30 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
     if (every < 32) mask_below(s[0], n, lane);      // wave-uniform
     float sc = a.sc, ref;
     st.raise(s, max16(s[0], -INFINITY) * sc, sc, ref);
-    take_values<T, DP>(st.o, s[0], sc, ref, st.l, sv, kw, !pre && ks.cross && every < 32, n, lane);
+    add_values<T, DP>(st.o, probs_of<T>(s[0], sc, ref, st.l), sv, kw, lane);
   };
 
   for (int kt = span.lo; kt < span.hi; ++kt) {
     __syncthreads();                                // the tile before is read
     if constexpr (AHEAD) {
-      lstore(0);
+      lstore(kt, 0);
     } else {
       for (int t0 = 0; t0 < CPT; t0 += STEP) {
         gload(kt, t0);
-        lstore(t0);
+        lstore(kt, t0);
       }
     }
     __syncthreads();
     if constexpr (AHEAD)
       if (kt + 1 < span.hi) gload(kt + 1, 0);
     if (r0 < rows) compute(kt);                     // wave-uniform
+  }
+  if (ks.cross) {
+    __syncthreads();
+    if (kw == 0 && (wild[0] | wild[1] | wild[2] | wild[3])) {
+      const int from = max(max(span.lo - ks.np, 0) * KT, all_see / KT * KT), to = min((span.hi - ks.np) * KT, ks.klen);
+      add_wild<T, ND>(st.o, vg, a.v_row, a.d, from, to, mine, lane);
+    }
   }
   if constexpr (KW > 1) {
     __syncthreads();
@@ -255,6 +256,9 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_prefix_stream(Pr
   const Part span = part_in(a, sq, ks, tile - sq.tile0, rows, 128, 32);
   const int r0 = span.row_tile * 128 + wave * 32;
   const int mine = ks.seen(min(r0 + lrow, rows - 1) / a.rep), least = ks.seen(r0 / a.rep);
+  const int all_see = ks.cross ? ks.seen(span.row_tile * 128 / a.rep) : INT_MAX;   // every row of the tile does
+  uint32_t *wild = (uint32_t *)(lds + S::BYTES / 16);   // a word a wave: it found some
+  if (lane == 0) wild[wave] = 0;
 
   const bf16 *pk = (const bf16 *)a.pk + (int64_t)g * a.pk_head, *pv = (const bf16 *)a.pv + (int64_t)g * a.pv_head;
   const int64_t k0 = max(sq.k0, 0);
@@ -317,6 +321,16 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_prefix_stream(Pr
       for (int i = 0; i < CP; ++i)
         if (RPC * (wave * CP + i) + lane / NCH >= n) ((u32x4 *)sv)[(wave * CP + i) * 64 + lane] = u32x4{0, 0, 0, 0};
     }
+    if (!pre && first + 32 > all_see) {             // uniform
+#pragma unroll
+      for (int i = 0; i < CP; ++i) {
+        u32x4 *at = (u32x4 *)sv + (wave * CP + i) * 64 + lane, x = *at;
+        if (tame<bf16>(x)) {
+          *at = x;
+          wild[wave] = 1;
+        }
+      }
+    }
     __syncthreads();                                // the tile is whole, and the one before it read
     if (t + 2 < t1) copy_tile(t + 2);
     if (r0 < rows) {                                // wave-uniform
@@ -330,9 +344,14 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_prefix_stream(Pr
       if (every < 32) mask_below(s[0], pre ? n : mine - first, lane);
       float sc = a.sc, ref;
       st.raise(s, max16(s[0], -INFINITY) * sc, sc, ref);
-      take_values<bf16, DP>(st.o, s[0], sc, ref, st.l, (const char *)sv, 0, !pre && ks.cross && every < 32, mine - first,
-                            lane);
+      add_values<bf16, DP>(st.o, probs_of<bf16>(s[0], sc, ref, st.l), (const char *)sv, 0, lane);
     }
+  }
+  if (ks.cross) {
+    __syncthreads();
+    if (r0 < rows && (wild[0] | wild[1] | wild[2] | wild[3]))
+      add_wild<bf16, ND>(st.o, vg, a.v_row, a.d, max(max(t0 - ks.np, 0) * 32, all_see / 32 * 32),
+                         min((t1 - ks.np) * 32, ks.klen), mine, lane);
   }
   if (r0 >= rows) return;
   if (span.used > 1 || a.shared) {
@@ -592,12 +611,12 @@ hipError_t run(PrefixArgs &a, const Plan &pl, bool copies, hipStream_t s) {
   hipError_t e;
   if (n > 0) {
     auto kern = pl.kind == Plan::FEW ? k_prefix<T, DP, 1> : k_prefix<T, DP, 4>;
-    int lds = 2 * pl.KT * DP * (int)sizeof(T);
+    int lds = 2 * pl.KT * DP * (int)sizeof(T) + 16;
     if (pl.kind == Plan::FEW) lds = std::max(lds, 3 * (2 + DP / 2) * 64 * 4);
     if constexpr (sizeof(T) == 2) {
       if (copies) {
         kern = k_prefix_stream<DP>;
-        lds = Stream<DP>::BYTES;
+        lds = Stream<DP>::BYTES + 16;
       }
     }
     if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
