@@ -7,6 +7,7 @@
 #include <cmath>
 
 #include "gemm_kernel.h"
+#include "i8_device.h"
 #include "proj_launch.h"
 
 namespace mte {
@@ -319,6 +320,189 @@ template <typename TO, bool ACT> hipError_t run_many(I8Args g, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
+// ---- many short rows, quantised on the way ------------------------------------------------------
+//
+// Rows of up to 1024 elements fit LDS as codes, 128 of them at a time: a workgroup reads its rows of x
+// once, quantises them into the layout of the products' operand and goes through all of the weight, which the
+// L2 holds, 128 rows and 128 bytes of K at a time (a ring of two slots). x is read once and no codes
+// are written or read; the stores of a tile drain beneath the products of the next.
+// Eight lanes a row: a lane takes every eighth chunk of 8 elements, maxima are three exchanges.
+// LDS: nk stages of [128 rows][8 chunks] of codes, two of the weight's, swizzled as the tiles above.
+constexpr int kFusedRows = 128, kFusedCols = 128, kFusedStage = kFusedRows * kStageBytes;
+int fused_lds(int pitch) { return (pitch / kStageBytes + 2) * kFusedStage; }
+
+template <typename T, typename TO, int NW, int NJ, bool ACT>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g, int vec_in) {
+  constexpr int CH = kStageBytes / 16, WN = NW / 2, WTN = kFusedCols / WN, TM = 4, TN = WTN / 16;
+  constexpr int BR = kFusedCols * CH / 64 / NW;   // copies of a wave a stage
+  extern __shared__ u32x4 lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nk = g.pitch / kStageBytes, M = g.m, N = g.n, m0 = blockIdx.x * kFusedRows;
+  const uint32_t ring0 = (uint32_t)nk * kFusedStage;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  char *ldsb = (char *)lds;
+  float *sa = (float *)(ldsb + ring0 + kFusedStage);   // the rows' scales, until the second slot is used
+
+  uint32_t pb[BR];
+  const int8_t *bb = g.b;
+  auto aim = [&](int n0) {                        // at the weight rows of a tile
+    bb = g.b + (int64_t)n0 * g.pitch;
+#pragma unroll
+    for (int c = 0; c < BR; ++c) {
+      const int q = (c * NW + wave) * 64 + lane, r = q / CH;
+      pb[c] = (uint32_t)min(r, N - 1 - n0) * (uint32_t)g.pitch + swz<CH>(r, q % CH) * 16;
+    }
+  };
+  auto copy = [&](int ks, int slot) {
+#pragma unroll
+    for (int c = 0; c < BR; ++c)
+      dma16(bb + ks * kStageBytes, pb[c], lds0 + ring0 + (uint32_t)(slot * kFusedStage + (c * NW + wave) * 1024));
+  };
+  aim(0);
+  copy(0, 0);
+
+  {
+    const int l8 = lane & 7, nj = g.pitch / 64;   // chunks of 8 elements a lane
+#pragma unroll 1
+    for (int r0 = wave * (kFusedRows / NW); r0 < (wave + 1) * (kFusedRows / NW); r0 += 8) {
+      const int r = r0 + (lane >> 3);
+      const T *row = (const T *)g.x + (int64_t)min(m0 + r, M - 1) * g.x_row;
+      float y[NJ][8];
+      uint32_t top = 0;
+      if (vec_in) {                               // uniform
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) load8<T, true>(y[j], row, (j * 8 + l8) * 8, g.k);
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) load8<T, false>(y[j], row, (j * 8 + l8) * 8, g.k);
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) top = top8(y[j], top);
+#pragma unroll
+      for (int m = 4; m >= 1; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, kWave));
+      const Scale sc(top);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int e = (j * 8 + l8) * 8, c = (e >> 4) & 7;
+        if (j < nj) *(u32x2 *)(ldsb + (e >> 7) * kFusedStage + (r * CH + swz<CH>(r, c)) * 16 + (e & 8)) = sc.codes(y[j]);
+      }
+      if (l8 == 0) sa[r] = row_scale(sc.stored());
+    }
+  }
+
+  const int wm = wave / WN, wn = wave % WN, lc = lane & 15, rg = lane >> 4;
+  uint32_t oa[2], ob[2];
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    oa[kk] = (uint32_t)((wm * 64 + lc) * CH + swz<CH>(lc, 4 * kk + rg)) * 16u;
+    ob[kk] = ring0 + (uint32_t)((wn * WTN + lc) * CH + swz<CH>(lc, 4 * kk + rg)) * 16u;
+  }
+  float sr[TM];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < TM; ++i) sr[i] = sa[wm * 64 + 16 * i + lc];
+  __syncthreads();
+  const bool vec = (((uintptr_t)g.out | (uint64_t)(g.out_row * (int64_t)sizeof(TO))) & 15) == 0;   // uniform
+  int slot = 0;
+  bool landed = false;
+#pragma unroll 1
+  for (int n0 = 0; n0 < N; n0 += kFusedCols) {
+    i32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+#pragma unroll 1
+    for (int ks = 0; ks < nk; ++ks) {
+      if (!landed) wait_vm<0>();
+      landed = false;
+      __syncthreads();                            // the stage is whole (first: the codes), and the slot beside it read
+      if (ks + 1 < nk) {
+        copy(ks + 1, slot ^ 1);
+      } else if (n0 + kFusedCols < N) {
+        aim(n0 + kFusedCols);
+        copy(0, slot ^ 1);
+      }
+      const char *pa = ldsb + ks * kFusedStage, *pw = ldsb + slot * kFusedStage;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        i32x4 fa[TM], fb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[i] = *(const i32x4 *)(pa + oa[kk] + i * 16 * kStageBytes);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[j] = *(const i32x4 *)(pw + ob[kk] + j * 16 * kStageBytes);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) mfma_i8(acc[i][j], fb[j], fa[i]);
+      }
+      slot ^= 1;
+    }
+    // row mw + 16 i + lc, columns cw + 16 j + 4 rg .. + 3
+    const int mw = m0 + wm * 64, cw = n0 + wn * WTN;
+    f32x4 tc[TN], bs[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int n = min(cw + 16 * j + 4 * rg + e, N - 1);
+        tc[j][e] = col_scale(g.sb[n]);
+        bs[j][e] = g.bias ? to_f32(((const TO *)g.bias)[n]) : 0.f;
+      }
+    wait_vm<0>();                                 // the next stage's copy: before the stores, not behind them
+    landed = true;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = mw + 16 * i + lc;
+      TO *out = (TO *)g.out + (int64_t)m * g.out_row + cw;
+#pragma unroll
+      for (int j = 0; j < TN; j += 2) {
+        float z[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[u][e] = finish<ACT>(acc[i][j + u][e], sr[i], tc[j + u][e], bs[j + u][e]);
+        if (vec && cw + WTN <= N) {               // uniform
+          if constexpr (sizeof(TO) == 2) {
+            // eight columns a lane: of blocks j and j + 1 the 16-lane rows trade places
+            const u32x2 x = __builtin_bit_cast(u32x2, bf16x4{(bf16)z[0][0], (bf16)z[0][1], (bf16)z[0][2], (bf16)z[0][3]});
+            const u32x2 y = __builtin_bit_cast(u32x2, bf16x4{(bf16)z[1][0], (bf16)z[1][1], (bf16)z[1][2], (bf16)z[1][3]});
+            const auto a = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
+            const auto b = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+            if (m < M) *(u32x4 *)(out + 16 * (j + (rg & 1)) + 8 * (rg >> 1)) = u32x4{a[0], b[0], a[1], b[1]};
+          } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              if (m < M) *(f32x4 *)(out + 16 * (j + u) + 4 * rg) = f32x4{z[u][0], z[u][1], z[u][2], z[u][3]};
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int c = 16 * (j + u) + 4 * rg + e;
+              if (m < M && cw + c < N) out[c] = from_f32<TO>(z[u][e]);
+            }
+        }
+      }
+    }
+  }
+}
+
+template <typename T, typename TO, bool ACT> hipError_t run_fused(const I8Args &g, hipStream_t s) {
+  const int vec = ((uintptr_t)g.x & 15) == 0 && g.x_row * (int64_t)sizeof(T) % 16 == 0, bytes = fused_lds(g.pitch);
+  const bool two = bytes <= 80 * 1024;            // two workgroups a compute unit
+  auto kern = two ? k_i8_fused<T, TO, 4, 6, ACT> : g.pitch <= 512 ? k_i8_fused<T, TO, 8, 8, ACT> : k_i8_fused<T, TO, 8, 16, ACT>;
+  if (bytes > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kern, dim3((g.m + kFusedRows - 1) / kFusedRows), dim3(two ? 256 : 512), bytes, s, g, vec);
+  return hipGetLastError();
+}
+// Whether rows are quantised on the way.
+bool takes_fused(int x_type, int m, int n, int pitch) { return x_type != MTE_I8_CODES && pitch <= 1024 && m >= 8192; }
+
 template <typename TO, bool ACT> hipError_t run(const I8Args &g, hipStream_t s) {
   return g.m <= 64 ? run_few<TO, ACT>(g, s) : run_many<TO, ACT>(g, s);
 }
@@ -326,11 +510,20 @@ template <typename TO, bool ACT> hipError_t run(const I8Args &g, hipStream_t s) 
 }  // namespace
 
 // Codes and scales of rows that the call quantises itself.
-int64_t i8_workspace(int x_type, int m, int, int k) {
-  return x_type == MTE_I8_CODES ? 0 : (int64_t)m * i8_pitch(k) + (int64_t)m * 4;
+int64_t i8_workspace(int x_type, int m, int n, int k) {
+  const int64_t pitch = i8_pitch(k);
+  return x_type == MTE_I8_CODES || takes_fused(x_type, m, n, (int)pitch) ? 0 : m * pitch + (int64_t)m * 4;
 }
 
 hipError_t launch_i8_linear(I8Args a, int x_type, int dtype, void *ws, hipStream_t s) {
+  if (takes_fused(x_type, a.m, a.n, a.pitch)) {
+    if (x_type == MTE_BF16) {
+      if (dtype == MTE_BF16) return a.act ? run_fused<bf16, bf16, true>(a, s) : run_fused<bf16, bf16, false>(a, s);
+      return a.act ? run_fused<bf16, float, true>(a, s) : run_fused<bf16, float, false>(a, s);
+    }
+    if (dtype == MTE_BF16) return a.act ? run_fused<float, bf16, true>(a, s) : run_fused<float, bf16, false>(a, s);
+    return a.act ? run_fused<float, float, true>(a, s) : run_fused<float, float, false>(a, s);
+  }
   if (x_type != MTE_I8_CODES) {
     int8_t *codes = (int8_t *)ws;
     float *scales = (float *)(codes + (int64_t)a.m * a.pitch);

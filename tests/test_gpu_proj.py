@@ -137,6 +137,8 @@ LINEAR = [
     (31, 640, 64), (33, 1001, 129), (64, 2048, 512), (65, 2048, 257), (96, 2048, 1024), (127, 513, 255), (128, 512, 256),
     (129, 129, 257), (200, 6144, 300), (255, 320, 640), (256, 384, 1283), (257, 4096, 1000), (777, 1001, 1283),
     (1030, 320, 640), (1536, 640, 1100), (2049, 300, 77), (300, 20000, 70),
+    # many short rows
+    (8192, 320, 640), (8200, 100, 70), (8193, 513, 257), (9000, 1000, 130), (8321, 384, 1), (16390, 128, 129), (8255, 1024, 200),
 ]
 
 
@@ -181,7 +183,7 @@ def test_linear_longest_rows(torch, P):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("m", [5, 300])
+@pytest.mark.parametrize("m", [5, 300, 8192])
 def test_linear_strides(torch, P, m, dtype):
     """x a slice of wider rows at an odd address, out a slice whose other channels stay, leading dimensions, a
     second call's results, and rows behind the last one."""
@@ -205,15 +207,15 @@ def test_linear_strides(torch, P, m, dtype):
 
 def test_linear_batch_invariant(torch, P):
     """A row's result does not depend on the rows beside it, nor on the kernel that takes them: the sums are exact."""
-    x, w = _randn(torch, 1, 700, 640, std=2.0), _randn(torch, 2, 330, 640, std=0.05)
+    x, w = _randn(torch, 1, 8300, 640, std=2.0), _randn(torch, 2, 330, 640, std=0.05)
     weight, b = P.quantize_rows(w), _randn(torch, 3, 330)
     whole = P.i8_linear(x, weight, b, act="silu")
-    for a, e in ((0, 1), (3, 17), (5, 69), (100, 400)):
+    for a, e in ((0, 1), (3, 17), (5, 69), (100, 400), (7, 8200)):
         assert torch.equal(P.i8_linear(x[a:e], weight, b, act="silu"), whole[a:e])
     assert torch.equal(P.i8_linear(P.quantize_rows(x), weight, b, act="silu"), whole)
 
 
-@pytest.mark.parametrize("m", [3, 150])
+@pytest.mark.parametrize("m", [3, 150, 8200])
 def test_linear_nan_rows(torch, P, m):
     """A token with an infinity or NaN gives a row of NaN, a weight row with one a column; the others are
     what they are without."""
