@@ -31,59 +31,137 @@ template <bool ACT> __device__ __forceinline__ float finish(int acc, float s, fl
   return z;
 }
 
-// ---- few rows -----------------------------------------------------------------------------------
+// ---- up to 16 rows ------------------------------------------------------------------------------
 //
-// Bound by the bytes of the weight, or by latency. A workgroup of eight waves takes 16 weight rows and all
-// rows of a (MT blocks of 16); the waves take K in turn, 128 bytes of each row at a time, straight from memory
-// to the operands, and add up through LDS.
-constexpr int kFewWaves = 8;
-template <typename TO, int MT, bool ACT>
-__global__ __launch_bounds__(64 * kFewWaves) void k_i8_few(I8Args g) {
-  __shared__ i32x4 part[kFewWaves][MT][64];
+// Bound by the bytes of the weight, or by latency. A workgroup of 16 waves takes blocks of 16 weight rows in
+// turn; its waves share K, 128 bytes of each row at a time, straight from memory to the operands (the next
+// block's loads are in flight meanwhile), and add up through LDS. The rows of a are few enough to lie in LDS
+// whole; every workgroup quantises them for itself, once, while its first weights arrive: a launch less than with
+// codes through memory.
+// LDS: rows of codes 64 bytes further apart than they are long, so that an operand's 16 rows of 64 bytes
+// fill the banks.
+constexpr int kFewWaves = 16, kFewRows = 16, kFewThreads = 64 * kFewWaves, kFewLds = 96 * 1024;
+int few_lds(int m, int pitch) { return m * (pitch + 64); }
+
+template <typename T, typename TO, bool ACT>
+__global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g, int vec_in) {
+  constexpr int AHEAD = 2;                        // blocks of 128 bytes of K a wave and weight row, ahead
+  __shared__ i32x4 part[2][kFewWaves][64];
+  __shared__ uint32_t tops[kFewRows];
+  __shared__ float sa[kFewRows];
+  extern __shared__ u32x4 lds[];
+  char *codes = (char *)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
-  const int lr = lane & 15, lk = (lane >> 4) * 16;
-  const int8_t *bp = g.b + (int64_t)min(n0 + lr, g.n - 1) * g.pitch + lk;
-  const int8_t *ap[MT];
+  const int lr = lane & 15, lk = (lane >> 4) * 16, row_bytes = g.pitch + 64;
+  const int blocks = (g.n + 15) / 16;
+  i32x4 w[2 * AHEAD];
+  auto fetch = [&](int nb) {
+    const int8_t *bp = g.b + (int64_t)min(nb * 16 + lr, g.n - 1) * g.pitch + lk;
 #pragma unroll
-  for (int t = 0; t < MT; ++t) ap[t] = g.a + (int64_t)min(m0 + 16 * t + lr, g.m - 1) * g.pitch + lk;
-  i32x4 acc[MT];
+    for (int b = 0; b < AHEAD; ++b) {
+      const int k = (wave + b * kFewWaves) * 128;
+      if (k < g.pitch) {                          // uniform
+        w[2 * b] = *(const i32x4 *)(bp + k);
+        w[2 * b + 1] = *(const i32x4 *)(bp + k + 64);
+      }
+    }
+  };
+  fetch(blockIdx.x);
+
+  if constexpr (sizeof(T) == 1) {
+    for (int i = tid; i < g.m * (g.pitch / 16); i += kFewThreads) {
+      const int r = i / (g.pitch / 16), c = i - r * (g.pitch / 16);
+      *(u32x4 *)(codes + r * row_bytes + c * 16) = *(const u32x4 *)(g.a + (int64_t)r * g.pitch + c * 16);
+    }
+    if (tid < g.m) sa[tid] = row_scale(g.sa[tid]);
+  } else {
+    if (tid < kFewRows) tops[tid] = 0;
+    __syncthreads();
+    // 1024, 512, .. 64 threads a row
+    const int per = kFewThreads >> (g.m > 8 ? 4 : g.m > 4 ? 3 : g.m > 2 ? 2 : g.m > 1 ? 1 : 0), r = tid / per, c0 = tid % per;
+    const T *row = (const T *)g.x + (int64_t)min(r, g.m - 1) * g.x_row;
+    constexpr int KEPT = 4;
+    Eight<T> y[KEPT];
+    Top<T> top;
+    auto read = [&](Eight<T> &z, int c) {
+      if (vec_in) load8<T, true>(z, row, c * 8, g.k);
+      else load8<T, false>(z, row, c * 8, g.k);
+    };
 #pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = i32x4{0, 0, 0, 0};
-#pragma unroll 2
-  for (int k = wave * 128; k < g.pitch; k += kFewWaves * 128) {
+    for (int j = 0; j < KEPT; ++j) read(y[j], c0 + j * per);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const i32x4 b = *(const i32x4 *)(bp + k + 64 * h);
+    for (int j = 0; j < KEPT; ++j) top.take(y[j]);
+    for (int c = c0 + KEPT * per; c * 8 < g.k; c += per) {
+      Eight<T> z;
+      read(z, c);
+      top.take(z);
+    }
+    const uint32_t t = lanes_top<32>(top.bits());  // a wave is within a row
+    if (lane == 0) atomicMax(&tops[r], t);
+    __syncthreads();
+    const Scale sc(tops[r]);
+    if (r < g.m) {
+      char *to = codes + r * row_bytes;
 #pragma unroll
-      for (int t = 0; t < MT; ++t) mfma_i8(acc[t], b, *(const i32x4 *)(ap[t] + k + 64 * h));
+      for (int j = 0; j < KEPT; ++j)
+        if ((c0 + j * per) * 8 < g.pitch) *(u32x2 *)(to + (c0 + j * per) * 8) = sc.codes(y[j]);
+      for (int c = c0 + KEPT * per; c * 8 < g.pitch; c += per) {
+        Eight<T> z;
+        read(z, c);
+        *(u32x2 *)(to + c * 8) = sc.codes(z);
+      }
+      if (c0 == 0) sa[r] = row_scale(sc.stored());
     }
   }
-#pragma unroll
-  for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
   __syncthreads();
-  // output (row 16 t + i, columns 4 c .. 4 c + 3) is lane 16 c + i of every part
-  for (int x = tid; x < MT * 64; x += 64 * kFewWaves) {
-    const int t = x >> 6, l = x & 63, m = m0 + 16 * t + (l & 15), n = n0 + 4 * (l >> 4);
-    i32x4 s = part[0][t][l];
+
+  const char *ap = codes + min(lr, g.m - 1) * row_bytes + lk;
+  int buf = 0;
+  for (int nb = blockIdx.x; nb < blocks; nb += gridDim.x, buf ^= 1) {
+    i32x4 acc{0, 0, 0, 0};
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) s += part[w][t][l];
-    if (m >= g.m) continue;
-    const float sr = row_scale(g.sa[m]);
-    TO *out = (TO *)g.out + (int64_t)m * g.out_row + n;
+    for (int b = 0; b < AHEAD; ++b) {
+      const int k = (wave + b * kFewWaves) * 128;
+      if (k < g.pitch) {
+        mfma_i8(acc, w[2 * b], *(const i32x4 *)(ap + k));
+        mfma_i8(acc, w[2 * b + 1], *(const i32x4 *)(ap + k + 64));
+      }
+    }
+    if (g.pitch > AHEAD * kFewWaves * 128) {      // long rows: the rest
+      const int8_t *bp = g.b + (int64_t)min(nb * 16 + lr, g.n - 1) * g.pitch + lk;
+#pragma unroll 2
+      for (int k = (wave + AHEAD * kFewWaves) * 128; k < g.pitch; k += kFewWaves * 128) {
+        mfma_i8(acc, *(const i32x4 *)(bp + k), *(const i32x4 *)(ap + k));
+        mfma_i8(acc, *(const i32x4 *)(bp + k + 64), *(const i32x4 *)(ap + k + 64));
+      }
+    }
+    part[buf][wave][lane] = acc;
+    if (nb + (int)gridDim.x < blocks) fetch(nb + gridDim.x);
+    __syncthreads();
+    if (tid < 256) {                              // register e of lane l of every part: row l % 16, column 4 (l / 16) + e
+      const int l = tid >> 2, e = tid & 3, m = l & 15, n = nb * 16 + 4 * (l >> 4) + e;
+      int sum = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < g.n)
-        out[e] = from_f32<TO>(finish<ACT>(s[e], sr, col_scale(g.sb[n + e]), g.bias ? to_f32(((const TO *)g.bias)[n + e]) : 0.f));
+      for (int v = 0; v < kFewWaves; ++v) sum += ((const int *)&part[buf][v][0])[tid];
+      if (m < g.m && n < g.n)
+        ((TO *)g.out)[(int64_t)m * g.out_row + n] =
+            from_f32<TO>(finish<ACT>(sum, sa[m], col_scale(g.sb[n]), g.bias ? to_f32(((const TO *)g.bias)[n]) : 0.f));
+    }
   }
 }
 
-template <typename TO, bool ACT> hipError_t run_few(const I8Args &g, hipStream_t s) {
-  const dim3 block(64 * kFewWaves), cols((g.n + 15) / 16);
-  if (g.m <= 16) hipLaunchKernelGGL((k_i8_few<TO, 1, ACT>), cols, block, 0, s, g);
-  else hipLaunchKernelGGL((k_i8_few<TO, 4, ACT>), dim3(cols.x, (g.m + 63) / 64), block, 0, s, g);
+template <typename T, typename TO, bool ACT> hipError_t run_few(const I8Args &g, hipStream_t s) {
+  const int vec = ((uintptr_t)g.x & 15) == 0 && (g.m == 1 || g.x_row * (int64_t)sizeof(T) % 16 == 0);
+  const int bytes = few_lds(g.m, g.pitch), blocks = (g.n + 15) / 16;
+  auto kern = k_i8_few<T, TO, ACT>;
+  if (bytes > 32768) {
+    static const hipError_t attr = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
+    if (attr != hipSuccess) return attr;
+  }
+  hipLaunchKernelGGL(kern, dim3(blocks < 256 ? blocks : 256), dim3(kFewThreads), bytes, s, g, vec);
   return hipGetLastError();
 }
+bool takes_few(int m, int pitch) { return m <= kFewRows && few_lds(m, pitch) <= kFewLds; }
 
 // ---- many rows ----------------------------------------------------------------------------------
 //
@@ -322,7 +400,7 @@ template <typename TO, bool ACT> hipError_t run_many(I8Args g, hipStream_t s) {
 
 // ---- many short rows, quantised on the way ------------------------------------------------------
 //
-// Rows of up to 1024 elements fit LDS as codes, 128 of them at a time: a workgroup reads its rows of x
+// Rows of up to 1024 elements (fp32: 512, by registers) fit LDS as codes, 128 of them at a time: a workgroup reads its rows of x
 // once, quantises them into the layout of the products' operand and goes through all of the weight, which the
 // L2 holds, 128 rows and 128 bytes of K at a time (a ring of two slots). x is read once and no codes
 // are written or read; the stores of a tile drain beneath the products of the next.
@@ -363,24 +441,31 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g,
 
   {
     const int l8 = lane & 7, nj = g.pitch / 64;   // chunks of 8 elements a lane
-#pragma unroll 1
-    for (int r0 = wave * (kFusedRows / NW); r0 < (wave + 1) * (kFusedRows / NW); r0 += 8) {
-      const int r = r0 + (lane >> 3);
+    constexpr int PASSES = kFusedRows / NW / 8;   // of 8 rows a wave
+    Eight<T> next[NJ];
+    auto fetch = [&](int pass) {
+      const int r = (wave * PASSES + pass) * 8 + (lane >> 3);
       const T *row = (const T *)g.x + (int64_t)min(m0 + r, M - 1) * g.x_row;
-      float y[NJ][8];
-      uint32_t top = 0;
       if (vec_in) {                               // uniform
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) load8<T, true>(y[j], row, (j * 8 + l8) * 8, g.k);
+        for (int j = 0; j < NJ; ++j) load8<T, true>(next[j], row, (j * 8 + l8) * 8, g.k);
       } else {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) load8<T, false>(y[j], row, (j * 8 + l8) * 8, g.k);
+        for (int j = 0; j < NJ; ++j) load8<T, false>(next[j], row, (j * 8 + l8) * 8, g.k);
       }
+    };
+    fetch(0);
+#pragma unroll 1
+    for (int pass = 0; pass < PASSES; ++pass) {
+      const int r = (wave * PASSES + pass) * 8 + (lane >> 3);
+      Eight<T> y[NJ];
+      Top<T> top;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) top = top8(y[j], top);
+      for (int j = 0; j < NJ; ++j) y[j] = next[j];
+      if (pass + 1 < PASSES) fetch(pass + 1);     // in flight meanwhile
 #pragma unroll
-      for (int m = 4; m >= 1; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, kWave));
-      const Scale sc(top);
+      for (int j = 0; j < NJ; ++j) top.take(y[j]);
+      const Scale sc(lanes_top<4>(top.bits()));
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const int e = (j * 8 + l8) * 8, c = (e >> 4) & 7;
@@ -492,7 +577,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g,
 template <typename T, typename TO, bool ACT> hipError_t run_fused(const I8Args &g, hipStream_t s) {
   const int vec = ((uintptr_t)g.x & 15) == 0 && g.x_row * (int64_t)sizeof(T) % 16 == 0, bytes = fused_lds(g.pitch);
   const bool two = bytes <= 80 * 1024;            // two workgroups a compute unit
-  auto kern = two ? k_i8_fused<T, TO, 4, 6, ACT> : g.pitch <= 512 ? k_i8_fused<T, TO, 8, 8, ACT> : k_i8_fused<T, TO, 8, 16, ACT>;
+  auto kern = two ? k_i8_fused<T, TO, 4, 6, ACT> : k_i8_fused<T, TO, 8, 8, ACT>;
+  if constexpr (sizeof(T) == 2)
+    if (g.pitch > 512) kern = k_i8_fused<T, TO, 8, 16, ACT>;
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
@@ -500,31 +587,34 @@ template <typename T, typename TO, bool ACT> hipError_t run_fused(const I8Args &
   hipLaunchKernelGGL(kern, dim3((g.m + kFusedRows - 1) / kFusedRows), dim3(two ? 256 : 512), bytes, s, g, vec);
   return hipGetLastError();
 }
-// Whether rows are quantised on the way.
-bool takes_fused(int x_type, int m, int n, int pitch) { return x_type != MTE_I8_CODES && pitch <= 1024 && m >= 8192; }
+// How a product is done, by its sizes alone: up to 16 rows and many short rows in one launch from rows as they are,
+// others quantised by a launch of their own.
+enum Way { FEW, FUSED, TILES };
+Way way_of(int x_type, int m, int pitch) {
+  if (takes_few(m, pitch)) return FEW;
+  return x_type != MTE_I8_CODES && m >= 8192 && pitch <= (x_type == MTE_BF16 ? 1024 : 512) ? FUSED : TILES;
+}
 
-template <typename TO, bool ACT> hipError_t run(const I8Args &g, hipStream_t s) {
-  return g.m <= 64 ? run_few<TO, ACT>(g, s) : run_many<TO, ACT>(g, s);
+template <typename T, typename TO, bool ACT> hipError_t run_rows(const I8Args &g, Way way, hipStream_t s) {
+  return way == FEW ? run_few<T, TO, ACT>(g, s) : run_fused<T, TO, ACT>(g, s);
+}
+template <typename TO, bool ACT> hipError_t run(const I8Args &g, Way way, int x_type, hipStream_t s) {
+  if (way == TILES) return run_many<TO, ACT>(g, s);
+  if (x_type == MTE_I8_CODES) return run_few<int8_t, TO, ACT>(g, s);
+  return x_type == MTE_BF16 ? run_rows<bf16, TO, ACT>(g, way, s) : run_rows<float, TO, ACT>(g, way, s);
 }
 
 }  // namespace
 
-// Codes and scales of rows that the call quantises itself.
-int64_t i8_workspace(int x_type, int m, int n, int k) {
+// Codes and scales of rows that the call quantises into memory.
+int64_t i8_workspace(int x_type, int m, int, int k) {
   const int64_t pitch = i8_pitch(k);
-  return x_type == MTE_I8_CODES || takes_fused(x_type, m, n, (int)pitch) ? 0 : m * pitch + (int64_t)m * 4;
+  return x_type == MTE_I8_CODES || way_of(x_type, m, (int)pitch) != TILES ? 0 : m * pitch + (int64_t)m * 4;
 }
 
 hipError_t launch_i8_linear(I8Args a, int x_type, int dtype, void *ws, hipStream_t s) {
-  if (takes_fused(x_type, a.m, a.n, a.pitch)) {
-    if (x_type == MTE_BF16) {
-      if (dtype == MTE_BF16) return a.act ? run_fused<bf16, bf16, true>(a, s) : run_fused<bf16, bf16, false>(a, s);
-      return a.act ? run_fused<bf16, float, true>(a, s) : run_fused<bf16, float, false>(a, s);
-    }
-    if (dtype == MTE_BF16) return a.act ? run_fused<float, bf16, true>(a, s) : run_fused<float, bf16, false>(a, s);
-    return a.act ? run_fused<float, float, true>(a, s) : run_fused<float, float, false>(a, s);
-  }
-  if (x_type != MTE_I8_CODES) {
+  const Way way = way_of(x_type, a.m, a.pitch);
+  if (way == TILES && x_type != MTE_I8_CODES) {
     int8_t *codes = (int8_t *)ws;
     float *scales = (float *)(codes + (int64_t)a.m * a.pitch);
     const hipError_t e = launch_i8_quantize(QuantArgs{a.x, codes, scales, a.x_row, a.m, a.k, a.pitch}, x_type, s);
@@ -532,8 +622,8 @@ hipError_t launch_i8_linear(I8Args a, int x_type, int dtype, void *ws, hipStream
     a.a = codes;
     a.sa = scales;
   }
-  if (dtype == MTE_BF16) return a.act ? run<bf16, true>(a, s) : run<bf16, false>(a, s);
-  return a.act ? run<float, true>(a, s) : run<float, false>(a, s);
+  if (dtype == MTE_BF16) return a.act ? run<bf16, true>(a, way, x_type, s) : run<bf16, false>(a, way, x_type, s);
+  return a.act ? run<float, true>(a, way, x_type, s) : run<float, false>(a, way, x_type, s);
 }
 
 }  // namespace mte

@@ -17,13 +17,13 @@ __global__ __launch_bounds__(kThreads) void k_i8_rows(QuantArgs a) {
   const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= a.rows) return;
   const T *row = (const T *)a.x + r * a.x_row;
-  float y[NC][8];
-  uint32_t top = 0;
+  Eight<T> y[NC];
+  Top<T> top;
 #pragma unroll
   for (int j = 0; j < NC; ++j) load8<T, VEC>(y[j], row, (j * 64 + lane) * 8, a.cols);
 #pragma unroll
-  for (int j = 0; j < NC; ++j) top = top8(y[j], top);
-  const Scale sc(wave_top(top));
+  for (int j = 0; j < NC; ++j) top.take(y[j]);
+  const Scale sc(lanes_top<32>(top.bits()));
   int8_t *out = a.codes + r * a.pitch;
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
@@ -40,15 +40,15 @@ __global__ __launch_bounds__(kThreads) void k_i8_long_rows(QuantArgs a) {
   const int tid = threadIdx.x;
   const int64_t r = blockIdx.x;
   const T *row = (const T *)a.x + r * a.x_row;
-  float y[8];
-  uint32_t top = 0;
+  Eight<T> y;
+  Top<T> top;
 #pragma unroll 4
   for (int e = tid * 8; e < a.cols; e += kThreads * 8) {
     load8<T, VEC>(y, row, e, a.cols);
-    top = top8(y, top);
+    top.take(y);
   }
-  top = wave_top(top);
-  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  const uint32_t mine = lanes_top<32>(top.bits());
+  if ((tid & 63) == 0) tops[tid >> 6] = mine;
   __syncthreads();
   const Scale sc(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
   int8_t *out = a.codes + r * a.pitch;

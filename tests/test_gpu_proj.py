@@ -133,7 +133,7 @@ def _check_linear(got, x, w, bias, silu, dtype):
 
 LINEAR = [
     # m, k, n
-    (1, 1, 1), (1, 2048, 2048), (2, 130, 17), (3, 128, 16), (15, 127, 33), (16, 320, 640), (17, 320, 40), (16, 2048, 1283),
+    (1, 1, 1), (1, 2048, 2048), (1, 30000, 37), (1, 100000, 20), (2, 9000, 70), (4, 640, 5000), (7, 3000, 4200), (16, 5000, 33), (16, 6144, 40), (16, 8192, 40), (9, 8192, 9000), (2, 130, 17), (3, 128, 16), (15, 127, 33), (16, 320, 640), (17, 320, 40), (16, 2048, 1283),
     (31, 640, 64), (33, 1001, 129), (64, 2048, 512), (65, 2048, 257), (96, 2048, 1024), (127, 513, 255), (128, 512, 256),
     (129, 129, 257), (200, 6144, 300), (255, 320, 640), (256, 384, 1283), (257, 4096, 1000), (777, 1001, 1283),
     (1030, 320, 640), (1536, 640, 1100), (2049, 300, 77), (300, 20000, 70),
