@@ -45,7 +45,7 @@ extern "C" {
 int64_t mte_i8_pitch(int32_t cols);       /* or MTE_E_INVALID */
 
 /*  x:      device, dtype (MTE_F32 / MTE_BF16), row r at x + r * x_row elements (x_row >= 0);
- *          aligned like one element (16 bytes and strides to match are faster).
+ *          aligned like one element.
  *  codes:  device int8 [rows][mte_i8_pitch(cols)], aligned to 16 bytes; scales: device float[rows].
  * Errors: MTE_E_INVALID, MTE_E_HIP. rows == 0 is MTE_OK. */
 int mte_i8_quantize_rows(const void *x, int64_t x_row, int32_t rows, int32_t cols, int32_t dtype, int8_t *codes,

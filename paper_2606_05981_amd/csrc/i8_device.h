@@ -5,7 +5,9 @@
 
 namespace mte {
 
-// Eight consecutive elements of a row as they lie in memory.
+// Eight consecutive elements of a row as they lie in memory. Rows are aligned like an element: the
+// hardware takes loads of 16 bytes at any such address.
+typedef uint32_t u32x4e __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T> struct Eight;
 template <> struct Eight<bf16> {
   u32x4 w;
@@ -13,7 +15,7 @@ template <> struct Eight<bf16> {
     return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
   }
   __device__ __forceinline__ void zero() { w = u32x4{0, 0, 0, 0}; }
-  __device__ __forceinline__ void load(const bf16 *p) { w = *(const u32x4 *)p; }
+  __device__ __forceinline__ void load(const bf16 *p) { w = *(const u32x4e *)p; }
   __device__ __forceinline__ void set(int i, bf16 x) {
     const uint32_t b = __builtin_bit_cast(uint16_t, x);
     w[i >> 1] |= i & 1 ? b << 16 : b;
@@ -24,8 +26,8 @@ template <> struct Eight<float> {
   __device__ __forceinline__ float get(int i) const { return i < 4 ? a[i] : b[i - 4]; }
   __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ void load(const float *p) {
-    a = *(const f32x4 *)p;
-    b = *(const f32x4 *)(p + 4);
+    a = *(const f32x4u *)p;
+    b = *(const f32x4u *)(p + 4);
   }
   __device__ __forceinline__ void set(int i, float x) {
     if (i < 4) a[i] = x;
@@ -33,17 +35,15 @@ template <> struct Eight<float> {
   }
 };
 
-// Elements e .. e + 7 of a row of cols, zeros past its end. VEC: rows aligned to 16 bytes.
-template <typename T, bool VEC> __device__ __forceinline__ void load8(Eight<T> &y, const T *row, int e, int cols) {
-  if constexpr (VEC) {
-    if (e + 8 <= cols) {
-      y.load(row + e);
-      return;
-    }
+// Elements e .. e + 7 of a row of cols, zeros past its end.
+template <typename T> __device__ __forceinline__ void load8(Eight<T> &y, const T *row, int e, int cols) {
+  if (e + 8 <= cols) {
+    y.load(row + e);
+    return;
   }
   y.zero();
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 7; ++i)
     if (e + i < cols) y.set(i, row[e + i]);
 }
 

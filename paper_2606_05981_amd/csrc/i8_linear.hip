@@ -44,7 +44,7 @@ constexpr int kFewWaves = 16, kFewRows = 16, kFewThreads = 64 * kFewWaves, kFewL
 int few_lds(int m, int pitch) { return m * (pitch + 64); }
 
 template <typename T, typename TO, bool ACT>
-__global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g, int vec_in) {
+__global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
   constexpr int AHEAD = 2;                        // blocks of 128 bytes of K a wave and weight row, ahead
   __shared__ i32x4 part[2][kFewWaves][64];
   __shared__ uint32_t tops[kFewRows];
@@ -83,10 +83,7 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g, int vec_in) {
     constexpr int KEPT = 4;
     Eight<T> y[KEPT];
     Top<T> top;
-    auto read = [&](Eight<T> &z, int c) {
-      if (vec_in) load8<T, true>(z, row, c * 8, g.k);
-      else load8<T, false>(z, row, c * 8, g.k);
-    };
+    auto read = [&](Eight<T> &z, int c) { load8<T>(z, row, c * 8, g.k); };
 #pragma unroll
     for (int j = 0; j < KEPT; ++j) read(y[j], c0 + j * per);
 #pragma unroll
@@ -151,14 +148,13 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g, int vec_in) {
 }
 
 template <typename T, typename TO, bool ACT> hipError_t run_few(const I8Args &g, hipStream_t s) {
-  const int vec = ((uintptr_t)g.x & 15) == 0 && (g.m == 1 || g.x_row * (int64_t)sizeof(T) % 16 == 0);
   const int bytes = few_lds(g.m, g.pitch), blocks = (g.n + 15) / 16;
   auto kern = k_i8_few<T, TO, ACT>;
-  if (bytes > 32768) {
+  if (bytes > 16384) {                            // with the partial sums' 33 KB
     static const hipError_t attr = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
     if (attr != hipSuccess) return attr;
   }
-  hipLaunchKernelGGL(kern, dim3(blocks < 256 ? blocks : 256), dim3(kFewThreads), bytes, s, g, vec);
+  hipLaunchKernelGGL(kern, dim3(blocks < 256 ? blocks : 256), dim3(kFewThreads), bytes, s, g);
   return hipGetLastError();
 }
 bool takes_few(int m, int pitch) { return m <= kFewRows && few_lds(m, pitch) <= kFewLds; }
@@ -410,7 +406,7 @@ constexpr int kFusedRows = 128, kFusedCols = 128, kFusedStage = kFusedRows * kSt
 int fused_lds(int pitch) { return (pitch / kStageBytes + 2) * kFusedStage; }
 
 template <typename T, typename TO, int NW, int NJ, bool ACT>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g, int vec_in) {
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g) {
   constexpr int CH = kStageBytes / 16, WN = NW / 2, WTN = kFusedCols / WN, TM = 4, TN = WTN / 16;
   constexpr int BR = kFusedCols * CH / 64 / NW;   // copies of a wave a stage
   extern __shared__ u32x4 lds[];
@@ -446,13 +442,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g,
     auto fetch = [&](int pass) {
       const int r = (wave * PASSES + pass) * 8 + (lane >> 3);
       const T *row = (const T *)g.x + (int64_t)min(m0 + r, M - 1) * g.x_row;
-      if (vec_in) {                               // uniform
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) load8<T, true>(next[j], row, (j * 8 + l8) * 8, g.k);
-      } else {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) load8<T, false>(next[j], row, (j * 8 + l8) * 8, g.k);
-      }
+      for (int j = 0; j < NJ; ++j) load8<T>(next[j], row, (j * 8 + l8) * 8, g.k);
     };
     fetch(0);
 #pragma unroll 1
@@ -575,7 +566,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g,
 }
 
 template <typename T, typename TO, bool ACT> hipError_t run_fused(const I8Args &g, hipStream_t s) {
-  const int vec = ((uintptr_t)g.x & 15) == 0 && g.x_row * (int64_t)sizeof(T) % 16 == 0, bytes = fused_lds(g.pitch);
+  const int bytes = fused_lds(g.pitch);
   const bool two = bytes <= 80 * 1024;            // two workgroups a compute unit
   auto kern = two ? k_i8_fused<T, TO, 4, 6, ACT> : k_i8_fused<T, TO, 8, 8, ACT>;
   if constexpr (sizeof(T) == 2)
@@ -584,7 +575,7 @@ template <typename T, typename TO, bool ACT> hipError_t run_fused(const I8Args &
     const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((g.m + kFusedRows - 1) / kFusedRows), dim3(two ? 256 : 512), bytes, s, g, vec);
+  hipLaunchKernelGGL(kern, dim3((g.m + kFusedRows - 1) / kFusedRows), dim3(two ? 256 : 512), bytes, s, g);
   return hipGetLastError();
 }
 // How a product is done, by its sizes alone: up to 16 rows and many short rows in one launch from rows as they are,

@@ -11,7 +11,7 @@ namespace {
 constexpr int kThreads = 256;
 
 // A wave a row, NC chunks of 8 elements a lane.
-template <typename T, bool VEC, int NC>
+template <typename T, int NC>
 __global__ __launch_bounds__(kThreads) void k_i8_rows(QuantArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -20,7 +20,7 @@ __global__ __launch_bounds__(kThreads) void k_i8_rows(QuantArgs a) {
   Eight<T> y[NC];
   Top<T> top;
 #pragma unroll
-  for (int j = 0; j < NC; ++j) load8<T, VEC>(y[j], row, (j * 64 + lane) * 8, a.cols);
+  for (int j = 0; j < NC; ++j) load8<T>(y[j], row, (j * 64 + lane) * 8, a.cols);
 #pragma unroll
   for (int j = 0; j < NC; ++j) top.take(y[j]);
   const Scale sc(lanes_top<32>(top.bits()));
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kThreads) void k_i8_rows(QuantArgs a) {
 }
 
 // A workgroup a row.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void k_i8_long_rows(QuantArgs a) {
   __shared__ uint32_t tops[4];
   const int tid = threadIdx.x;
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void k_i8_long_rows(QuantArgs a) {
   Top<T> top;
 #pragma unroll 4
   for (int e = tid * 8; e < a.cols; e += kThreads * 8) {
-    load8<T, VEC>(y, row, e, a.cols);
+    load8<T>(y, row, e, a.cols);
     top.take(y);
   }
   const uint32_t mine = lanes_top<32>(top.bits());
@@ -54,29 +54,26 @@ __global__ __launch_bounds__(kThreads) void k_i8_long_rows(QuantArgs a) {
   int8_t *out = a.codes + r * a.pitch;
 #pragma unroll 4
   for (int e = tid * 8; e < a.pitch; e += kThreads * 8) {
-    load8<T, VEC>(y, row, e, a.cols);
+    load8<T>(y, row, e, a.cols);
     *(u32x2 *)(out + e) = sc.codes(y);
   }
   if (tid == 0) a.scales[r] = sc.stored();
 }
 
-template <typename T, bool VEC> hipError_t run(const QuantArgs &a, hipStream_t s) {
+template <typename T> hipError_t run(const QuantArgs &a, hipStream_t s) {
   const dim3 grid((uint32_t)(((int64_t)a.rows + 3) / 4)), block(kThreads);
-  if (a.pitch <= 512) hipLaunchKernelGGL((k_i8_rows<T, VEC, 1>), grid, block, 0, s, a);
-  else if (a.pitch <= 1024) hipLaunchKernelGGL((k_i8_rows<T, VEC, 2>), grid, block, 0, s, a);
-  else if (a.pitch <= 2048) hipLaunchKernelGGL((k_i8_rows<T, VEC, 4>), grid, block, 0, s, a);
-  else if (a.pitch <= 4096) hipLaunchKernelGGL((k_i8_rows<T, VEC, 8>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_i8_long_rows<T, VEC>), dim3(a.rows), block, 0, s, a);
+  if (a.pitch <= 512) hipLaunchKernelGGL((k_i8_rows<T, 1>), grid, block, 0, s, a);
+  else if (a.pitch <= 1024) hipLaunchKernelGGL((k_i8_rows<T, 2>), grid, block, 0, s, a);
+  else if (a.pitch <= 2048) hipLaunchKernelGGL((k_i8_rows<T, 4>), grid, block, 0, s, a);
+  else if (a.pitch <= 4096) hipLaunchKernelGGL((k_i8_rows<T, 8>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_i8_long_rows<T>), dim3(a.rows), block, 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_i8_quantize(const QuantArgs &a, int dtype, hipStream_t s) {
-  const int64_t es = dtype == MTE_BF16 ? 2 : 4;
-  const bool vec = ((uintptr_t)a.x & 15) == 0 && (a.rows == 1 || a.x_row * es % 16 == 0);
-  if (dtype == MTE_BF16) return vec ? run<bf16, true>(a, s) : run<bf16, false>(a, s);
-  return vec ? run<float, true>(a, s) : run<float, false>(a, s);
+  return dtype == MTE_BF16 ? run<bf16>(a, s) : run<float>(a, s);
 }
 
 }  // namespace mte
