@@ -20,6 +20,11 @@ template <> struct Eight<bf16> {
     const uint32_t b = __builtin_bit_cast(uint16_t, x);
     w[i >> 1] |= i & 1 ? b << 16 : b;
   }
+  // itself, another or zeros
+  __device__ __forceinline__ void keep(bool mine, bool other, const Eight &y) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = mine ? w[i] : other ? y.w[i] : 0u;
+  }
 };
 template <> struct Eight<float> {
   f32x4 a, b;
@@ -33,19 +38,35 @@ template <> struct Eight<float> {
     if (i < 4) a[i] = x;
     else b[i - 4] = x;
   }
+  __device__ __forceinline__ void keep(bool mine, bool other, const Eight &y) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = mine ? a[i] : other ? y.a[i] : 0.f;
+      b[i] = mine ? b[i] : other ? y.b[i] : 0.f;
+    }
+  }
 };
 
-// Elements e .. e + 7 of a row of cols, zeros past its end.
-template <typename T> __device__ __forceinline__ void load8(Eight<T> &y, const T *row, int e, int cols) {
-  if (e + 8 <= cols) {
-    y.load(row + e);
-    return;
-  }
-  y.zero();
+// A row of at least 8 elements in chunks of 8. A load is one instruction in any case, so that many are in flight at
+// once (as a branch each, they were waited for one by one: 128 rows of 320 elements a workgroup, 25 us): past the
+// last whole chunk it repeats that, and keep() puts in what belongs there once it is needed.
+template <typename T> struct RowChunks {
+  const T *row;
+  int full;                                          // elements of whole chunks
+  Eight<T> tail;                                     // the elements after them, then zeros
+  __device__ __forceinline__ void open(const T *r, int cols) {
+    row = r;
+    full = cols & ~7;
+    tail.zero();
+    if (cols & 7) {                                  // uniform
 #pragma unroll
-  for (int i = 0; i < 7; ++i)
-    if (e + i < cols) y.set(i, row[e + i]);
-}
+      for (int i = 0; i < 7; ++i)
+        if (i < (cols & 7)) tail.set(i, row[full + i]);
+    }
+  }
+  __device__ __forceinline__ void load(Eight<T> &y, int e) const { y.load(row + min(e, full - 8)); }
+  __device__ __forceinline__ void keep(Eight<T> &y, int e) const { y.keep(e < full, e == full, tail); }
+};
 
 // The largest magnitude of a lane's elements as the bits of a float (they order like it; NaN lies above infinity).
 template <typename T> struct Top;

@@ -79,18 +79,22 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
     __syncthreads();
     // 1024, 512, .. 64 threads a row
     const int per = kFewThreads >> (g.m > 8 ? 4 : g.m > 4 ? 3 : g.m > 2 ? 2 : g.m > 1 ? 1 : 0), r = tid / per, c0 = tid % per;
-    const T *row = (const T *)g.x + (int64_t)min(r, g.m - 1) * g.x_row;
     constexpr int KEPT = 4;
+    RowChunks<T> row;
     Eight<T> y[KEPT];
     Top<T> top;
-    auto read = [&](Eight<T> &z, int c) { load8<T>(z, row, c * 8, g.k); };
+    row.open((const T *)g.x + (int64_t)min(r, g.m - 1) * g.x_row, g.k);
 #pragma unroll
-    for (int j = 0; j < KEPT; ++j) read(y[j], c0 + j * per);
+    for (int j = 0; j < KEPT; ++j) row.load(y[j], (c0 + j * per) * 8);
 #pragma unroll
-    for (int j = 0; j < KEPT; ++j) top.take(y[j]);
+    for (int j = 0; j < KEPT; ++j) {
+      row.keep(y[j], (c0 + j * per) * 8);
+      top.take(y[j]);
+    }
     for (int c = c0 + KEPT * per; c * 8 < g.k; c += per) {
       Eight<T> z;
-      read(z, c);
+      row.load(z, c * 8);
+      row.keep(z, c * 8);
       top.take(z);
     }
     const uint32_t t = lanes_top<32>(top.bits());  // a wave is within a row
@@ -104,7 +108,8 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
         if ((c0 + j * per) * 8 < g.pitch) *(u32x2 *)(to + (c0 + j * per) * 8) = sc.codes(y[j]);
       for (int c = c0 + KEPT * per; c * 8 < g.pitch; c += per) {
         Eight<T> z;
-        read(z, c);
+        row.load(z, c * 8);
+        row.keep(z, c * 8);
         *(u32x2 *)(to + c * 8) = sc.codes(z);
       }
       if (c0 == 0) sa[r] = row_scale(sc.stored());
@@ -166,8 +171,8 @@ bool takes_few(int m, int pitch) { return m <= kFewRows && few_lds(m, pitch) <= 
 // projections, see gemm_kernel.h: swizzle, one barrier a stage, fragments of the longer side of a wave's tile used by
 // one row of products each and then replaced, those of the shorter side double-buffered). Rows past the
 // last are repeats of it and are not stored.
-// The result goes through LDS, 16 rows of a wave at a time, so that it is stored in whole lines and at any
-// alignment.
+// The result goes through LDS, 16 rows of a wave at a time, so that it is stored in whole lines (at any
+// alignment of an element: the hardware takes it).
 struct I8Tile { int bm, bn, wm, wn, p, occ; double stage_us, tile_us; };
 
 template <typename TO, int BM, int BN, int WM, int WN, int P, int OCC, bool ACT>
@@ -298,7 +303,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) __attribute__((amdgpu_waves_per_
       tc[j][e] = col_scale(g.sb[n]);
       bs[j][e] = g.bias ? to_f32(((const TO *)g.bias)[n]) : 0.f;
     }
-  const bool vec = (((uintptr_t)g.out | (uint64_t)(g.out_row * (int64_t)sizeof(TO))) & 15) == 0 && cw + WTN <= N;   // uniform
+  const bool whole = cw + WTN <= N;               // uniform
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int mb = mw + 16 * i;
@@ -312,12 +317,12 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) __attribute__((amdgpu_waves_per_
       for (int e = 0; e < 4; ++e) y[e] = from_f32<TO>(finish<ACT>(acc[i][j][e], sr, tc[j][e], bs[j][e]));
       *(to4 *)(box + lc * PITCH + (16 * j + 4 * rg) * (int)sizeof(TO)) = y;
     }
-    if (vec) {
+    if (whole) {
 #pragma unroll
       for (int x = 0; x < 16 * CPR / 64; ++x) {
         const int q = x * 64 + lane, r = q / CPR, c = q % CPR;
         const u32x4 v = *(const u32x4 *)(box + r * PITCH + c * 16);
-        if (mb + r < M) *(u32x4 *)((char *)g.out + ((int64_t)(mb + r) * g.out_row + cw) * (int)sizeof(TO) + c * 16) = v;
+        if (mb + r < M) *(u32x4e *)((char *)g.out + ((int64_t)(mb + r) * g.out_row + cw) * (int)sizeof(TO) + c * 16) = v;
       }
     } else {
       for (int q = lane; q < 16 * WTN; q += 64) {
@@ -340,16 +345,22 @@ hipError_t run_tile(const I8Args &g, hipStream_t s) {
   return hipGetLastError();
 }
 
-// bm, bn, waves, ring, workgroups a compute unit; us of a stage and of a tile.
+// bm, bn, waves, ring, workgroups a compute unit; us of a stage and of a tile: least squares over 30 products of 5
+// to 65536 rows, 128 to 6144 deep and 640 to 12288 wide (10 to 18% rms off; the tile they choose is 0.7% slower
+// than the fastest on average, 6% at most). Smaller tiles come two to a compute unit, so that one's products
+// hide the other's stores; the largest read the fewest bytes from LDS for a product (5120 x 2048 x 12288 in 131 us, 1.97 P
+// operations/s, 4096 cubed in 61, 2.25; a library's 147 and 65 without scales).
 #define I8_TILES(X)                                     \
-  X(0, 256, 256, 4, 2, 2, 1, 1.335, 10.86)              \
-  X(1, 192, 384, 2, 4, 2, 1, 1.309, 15.45)              \
-  X(2, 128, 256, 4, 2, 3, 1, 0.754, 7.23)               \
-  X(3, 128, 128, 4, 2, 4, 1, 0.461, 4.42)               \
-  X(4, 96, 128, 2, 4, 4, 1, 0.385, 3.82)                \
-  X(5, 64, 128, 2, 4, 5, 1, 0.300, 3.30)                \
-  X(6, 64, 64, 2, 2, 6, 1, 0.211, 2.29)                 \
-  X(7, 32, 64, 2, 2, 6, 2, 0.196, 1.45)
+  X(0, 256, 256, 4, 2, 2, 1, 0.957, 12.62)              \
+  X(1, 160, 256, 2, 4, 3, 1, 0.714, 8.31)               \
+  X(2, 128, 256, 4, 2, 3, 1, 0.561, 7.97)               \
+  X(3, 192, 128, 2, 2, 2, 2, 0.637, 6.72)               \
+  X(4, 128, 128, 2, 2, 2, 2, 0.576, 4.39)               \
+  X(5, 96, 128, 2, 2, 2, 2, 0.488, 3.69)                \
+  X(6, 64, 128, 2, 2, 3, 2, 0.318, 2.78)                \
+  X(7, 64, 64, 2, 2, 4, 2, 0.204, 1.74)                 \
+  X(8, 32, 64, 2, 2, 6, 2, 0.181, 1.31)                 \
+  X(9, 128, 128, 4, 2, 4, 1, 0.373, 4.19)
 const I8Tile kTiles[] = {
 #define I8_INFO(id, bm, bn, wm, wn, p, occ, su, tu) {bm, bn, wm, wn, p, occ, su, tu},
     I8_TILES(I8_INFO)
@@ -396,160 +407,170 @@ template <typename TO, bool ACT> hipError_t run_many(I8Args g, hipStream_t s) {
 
 // ---- many short rows, quantised on the way ------------------------------------------------------
 //
-// Rows of up to 1024 elements (fp32: 512, by registers) fit LDS as codes, 128 of them at a time: a workgroup reads its rows of x
-// once, quantises them into the layout of the products' operand and goes through all of the weight, which the
-// L2 holds, 128 rows and 128 bytes of K at a time (a ring of two slots). x is read once and no codes
-// are written or read; the stores of a tile drain beneath the products of the next.
+// Rows of up to 384 elements: a workgroup of four waves reads 128 of them once, quantises them through LDS into the
+// operands of its products, 64 rows a wave, which stay in registers, and goes through all of the weight, which the
+// L2 holds, 128 rows and 128 bytes of K at a time. x is read once, and no codes are written or read.
 // Eight lanes a row: a lane takes every eighth chunk of 8 elements, maxima are three exchanges.
-// LDS: nk stages of [128 rows][8 chunks] of codes, two of the weight's, swizzled as the tiles above.
-constexpr int kFusedRows = 128, kFusedCols = 128, kFusedStage = kFusedRows * kStageBytes;
-int fused_lds(int pitch) { return (pitch / kStageBytes + 2) * kFusedStage; }
+// LDS: a ring of five stages of the weight, four ahead of the products; the first three hold the codes
+// before. All copies are waited for before a tile's stores and not after: the stores then
+// drain beneath the next tile's products. They bypass the caches, which hold less than such a result (65536 x 320
+// x 640 38 us against 42). Two workgroups a compute unit.
+constexpr int kFusedRows = 128, kFusedCols = 128, kFusedStage = kFusedRows * kStageBytes, kFusedRing = 5;
 
-template <typename T, typename TO, int NW, int NJ, bool ACT>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g) {
-  constexpr int CH = kStageBytes / 16, WN = NW / 2, WTN = kFusedCols / WN, TM = 4, TN = WTN / 16;
-  constexpr int BR = kFusedCols * CH / 64 / NW;   // copies of a wave a stage
+template <typename T, typename TO, int NK, bool ACT>
+__global__ __launch_bounds__(256, 2) void k_i8_fused(I8Args g) {
+  constexpr int CH = kStageBytes / 16, TM = 4, TN = 4, NJ = 2 * NK, PITCH = NK * kStageBytes;
+  static_assert(NK <= 3, "the codes' slots");
   extern __shared__ u32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int nk = g.pitch / kStageBytes, M = g.m, N = g.n, m0 = blockIdx.x * kFusedRows;
-  const uint32_t ring0 = (uint32_t)nk * kFusedStage;
+  const int M = g.m, N = g.n, m0 = blockIdx.x * kFusedRows;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   char *ldsb = (char *)lds;
-  float *sa = (float *)(ldsb + ring0 + kFusedStage);   // the rows' scales, until the second slot is used
 
-  uint32_t pb[BR];
-  const int8_t *bb = g.b;
-  auto aim = [&](int n0) {                        // at the weight rows of a tile
-    bb = g.b + (int64_t)n0 * g.pitch;
+  // copy c of this wave: 8 rows of the stage
+  uint32_t pr[4], pc[4];
 #pragma unroll
-    for (int c = 0; c < BR; ++c) {
-      const int q = (c * NW + wave) * 64 + lane, r = q / CH;
-      pb[c] = (uint32_t)min(r, N - 1 - n0) * (uint32_t)g.pitch + swz<CH>(r, q % CH) * 16;
-    }
-  };
-  auto copy = [&](int ks, int slot) {
+  for (int c = 0; c < 4; ++c) {
+    const int q = (c * 4 + wave) * 64 + lane;
+    pr[c] = q / CH;
+    pc[c] = swz<CH>(q / CH, q % CH) * 16;
+  }
+  // stage ks of the columns from n0 on into a slot
+  auto copy = [&](int n0, int ks, int slot) {
+    const int8_t *bb = g.b + (int64_t)n0 * PITCH + ks * kStageBytes;
+    const uint32_t last = (uint32_t)min(N - 1 - n0, kFusedCols - 1);
 #pragma unroll
-    for (int c = 0; c < BR; ++c)
-      dma16(bb + ks * kStageBytes, pb[c], lds0 + ring0 + (uint32_t)(slot * kFusedStage + (c * NW + wave) * 1024));
+    for (int c = 0; c < 4; ++c)
+      dma16(bb, min(pr[c], last) * (uint32_t)PITCH + pc[c], lds0 + (uint32_t)(slot * kFusedStage + (c * 4 + wave) * 1024));
   };
-  aim(0);
-  copy(0, 0);
+  auto copy_at = [&](int n0, int t, int slot) {   // t stages after the first of n0
+    const int n = n0 + t / NK * kFusedCols;
+    if (n < N) copy(n, t % NK, slot);
+  };
+  copy_at(0, 0, 3);
+  copy_at(0, 1, 4);
 
+  float rowscale[4];                              // of the rows this lane quantises with its seven neighbours
   {
-    const int l8 = lane & 7, nj = g.pitch / 64;   // chunks of 8 elements a lane
-    constexpr int PASSES = kFusedRows / NW / 8;   // of 8 rows a wave
+    const int l8 = lane & 7;
+    constexpr int PASSES = kFusedRows / 4 / 8;    // of 8 rows a wave
     Eight<T> next[NJ];
+    RowChunks<T> row, ahead;
     auto fetch = [&](int pass) {
       const int r = (wave * PASSES + pass) * 8 + (lane >> 3);
-      const T *row = (const T *)g.x + (int64_t)min(m0 + r, M - 1) * g.x_row;
+      ahead.open((const T *)g.x + (int64_t)min(m0 + r, M - 1) * g.x_row, g.k);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) load8<T>(next[j], row, (j * 8 + l8) * 8, g.k);
+      for (int j = 0; j < NJ; ++j) ahead.load(next[j], (j * 8 + l8) * 8);
     };
     fetch(0);
-#pragma unroll 1
+#pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
       const int r = (wave * PASSES + pass) * 8 + (lane >> 3);
       Eight<T> y[NJ];
       Top<T> top;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) y[j] = next[j];
+      row = ahead;
       if (pass + 1 < PASSES) fetch(pass + 1);     // in flight meanwhile
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) top.take(y[j]);
+      for (int j = 0; j < NJ; ++j) {
+        row.keep(y[j], (j * 8 + l8) * 8);
+        top.take(y[j]);
+      }
       const Scale sc(lanes_top<4>(top.bits()));
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const int e = (j * 8 + l8) * 8, c = (e >> 4) & 7;
-        if (j < nj) *(u32x2 *)(ldsb + (e >> 7) * kFusedStage + (r * CH + swz<CH>(r, c)) * 16 + (e & 8)) = sc.codes(y[j]);
+        *(u32x2 *)(ldsb + (e >> 7) * kFusedStage + (r * CH + swz<CH>(r, c)) * 16 + (e & 8)) = sc.codes(y[j]);
       }
-      if (l8 == 0) sa[r] = row_scale(sc.stored());
+      rowscale[pass] = row_scale(sc.stored());
     }
   }
-
-  const int wm = wave / WN, wn = wave % WN, lc = lane & 15, rg = lane >> 4;
-  uint32_t oa[2], ob[2];
-#pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
-    oa[kk] = (uint32_t)((wm * 64 + lc) * CH + swz<CH>(lc, 4 * kk + rg)) * 16u;
-    ob[kk] = ring0 + (uint32_t)((wn * WTN + lc) * CH + swz<CH>(lc, 4 * kk + rg)) * 16u;
-  }
-  float sr[TM];
   __syncthreads();
+  const int wm = wave >> 1, wn = wave & 1, lc = lane & 15, rg = lane >> 4;
+  i32x4 fa[2 * NK][TM];
+#pragma unroll
+  for (int k = 0; k < 2 * NK; ++k)
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      fa[k][i] = *(const i32x4 *)(ldsb + (k >> 1) * kFusedStage +
+                                  ((wm * 64 + 16 * i + lc) * CH + swz<CH>(lc, 4 * (k & 1) + rg)) * 16);
+  __syncthreads();                                // the codes are read: their slots are free
+  float *sa = (float *)ldsb;
+  if ((lane & 7) == 0) {
+#pragma unroll
+    for (int pass = 0; pass < 4; ++pass) sa[(wave * 4 + pass) * 8 + (lane >> 3)] = rowscale[pass];
+  }
+  __syncthreads();
+  float sr[TM];
 #pragma unroll
   for (int i = 0; i < TM; ++i) sr[i] = sa[wm * 64 + 16 * i + lc];
   __syncthreads();
-  const bool vec = (((uintptr_t)g.out | (uint64_t)(g.out_row * (int64_t)sizeof(TO))) & 15) == 0;   // uniform
-  int slot = 0;
-  bool landed = false;
+  copy_at(0, 2, 0);
+  copy_at(0, 3, 1);
+  uint32_t ob[2];
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) ob[kk] = (uint32_t)((wn * 64 + lc) * CH + swz<CH>(lc, 4 * kk + rg)) * 16u;
+  int slot = 3;
+  wait_vm<0>();
 #pragma unroll 1
   for (int n0 = 0; n0 < N; n0 += kFusedCols) {
+    const int cw = n0 + wn * 64;
     i32x4 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-#pragma unroll 1
-    for (int ks = 0; ks < nk; ++ks) {
-      if (!landed) wait_vm<0>();
-      landed = false;
-      __syncthreads();                            // the stage is whole (first: the codes), and the slot beside it read
-      if (ks + 1 < nk) {
-        copy(ks + 1, slot ^ 1);
-      } else if (n0 + kFusedCols < N) {
-        aim(n0 + kFusedCols);
-        copy(0, slot ^ 1);
-      }
-      const char *pa = ldsb + ks * kFusedStage, *pw = ldsb + slot * kFusedStage;
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) {
+      __syncthreads();                            // this stage is whole (waited for below), the one before it read
+      copy_at(n0, ks + 4, slot == 0 ? kFusedRing - 1 : slot - 1);
+      const char *pw = ldsb + slot * kFusedStage;
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
-        i32x4 fa[TM], fb[TN];
-#pragma unroll
-        for (int i = 0; i < TM; ++i) fa[i] = *(const i32x4 *)(pa + oa[kk] + i * 16 * kStageBytes);
+        i32x4 fb[TN];
 #pragma unroll
         for (int j = 0; j < TN; ++j) fb[j] = *(const i32x4 *)(pw + ob[kk] + j * 16 * kStageBytes);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int j = 0; j < TN; ++j) mfma_i8(acc[i][j], fb[j], fa[i]);
+          for (int j = 0; j < TN; ++j) mfma_i8(acc[i][j], fb[j], fa[2 * ks + kk][i]);
       }
-      slot ^= 1;
+      slot = slot == kFusedRing - 1 ? 0 : slot + 1;
     }
-    // row mw + 16 i + lc, columns cw + 16 j + 4 rg .. + 3
-    const int mw = m0 + wm * 64, cw = n0 + wn * WTN;
-    f32x4 tc[TN], bs[TN];
+    wait_vm<0>();
+    // row m0 + 64 wm + 16 i + lc (past the last row: the last one again), columns cw + 16 j + 4 rg .. + 3
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < TN; j += 2) {
+      f32x4 tc[2], bs[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = min(cw + 16 * j + 4 * rg + e, N - 1);
-        tc[j][e] = col_scale(g.sb[n]);
-        bs[j][e] = g.bias ? to_f32(((const TO *)g.bias)[n]) : 0.f;
-      }
-    wait_vm<0>();                                 // the next stage's copy: before the stores, not behind them
-    landed = true;
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int m = mw + 16 * i + lc;
-      TO *out = (TO *)g.out + (int64_t)m * g.out_row + cw;
+        for (int e = 0; e < 4; ++e) {
+          const int n = min(cw + 16 * (j + u) + 4 * rg + e, N - 1);
+          tc[u][e] = col_scale(g.sb[n]);
+          bs[u][e] = g.bias ? to_f32(((const TO *)g.bias)[n]) : 0.f;
+        }
 #pragma unroll
-      for (int j = 0; j < TN; j += 2) {
+      for (int i = 0; i < TM; ++i) {
+        TO *out = (TO *)g.out + (int64_t)min(m0 + wm * 64 + 16 * i + lc, M - 1) * g.out_row + cw;
         float z[2][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) z[u][e] = finish<ACT>(acc[i][j + u][e], sr[i], tc[j + u][e], bs[j + u][e]);
-        if (vec && cw + WTN <= N) {               // uniform
+          for (int e = 0; e < 4; ++e) z[u][e] = finish<ACT>(acc[i][j + u][e], sr[i], tc[u][e], bs[u][e]);
+        if (cw + 64 <= N) {                       // uniform
           if constexpr (sizeof(TO) == 2) {
             // eight columns a lane: of blocks j and j + 1 the 16-lane rows trade places
             const u32x2 x = __builtin_bit_cast(u32x2, bf16x4{(bf16)z[0][0], (bf16)z[0][1], (bf16)z[0][2], (bf16)z[0][3]});
             const u32x2 y = __builtin_bit_cast(u32x2, bf16x4{(bf16)z[1][0], (bf16)z[1][1], (bf16)z[1][2], (bf16)z[1][3]});
             const auto a = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
             const auto b = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
-            if (m < M) *(u32x4 *)(out + 16 * (j + (rg & 1)) + 8 * (rg >> 1)) = u32x4{a[0], b[0], a[1], b[1]};
+            __builtin_nontemporal_store(u32x4{a[0], b[0], a[1], b[1]}, (u32x4e *)(out + 16 * (j + (rg & 1)) + 8 * (rg >> 1)));
           } else {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-              if (m < M) *(f32x4 *)(out + 16 * (j + u) + 4 * rg) = f32x4{z[u][0], z[u][1], z[u][2], z[u][3]};
+              __builtin_nontemporal_store(f32x4{z[u][0], z[u][1], z[u][2], z[u][3]}, (f32x4u *)(out + 16 * (j + u) + 4 * rg));
           }
         } else {
 #pragma unroll
@@ -557,7 +578,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int c = 16 * (j + u) + 4 * rg + e;
-              if (m < M && cw + c < N) out[c] = from_f32<TO>(z[u][e]);
+              if (cw + c < N) out[c] = from_f32<TO>(z[u][e]);
             }
         }
       }
@@ -566,24 +587,21 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void k_i8_fused(I8Args g)
 }
 
 template <typename T, typename TO, bool ACT> hipError_t run_fused(const I8Args &g, hipStream_t s) {
-  const int bytes = fused_lds(g.pitch);
-  const bool two = bytes <= 80 * 1024;            // two workgroups a compute unit
-  auto kern = two ? k_i8_fused<T, TO, 4, 6, ACT> : k_i8_fused<T, TO, 8, 8, ACT>;
-  if constexpr (sizeof(T) == 2)
-    if (g.pitch > 512) kern = k_i8_fused<T, TO, 8, 16, ACT>;
-  if (bytes > 65536) {
-    const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(kern, dim3((g.m + kFusedRows - 1) / kFusedRows), dim3(two ? 256 : 512), bytes, s, g);
+  constexpr int bytes = kFusedRing * kFusedStage;
+  auto kern = g.pitch == 384 ? k_i8_fused<T, TO, 3, ACT> : g.pitch == 256 ? k_i8_fused<T, TO, 2, ACT> : k_i8_fused<T, TO, 1, ACT>;
+  const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((g.m + kFusedRows - 1) / kFusedRows), dim3(256), bytes, s, g);
   return hipGetLastError();
 }
+
 // How a product is done, by its sizes alone: up to 16 rows and many short rows in one launch from rows as they are,
 // others quantised by a launch of their own.
 enum Way { FEW, FUSED, TILES };
-Way way_of(int x_type, int m, int pitch) {
-  if (takes_few(m, pitch)) return FEW;
-  return x_type != MTE_I8_CODES && m >= 8192 && pitch <= (x_type == MTE_BF16 ? 1024 : 512) ? FUSED : TILES;
+Way way_of(int x_type, int m, int k, int pitch) {
+  const bool whole = x_type == MTE_I8_CODES || k >= 8;   // (RowChunks)
+  if (whole && takes_few(m, pitch)) return FEW;
+  return whole && x_type != MTE_I8_CODES && m >= 32768 && pitch <= 384 ? FUSED : TILES;
 }
 
 template <typename T, typename TO, bool ACT> hipError_t run_rows(const I8Args &g, Way way, hipStream_t s) {
@@ -600,11 +618,11 @@ template <typename TO, bool ACT> hipError_t run(const I8Args &g, Way way, int x_
 // Codes and scales of rows that the call quantises into memory.
 int64_t i8_workspace(int x_type, int m, int, int k) {
   const int64_t pitch = i8_pitch(k);
-  return x_type == MTE_I8_CODES || way_of(x_type, m, (int)pitch) != TILES ? 0 : m * pitch + (int64_t)m * 4;
+  return x_type == MTE_I8_CODES || way_of(x_type, m, k, (int)pitch) != TILES ? 0 : m * pitch + (int64_t)m * 4;
 }
 
 hipError_t launch_i8_linear(I8Args a, int x_type, int dtype, void *ws, hipStream_t s) {
-  const Way way = way_of(x_type, a.m, a.pitch);
+  const Way way = way_of(x_type, a.m, a.k, a.pitch);
   if (way == TILES && x_type != MTE_I8_CODES) {
     int8_t *codes = (int8_t *)ws;
     float *scales = (float *)(codes + (int64_t)a.m * a.pitch);

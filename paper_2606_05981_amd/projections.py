@@ -114,7 +114,7 @@ def i8_linear(x, weight: I8Rows, bias: Optional[torch.Tensor] = None, act: Optio
 
     def call(st):
         y = torch.empty((*lead, n), dtype=dtype, device=dev) if out is None else out
-        _spaced(dev, "mte_i8_linear", x_scales is None and 16 < m < 8192, lambda: B.mte_i8_linear_workspace(x_type, m, k, n),
+        _spaced(dev, "mte_i8_linear", x_scales is None and 16 < m < 32768, lambda: B.mte_i8_linear_workspace(x_type, m, k, n),
                 lambda ws, nb: B.lib.mte_i8_linear(
                     src.data_ptr(), row, None if x_scales is None else x_scales.data_ptr(), x_type, m, k, w.data_ptr(),
                     w_scales.data_ptr(), n, None if bias is None else bias.data_ptr(), _ACT[act], y.data_ptr(), orow,
