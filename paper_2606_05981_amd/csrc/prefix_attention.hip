@@ -110,6 +110,34 @@ __device__ __forceinline__ void add_wild(f32x16 (&o)[ND], const T *vg, int64_t v
   }
 }
 
+// store_part through LDS (`box`, kBox of the wave's own), so that whole lines are written: a lane holds 16 bytes of a row at
+// a time, and as partial lines the parts of a step (18 MB, 64 streams over 16384 tokens) took 9 of its 41 us.
+// left: rows that exist; row: of the unit, this wave's first.
+template <int ND>
+__device__ __forceinline__ void store_part_rows(const AttnCommon &a, Rows<ND> &st, int left, int unit, int g, int row,
+                                                u32x4 *box, int lane) {
+  const float l = st.l + __shfl_xor(st.l, 32, kWave);
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const int r = lane & 31, h = lane >> 5;
+  const int64_t at = ((int64_t)unit * a.hkv + g) * a.ws_rows + row;
+  if (lane < 32 && r < left) *(float2 *)(a.ws + a.ws_ml + (at + r) * 2) = float2{st.m, l};
+  float *to = a.ws + at * (32 * ND);
+#pragma unroll
+  for (int n = 0; n < ND; ++n) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      box[box_at(r, 2 * b + h)] =
+          __builtin_bit_cast(u32x4, f32x4{st.o[n][4 * b] * inv, st.o[n][4 * b + 1] * inv, st.o[n][4 * b + 2] * inv,
+                                          st.o[n][4 * b + 3] * inv});
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int rr = 8 * i + (lane >> 3), c = lane & 7;
+      const u32x4 x = box[box_at(rr, c)];
+      if (rr < left) *(u32x4 *)(to + rr * (32 * ND) + 32 * n + 4 * c) = x;
+    }
+  }
+}
+
 // As k_cross: four waves, 32 RW rows, 4 / RW ways over the keys of a tile.
 template <typename T, int DP, int RW>
 __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
@@ -354,16 +382,13 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_prefix_stream(Pr
                          min((t1 - ks.np) * 32, ks.klen), mine, lane);
   }
   if (r0 >= rows) return;
-  if (span.used > 1 || a.shared) {
-    store_part<ND>(a, st, 1.f, r0 + lrow < rows, a.unit0 + tile, g, 0, wave * 32 + lrow, lane);
-    return;
-  }
   // all slots but the last tile's and the one before hold nothing that is still read
   constexpr int ROOM = S::NB * 2 * S::TILE;
   int free0 = t1 > t0 ? (t1 - t0) % S::NB * 2 * S::TILE : 0;
   free0 += wave * (kBox / 16);
   if (free0 >= ROOM) free0 -= ROOM;
-  store_tile<bf16, ND>(a, st, 1.f, rw, g, lds + free0, lane);
+  if (span.used > 1 || a.shared) store_part_rows<ND>(a, st, rows - r0, a.unit0 + tile, g, wave * 32, lds + free0, lane);
+  else store_tile<bf16, ND>(a, st, 1.f, rw, g, lds + free0, lane);
 }
 
 // ---- joining parts ------------------------------------------------------------------------------
@@ -419,26 +444,30 @@ __global__ __launch_bounds__(kThreads) void k_prefix_join(JoinArgs a) {
   float m = -INFINITY, l = 0.f;
   if (mine) {
     const Parts p = parts_at(a, sq, un.g, r);
-    // four parts at a time, relative to the largest so far
-    for (int s0 = team; s0 < p.n; s0 += 4 * TEAMS) {
-      float ms[4], ls[4];
-      f32x4 x[4];
+    // U parts at a time, relative to the largest so far
+    constexpr int U = 8;
+    for (int s0 = team; s0 < p.n; s0 += U * TEAMS) {
+      float ms[U], ls[U];
+      f32x4 x[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int s = s0 + u * TEAMS;
         const int64_t at = p.place(min(s, p.n - 1));
         ms[u] = s < p.n ? p.ws[p.ml + at * 2] : -INFINITY;
         ls[u] = s < p.n ? p.ws[p.ml + at * 2 + 1] : 0.f;
         x[u] = *(const f32x4 *)(p.ws + at * DP + c);
       }
-      const float top = fmaxf(fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), m), ref = finite_ref(top);
+      float top = m;
+#pragma unroll
+      for (int u = 0; u < U; ++u) top = fmaxf(top, ms[u]);
+      const float ref = finite_ref(top);
       const float f = __builtin_amdgcn_exp2f(m - ref);
       l *= f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] *= f;
       m = top;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < U; ++u) {
         const float w = __builtin_amdgcn_exp2f(ms[u] - ref) * ls[u];
         l += w;
         if (s0 + u * TEAMS < p.n) {
