@@ -552,7 +552,7 @@ Plan prefix_plan(const AttnProblem &p, int p_len, const int32_t *kv_lens) {
   // one pass: as cross attention, tiles of 32 rows where the rows are few
   const bool few = pl.rows_at_once <= 32 || tiles32 * hkv < 256;
   // steps of a row tile over 32 keys, both ways
-  const int TR1 = few ? 32 : 128, TR2 = all <= 32 ? 32 : 128;
+  const int TR1 = few ? 32 : 128, TR2 = all <= 32 && !b16 ? 32 : 128;
   double one = 0, two = (double)ceil_div(all, TR2) * ceil_div(p_len, 32);
   for (int i = 0; i < p.n; ++i) {
     const int64_t rows = (int64_t)p.q_lens[i] * rep;
@@ -564,7 +564,7 @@ Plan prefix_plan(const AttnProblem &p, int p_len, const int32_t *kv_lens) {
   pl.TR = pl.shared ? TR2 : TR1;
   pl.kind = pl.TR == 32 ? Plan::FEW : Plan::MANY;
   pl.KT = pl.kind == Plan::FEW ? 128 : 32;
-  const int least = pl.kind == Plan::FEW ? (b16 ? 2 : 1) : 256 / pl.KT;
+  const int least = pl.kind == Plan::FEW ? (b16 ? 2 : 1) : 128 / pl.KT;
   const int from = pl.kind == Plan::FEW ? (b16 ? 8 : p.c.d > 64 ? 3 : 4) : 0;
   const int np = ceil_div(p_len, pl.KT);
   double work = 0;
