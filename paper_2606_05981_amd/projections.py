@@ -38,6 +38,8 @@ def _matrix(name: str, x):
     row, one = x.stride()
     if k > 1 and one != 1:
         raise ValueError(f"{name}: expected contiguous channels, got strides {x.stride()}")
+    if x.shape[0] >= 1 << 31:                        # (counted in 31 bits)
+        raise ValueError(f"{name}: expected fewer than 2^31 rows, got {x.shape[0]}")
     return x, row if x.shape[0] > 1 else 0
 
 
@@ -53,6 +55,8 @@ def _i8_rows(name: str, t, dev: torch.device):
     if not isinstance(scales, torch.Tensor) or scales.dtype != torch.float32 or scales.device != dev or \
             tuple(scales.shape) != (codes.shape[0],) or not scales.is_contiguous():
         raise ValueError(f"{name} scales: expected a contiguous float32 tensor of {codes.shape[0]} values on {dev}")
+    if codes.shape[0] >= 1 << 31:
+        raise ValueError(f"{name}: expected fewer than 2^31 rows, got {codes.shape[0]}")
     return codes, scales, codes.shape[0], cols
 
 
@@ -171,14 +175,16 @@ def rotary(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, k: Opti
         raise ValueError("q: expected a [tokens, heads, head_dim] bf16 or fp32 tensor on the GPU")
     t, hq, d = q.shape
     dev, dtype = q.device, q.dtype
+    if max(t, hq, d) >= 1 << 31:                     # (counted in 31 bits)
+        raise ValueError(f"q: expected fewer than 2^31 tokens and heads, got shape {tuple(q.shape)}")
     sq, hk, sk = _rows("q", q, dtype, hq, d, dev), 0, (0, 0)
     if k is not None:
         hk = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
         sk = _rows("k", k, dtype, hk, d, dev)
         if k.shape[0] != t:
             raise ValueError(f"k: expected {t} rows, got {k.shape[0]}")
-        if hk == 0:
-            raise ValueError("k: expected at least one head")
+        if not 0 < hk < 1 << 31:
+            raise ValueError(f"k: expected 1 to 2^31 - 1 heads, got {hk}")
     if not isinstance(freq, torch.Tensor) or freq.dtype != torch.float64 or freq.device != dev or freq.dim() != 1 or \
             not 0 < freq.shape[0] <= d // 2 or not freq.is_contiguous():
         raise ValueError(f"freq: expected a contiguous float64 tensor of 1 to {d // 2} values on {dev}")
