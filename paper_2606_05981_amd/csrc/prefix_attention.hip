@@ -509,6 +509,8 @@ __global__ __launch_bounds__(kThreads) void k_prefix_join(JoinArgs a) {
 // ---- host ---------------------------------------------------------------------------------------
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+// Tiles of 32 or 128 (a call's plan counts them a dozen times a sequence: no divisions).
+int tiles_of(int64_t n, int size) { return (int)(size == 32 ? (n + 31) >> 5 : (n + 127) >> 7); }
 int pad_d(int d) { return d <= 64 ? 64 : 128; }
 
 constexpr int kFill = 512;           // workgroups that fill the compute units with two each
@@ -544,7 +546,7 @@ Plan prefix_plan(const AttnProblem &p, int p_len, const int32_t *kv_lens) {
   for (int i = 0; i < p.n; ++i) {
     const int64_t rows = (int64_t)p.q_lens[i] * rep;
     all += rows;
-    tiles32 += ceil_div(rows, 32);
+    tiles32 += tiles_of(rows, 32);
     pl.rows_at_once = std::max(pl.rows_at_once, rows);
   }
   if (all == 0) return pl;
@@ -553,12 +555,12 @@ Plan prefix_plan(const AttnProblem &p, int p_len, const int32_t *kv_lens) {
   const bool few = pl.rows_at_once <= 32 || tiles32 * hkv < 256;
   // steps of a row tile over 32 keys, both ways
   const int TR1 = few ? 32 : 128, TR2 = all <= 32 && !b16 ? 32 : 128;
-  double one = 0, two = (double)ceil_div(all, TR2) * ceil_div(p_len, 32);
+  double one = 0, two = (double)tiles_of(all, TR2) * tiles_of(p_len, 32);
   for (int i = 0; i < p.n; ++i) {
     const int64_t rows = (int64_t)p.q_lens[i] * rep;
     if (rows == 0) continue;
-    one += (double)ceil_div(rows, TR1) * (ceil_div(p_len, 32) + ceil_div(kv_lens[i], 32));
-    two += (double)ceil_div(rows, TR2) * ceil_div(kv_lens[i], 32);
+    one += (double)tiles_of(rows, TR1) * (tiles_of(p_len, 32) + tiles_of(kv_lens[i], 32));
+    two += (double)tiles_of(rows, TR2) * tiles_of(kv_lens[i], 32);
   }
   pl.shared = p_len > 0 && (one - two) * hkv > 2048;
   pl.TR = pl.shared ? TR2 : TR1;
@@ -566,17 +568,17 @@ Plan prefix_plan(const AttnProblem &p, int p_len, const int32_t *kv_lens) {
   pl.KT = pl.kind == Plan::FEW ? 128 : 32;
   const int least = pl.kind == Plan::FEW ? (b16 ? 2 : 1) : 128 / pl.KT;
   const int from = pl.kind == Plan::FEW ? (b16 ? 8 : p.c.d > 64 ? 3 : 4) : 0;
-  const int np = ceil_div(p_len, pl.KT);
+  const int np = tiles_of(p_len, pl.KT);
   double work = 0;
   int longest = 0;
-  const auto list = [&](int i) { return (pl.shared ? 0 : np) + ceil_div(kv_lens[i], pl.KT); };
+  const auto list = [&](int i) { return (pl.shared ? 0 : np) + tiles_of(kv_lens[i], pl.KT); };
   for (int i = 0; i < p.n; ++i)
     if (p.q_lens[i] > 0) {
-      work += (double)ceil_div((int64_t)p.q_lens[i] * rep, pl.TR) * list(i);
+      work += (double)tiles_of((int64_t)p.q_lens[i] * rep, pl.TR) * list(i);
       longest = std::max(longest, list(i));
     }
   if (pl.shared) {
-    pl.p_tiles = ceil_div(all, pl.TR);
+    pl.p_tiles = tiles_of(all, pl.TR);
     work += (double)pl.p_tiles * np;
     pl.p_cut = cut_for(work, hkv, least, 0, np);
     pl.p_parts = parts_of(np, pl.p_cut);
@@ -590,7 +592,7 @@ Plan prefix_plan(const AttnProblem &p, int p_len, const int32_t *kv_lens) {
     const int used = list(i) == 0 ? 0 : parts_of(list(i), pl.cut);
     own = std::max(own, used);
     pl.split |= used > 1;
-    if (used > 1 || pl.shared) at += (int64_t)ceil_div((int64_t)p.q_lens[i] * rep, pl.TR) * used;
+    if (used > 1 || pl.shared) at += (int64_t)tiles_of((int64_t)p.q_lens[i] * rep, pl.TR) * used;
     top = std::max(top, at);
     if (++in == kCondSeqs) in = 0, at = 0;
   }
@@ -608,16 +610,18 @@ template <typename K> hipError_t allow_lds(K kern, int bytes) {
 template <typename T, int DP>
 hipError_t run(PrefixArgs &a, const Plan &pl, bool copies, hipStream_t s) {
   // units of the launch: the prefix's first, then those with partial results, then longest first
-  const int KT = pl.KT;
-  const auto list = [&](const CondSeq &q) {
-    return q.k0 < 0 ? ceil_div(a.p_len, KT) : (pl.shared ? 0 : ceil_div(a.p_len, KT)) + ceil_div(q.k_len, KT);
-  };
-  const auto parts = [&](const CondSeq &q) {
-    const int nt = list(q);
-    return nt == 0 && pl.shared ? 0 : parts_of(nt, q.k0 < 0 ? pl.p_cut : pl.cut);
-  };
-  const auto rank = [&](const CondSeq &q) { return q.k0 < 0 ? INT_MAX : parts(q) > 1 ? INT_MAX - 1 : list(q); };
-  std::stable_sort(a.seq, a.seq + a.n_seq, [&](const CondSeq &x, const CondSeq &y) { return rank(x) > rank(y); });
+  struct Item { int rank, tiles, used, seq; };
+  Item item[kCondSeqs];
+  CondSeq seq[kCondSeqs];
+  const int np = tiles_of(a.p_len, pl.KT);
+  for (int i = 0; i < a.n_seq; ++i) {
+    const CondSeq &q = seq[i] = a.seq[i];
+    const bool alone = q.k0 < 0;
+    const int nt = alone ? np : (pl.shared ? 0 : np) + tiles_of(q.k_len, pl.KT);
+    const int used = nt == 0 && pl.shared ? 0 : parts_of(nt, alone ? pl.p_cut : pl.cut);
+    item[i] = Item{alone ? INT_MAX : used > 1 ? INT_MAX - 1 : nt, tiles_of((int64_t)q.q_len * a.rep, pl.TR), used, i};
+  }
+  std::stable_sort(item, item + a.n_seq, [](const Item &x, const Item &y) { return x.rank > y.rank; });
   JoinArgs j;
   (AttnCommon &)j = a;
   j.p_parts = pl.p_parts;
@@ -626,15 +630,15 @@ hipError_t run(PrefixArgs &a, const Plan &pl, bool copies, hipStream_t s) {
   j.n_seq = 0;
   int units = 0, join_tiles = 0, n = 0;
   for (int i = 0; i < a.n_seq; ++i) {
-    CondSeq q = a.seq[i];
-    const int used = parts(q), tiles = ceil_div((int64_t)q.q_len * a.rep, pl.TR);
+    const Item &it = item[i];
+    CondSeq q = seq[it.seq];
     q.tile0 = units;
-    if (q.k0 >= 0 && (pl.shared || used > 1)) {
-      j.seq[j.n_seq++] = CondSeq{q.q0, q.q_len, a.unit0 + units, used, join_tiles};
-      join_tiles += tiles;
+    if (q.k0 >= 0 && (pl.shared || it.used > 1)) {
+      j.seq[j.n_seq++] = CondSeq{q.q0, q.q_len, a.unit0 + units, it.used, join_tiles};
+      join_tiles += it.tiles;
     }
-    units += tiles * used;
-    if (used > 0) a.seq[n++] = q;                    // (no keys at all: nothing but the join)
+    units += it.tiles * it.used;
+    if (it.used > 0) a.seq[n++] = q;                 // (no keys at all: nothing but the join)
   }
   a.n_seq = n;
   hipError_t e;
