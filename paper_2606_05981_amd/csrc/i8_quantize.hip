@@ -2,6 +2,8 @@
 //
 // Bound by bytes: x is read once, into registers where a row is 4096 elements or fewer (a wave a
 // row); longer rows (a workgroup a row) are read twice, the second time from the caches.
+#include <algorithm>
+
 #include "i8_device.h"
 #include "proj_launch.h"
 
@@ -14,27 +16,27 @@ constexpr int kThreads = 256;
 template <typename T, int NC>
 __global__ __launch_bounds__(kThreads) void k_i8_rows(QuantArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= a.rows) return;
-  RowChunks<T> row;
-  Eight<T> y[NC];
-  row.open((const T *)a.x + r * a.x_row, a.cols);
+  for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += (int64_t)gridDim.x * 4) {
+    RowChunks<T> row;
+    Eight<T> y[NC];
+    row.open((const T *)a.x + r * a.x_row, a.cols);
 #pragma unroll
-  for (int j = 0; j < NC; ++j) row.load(y[j], (j * 64 + lane) * 8);
-  Top<T> top;
+    for (int j = 0; j < NC; ++j) row.load(y[j], (j * 64 + lane) * 8);
+    Top<T> top;
 #pragma unroll
-  for (int j = 0; j < NC; ++j) {
-    row.keep(y[j], (j * 64 + lane) * 8);
-    top.take(y[j]);
+    for (int j = 0; j < NC; ++j) {
+      row.keep(y[j], (j * 64 + lane) * 8);
+      top.take(y[j]);
+    }
+    const Scale sc(lanes_top<32>(top.bits()));
+    int8_t *out = a.codes + r * a.pitch;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int e = (j * 64 + lane) * 8;
+      if (e < a.pitch) *(u32x2 *)(out + e) = sc.codes(y[j]);
+    }
+    if (lane == 0) a.scales[r] = sc.stored();
   }
-  const Scale sc(lanes_top<32>(top.bits()));
-  int8_t *out = a.codes + r * a.pitch;
-#pragma unroll
-  for (int j = 0; j < NC; ++j) {
-    const int e = (j * 64 + lane) * 8;
-    if (e < a.pitch) *(u32x2 *)(out + e) = sc.codes(y[j]);
-  }
-  if (lane == 0) a.scales[r] = sc.stored();
 }
 
 // A workgroup a row, four chunks a lane at a time.
@@ -43,36 +45,38 @@ __global__ __launch_bounds__(kThreads) void k_i8_long_rows(QuantArgs a) {
   constexpr int NC = 4;
   __shared__ uint32_t tops[4];
   const int tid = threadIdx.x;
-  const int64_t r = blockIdx.x;
-  RowChunks<T> row;
-  row.open((const T *)a.x + r * a.x_row, a.cols);
-  Eight<T> y[NC];
-  Top<T> top;
-  for (int e0 = tid * 8; e0 < a.cols; e0 += NC * kThreads * 8) {
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    RowChunks<T> row;
+    row.open((const T *)a.x + r * a.x_row, a.cols);
+    Eight<T> y[NC];
+    Top<T> top;
+    for (int e0 = tid * 8; e0 < a.cols; e0 += NC * kThreads * 8) {
 #pragma unroll
-    for (int j = 0; j < NC; ++j) row.load(y[j], e0 + j * kThreads * 8);
+      for (int j = 0; j < NC; ++j) row.load(y[j], e0 + j * kThreads * 8);
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      row.keep(y[j], e0 + j * kThreads * 8);
-      top.take(y[j]);
+      for (int j = 0; j < NC; ++j) {
+        row.keep(y[j], e0 + j * kThreads * 8);
+        top.take(y[j]);
+      }
     }
-  }
-  const uint32_t mine = lanes_top<32>(top.bits());
-  if ((tid & 63) == 0) tops[tid >> 6] = mine;
-  __syncthreads();
-  const Scale sc(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
-  int8_t *out = a.codes + r * a.pitch;
-  for (int e0 = tid * 8; e0 < a.pitch; e0 += NC * kThreads * 8) {
+    const uint32_t mine = lanes_top<32>(top.bits());
+    if ((tid & 63) == 0) tops[tid >> 6] = mine;
+    __syncthreads();
+    const Scale sc(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+    int8_t *out = a.codes + r * a.pitch;
+    for (int e0 = tid * 8; e0 < a.pitch; e0 += NC * kThreads * 8) {
 #pragma unroll
-    for (int j = 0; j < NC; ++j) row.load(y[j], e0 + j * kThreads * 8);
+      for (int j = 0; j < NC; ++j) row.load(y[j], e0 + j * kThreads * 8);
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int e = e0 + j * kThreads * 8;
-      row.keep(y[j], e);
-      if (e < a.pitch) *(u32x2 *)(out + e) = sc.codes(y[j]);
+      for (int j = 0; j < NC; ++j) {
+        const int e = e0 + j * kThreads * 8;
+        row.keep(y[j], e);
+        if (e < a.pitch) *(u32x2 *)(out + e) = sc.codes(y[j]);
+      }
     }
+    if (tid == 0) a.scales[r] = sc.stored();
+    __syncthreads();                                 // the maxima are read
   }
-  if (tid == 0) a.scales[r] = sc.stored();
 }
 
 // Rows of fewer than 8 elements: a lane a row.
@@ -96,13 +100,15 @@ __global__ __launch_bounds__(kThreads) void k_i8_tiny_rows(QuantArgs a) {
 }
 
 template <typename T> hipError_t run(const QuantArgs &a, hipStream_t s) {
-  const dim3 grid((uint32_t)(((int64_t)a.rows + 3) / 4)), block(kThreads);
+  // (a launch has under 2^32 threads: the kernels go on in strides of the grid)
+  constexpr int64_t kMostGroups = 1 << 22;
+  const dim3 grid((uint32_t)std::min(((int64_t)a.rows + 3) / 4, kMostGroups)), block(kThreads);
   if (a.cols < 8) hipLaunchKernelGGL((k_i8_tiny_rows<T>), dim3((uint32_t)(((int64_t)a.rows + kThreads - 1) / kThreads)), block, 0, s, a);
   else if (a.pitch <= 512) hipLaunchKernelGGL((k_i8_rows<T, 1>), grid, block, 0, s, a);
   else if (a.pitch <= 1024) hipLaunchKernelGGL((k_i8_rows<T, 2>), grid, block, 0, s, a);
   else if (a.pitch <= 2048) hipLaunchKernelGGL((k_i8_rows<T, 4>), grid, block, 0, s, a);
   else if (a.pitch <= 4096) hipLaunchKernelGGL((k_i8_rows<T, 8>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_i8_long_rows<T>), dim3(a.rows), block, 0, s, a);
+  else hipLaunchKernelGGL((k_i8_long_rows<T>), dim3((uint32_t)std::min((int64_t)a.rows, kMostGroups)), block, 0, s, a);
   return hipGetLastError();
 }
 

@@ -131,6 +131,9 @@ int mte_rotary(const mte_rotary_shape *s, const void *q, const void *k, const in
       !aligned(freq, 8))
     return MTE_E_INVALID;
   if (s->n_k_heads > 0 && (!k || !k_out || !aligned(k, 16) || !aligned(k_out, 16))) return MTE_E_INVALID;
+  // in place: the same rows
+  if (q == q_out && (s->q_row != s->qo_row || s->q_head != s->qo_head)) return MTE_E_INVALID;
+  if (s->n_k_heads > 0 && k == k_out && (s->k_row != s->ko_row || s->k_head != s->ko_head)) return MTE_E_INVALID;
   a.q = q;
   a.k = k;
   a.qo = q_out;

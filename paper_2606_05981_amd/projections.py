@@ -46,18 +46,20 @@ def _matrix(name: str, x):
 def _i8_rows(name: str, t, dev: torch.device):
     """Checks 8-bit rows -> (codes, scales, rows, cols)."""
     codes, scales, cols = t
+    try:                                             # one expression: a call is bound by the host
+        n, pitch = codes.shape
+        fits = (codes.dtype is torch.int8 and scales.dtype is torch.float32 and
+                codes.get_device() == scales.get_device() == dev.index and 0 < cols <= B.MTE_I8_COLS and
+                pitch == (cols + 127) & -128 and scales.shape == (n,) and n < 1 << 31 and codes.is_contiguous() and
+                scales.is_contiguous() and codes.data_ptr() % 16 == 0)
+    except (AttributeError, ValueError, TypeError):
+        fits = False
+    if fits:
+        return codes, scales, n, cols
     if not isinstance(cols, int) or not 0 < cols <= B.MTE_I8_COLS:
         raise ValueError(f"{name}: expected 1 to {B.MTE_I8_COLS} channels, got {cols}")
-    if not isinstance(codes, torch.Tensor) or codes.dtype != torch.int8 or codes.dim() != 2 or codes.device != dev or \
-            codes.shape[1] != (cols + 127) // 128 * 128 or not codes.is_contiguous() or codes.data_ptr() % 16:
-        raise ValueError(f"{name} codes: expected a contiguous int8 [rows, {(cols + 127) // 128 * 128}] tensor on {dev}, "
-                         "aligned to 16 bytes")
-    if not isinstance(scales, torch.Tensor) or scales.dtype != torch.float32 or scales.device != dev or \
-            tuple(scales.shape) != (codes.shape[0],) or not scales.is_contiguous():
-        raise ValueError(f"{name} scales: expected a contiguous float32 tensor of {codes.shape[0]} values on {dev}")
-    if codes.shape[0] >= 1 << 31:
-        raise ValueError(f"{name}: expected fewer than 2^31 rows, got {codes.shape[0]}")
-    return codes, scales, codes.shape[0], cols
+    raise ValueError(f"{name}: expected fewer than 2^31 rows as contiguous int8 codes [rows, {(cols + 127) // 128 * 128}], "
+                     f"aligned to 16 bytes, and float32 scales [rows], both on {dev}")
 
 
 def quantize_rows(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> I8Rows:
@@ -117,12 +119,11 @@ def i8_linear(x, weight: I8Rows, bias: Optional[torch.Tensor] = None, act: Optio
             raise ValueError("out: rows overlap")
 
     def call(st):
-        y = torch.empty((*lead, n), dtype=dtype, device=dev) if out is None else out
+        y = w.new_empty((*lead, n), dtype=dtype) if out is None else out
+        args = (src.data_ptr(), row, None if x_scales is None else x_scales.data_ptr(), x_type, m, k, w.data_ptr(),
+                w_scales.data_ptr(), n, None if bias is None else bias.data_ptr(), _ACT[act], y.data_ptr(), orow, _DTYPE[dtype])
         _spaced(dev, "mte_i8_linear", x_scales is None and 16 < m < 32768, lambda: B.mte_i8_linear_workspace(x_type, m, k, n),
-                lambda ws, nb: B.lib.mte_i8_linear(
-                    src.data_ptr(), row, None if x_scales is None else x_scales.data_ptr(), x_type, m, k, w.data_ptr(),
-                    w_scales.data_ptr(), n, None if bias is None else bias.data_ptr(), _ACT[act], y.data_ptr(), orow,
-                    _DTYPE[dtype], ws, nb, st))
+                lambda ws, nb: B.lib.mte_i8_linear(*args, ws, nb, st))
         return y
     return _on(dev, stream, (src, x_scales, w, w_scales, bias, out), call)
 

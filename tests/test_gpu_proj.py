@@ -119,6 +119,17 @@ def test_quantize_strided(torch, P, m, k, wide, skip, dtype):
     _check_rows(P.quantize_rows(x), x)
 
 
+@pytest.mark.parametrize("k", [8, 5, 4100])
+def test_quantize_more_rows_than_a_grid(torch, P, k):
+    """More rows than a launch has workgroups for: the first, some in between and the last."""
+    m = {8: (1 << 24) + 9, 5: (1 << 24) + 9, 4100: (1 << 22) + 3}[k]
+    x = _randn(torch, 1, 1, k).expand(m, k) if k == 4100 else \
+        torch.randn((m, k), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    got = P.quantize_rows(x)
+    at = torch.tensor([0, 1, 4095, m // 2, m - 6, m - 2, m - 1], device="cuda")
+    _check_rows(P.I8Rows(got.codes[at], got.scales[at], k), x[at])
+
+
 # ---- products -----------------------------------------------------------------------------------
 
 

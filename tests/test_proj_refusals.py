@@ -97,6 +97,7 @@ def _rot(B, q=P, k=P, pos=P, axis=64, freq=P, tokens=64, qo=P, ko=P, shape=None,
     (dict(n_axes=3, section=(24, 20, 19, 0)), INVALID), (dict(n_axes=2, section=(65, -1, 0, 0)), INVALID),
     (dict(n_axes=2, section=(2**31 - 1, 2**31 - 1, 0, 0)), INVALID), (dict(n_axes=2, section=(32, 32, 0, 0), axis=-1), INVALID),
     (dict(tokens=-1), INVALID), (dict(tokens=TOP // 24 + 1), INVALID),
+    (dict(qo_row=4096), INVALID), (dict(qo_head=256), INVALID), (dict(ko_row=2048), INVALID),   # in place, other rows
     (dict(q_row=2044), INVALID), (dict(q_head=-8), INVALID), (dict(k_row=4), INVALID), (dict(ko_head=1 << 41), INVALID),
     (dict(q=P + 8), INVALID), (dict(k=P + 2), INVALID), (dict(qo=P + 4), INVALID), (dict(ko=P + 8), INVALID),
     (dict(pos=P + 2), INVALID), (dict(freq=P + 4), INVALID),
