@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * WM * WN, OCC) __attribute__((amdgpu_waves_per_
   // row mw + 16 i + lc, columns cw + 16 j + 4 rg .. + 3
   const int mw = m0 + uwave / WN * WTM, cw = n0 + uwave % WN * WTN;
   if (mw >= M || cw >= N) return;
-  constexpr int PITCH = WTN * (int)sizeof(TO) + 32;
+  constexpr int PITCH = WTN * (int)sizeof(TO) + 16;   // 16 rows on 16 sets of 4 banks
   constexpr int CPR = WTN * (int)sizeof(TO) / 16; // 16-byte chunks of a row
   char *box = (char *)lds + uwave * 16 * PITCH;
   static_assert(NW * 16 * PITCH <= P * STAGE * 16, "room to turn the result");

@@ -21,7 +21,7 @@ template <typename T> struct Vec<T, 1> { typedef T type __attribute__((ext_vecto
 // V: channels of a load. tb: tokens of a workgroup.
 template <typename T, int V, bool INTER>
 __global__ __launch_bounds__(kRotThreads) void k_rotary(RotaryArgs a, int tb) {
-  __shared__ float2 turn[kTableMax];
+  __shared__ __attribute__((aligned(16))) float sines[kTableMax], cosines[kTableMax];
   const int tid = threadIdx.x, pairs = a.rot >> 1;
   const int t0 = blockIdx.x * tb, nt = min(tb, a.tokens - t0);
   for (int i = tid; i < nt * pairs; i += kRotThreads) {
@@ -33,7 +33,8 @@ __global__ __launch_bounds__(kRotThreads) void k_rotary(RotaryArgs a, int tb) {
     const double r = fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, w));
     float s, c;
     sincosf((float)r, &s, &c);
-    turn[i] = float2{s * a.sign, c};
+    sines[i] = s * a.sign;
+    cosines[i] = c;
   }
   __syncthreads();
   // units of a head: of the rotated channels, then of the rest where that is copied. Two units a thread are
@@ -46,7 +47,7 @@ __global__ __launch_bounds__(kRotThreads) void k_rotary(RotaryArgs a, int tb) {
   for (int i0 = tid; i0 < all; i0 += U * kRotThreads) {
     T *to[U];
     vec x1[U], x2[U];
-    int at[U];                                         // of the unit's first pair in `turn`; -1: copied, -2: left
+    int at[U];                                         // of the unit's first pair in the tables; -1: copied, -2: left
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int i = min(i0 + k * kRotThreads, all - 1);
@@ -63,22 +64,20 @@ __global__ __launch_bounds__(kRotThreads) void k_rotary(RotaryArgs a, int tb) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       if (at[k] >= 0) {
-        const float2 *tr = turn + at[k];
+        const float *sn = sines + at[k], *cs = cosines + at[k];
         if constexpr (INTER) {
 #pragma unroll
           for (int e = 0; e < V; e += 2) {
-            const float2 sc = tr[e / 2];
             const float p = to_f32((T)x1[k][e]), q = to_f32((T)x1[k][e + 1]);
-            x1[k][e] = from_f32<T>(a.factor * (p * sc.y - q * sc.x));
-            x1[k][e + 1] = from_f32<T>(a.factor * (q * sc.y + p * sc.x));
+            x1[k][e] = from_f32<T>(a.factor * (p * cs[e / 2] - q * sn[e / 2]));
+            x1[k][e + 1] = from_f32<T>(a.factor * (q * cs[e / 2] + p * sn[e / 2]));
           }
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float2 sc = tr[e];
             const float p = to_f32((T)x1[k][e]), q = to_f32((T)x2[k][e]);
-            x1[k][e] = from_f32<T>(a.factor * (p * sc.y - q * sc.x));
-            x2[k][e] = from_f32<T>(a.factor * (q * sc.y + p * sc.x));
+            x1[k][e] = from_f32<T>(a.factor * (p * cs[e] - q * sn[e]));
+            x2[k][e] = from_f32<T>(a.factor * (q * cs[e] + p * sn[e]));
           }
           *(vec *)(to[k] + pairs) = x2[k];
         }
