@@ -37,7 +37,9 @@ template <bool ACT> __device__ __forceinline__ float finish(int acc, float s, fl
 // turn; its waves share K, 128 bytes of each row at a time, straight from memory to the operands (the next
 // block's loads are in flight meanwhile), and add up through LDS. The rows of a are few enough to lie in LDS
 // whole; every workgroup quantises them for itself, once, while its first weights arrive: a launch less than with
-// codes through memory.
+// codes through memory (1 x 2048 x 2048: 8.4 us replayed, 14.2 called; so 5.3 and 8.7). 16 x 2048 x 12288: 10.7 us, 2.4
+// TB/s, of which launch, quantising and the last sums are about 5; 4 x 6144 x 12288: 20 us, 3.7 TB/s. Three blocks of weights
+// ahead instead of one change nothing.
 // LDS: rows of codes 64 bytes further apart than they are long, so that an operand's 16 rows of 64 bytes
 // fill the banks.
 constexpr int kFewWaves = 16, kFewRows = 16, kFewThreads = 64 * kFewWaves, kFewLds = 96 * 1024;
@@ -171,6 +173,8 @@ bool takes_few(int m, int pitch) { return m <= kFewRows && few_lds(m, pitch) <= 
 // projections, see gemm_kernel.h: swizzle, one barrier a stage, fragments of the longer side of a wave's tile used by
 // one row of products each and then replaced, those of the shorter side double-buffered). Rows past the
 // last are repeats of it and are not stored.
+// Bound by the matrix cores where K is long, else by prologue and epilogue, which nothing overlaps in the larger tiles
+// (5120 x 2048 x 12288: busy 51 of 131 us; SiLU, two quarter-rate instructions an element, makes them 139).
 // The result goes through LDS, 16 rows of a wave at a time, so that it is stored in whole lines (at any
 // alignment of an element: the hardware takes it).
 struct I8Tile { int bm, bn, wm, wn, p, occ; double stage_us, tile_us; };
@@ -415,6 +419,10 @@ template <typename TO, bool ACT> hipError_t run_many(I8Args g, hipStream_t s) {
 // before. All copies are waited for before a tile's stores and not after: the stores then
 // drain beneath the next tile's products. They bypass the caches, which hold less than such a result (65536 x 320
 // x 640 38 us against 42). Two workgroups a compute unit.
+// Bound by the rows in and out, one after the other: all workgroups quantise first (about 10 us) and store then (126
+// MB in 38 us, 3.3 TB/s; codes through memory 62). From 32768 rows on: a workgroup alone takes 25 us (32768 x 320 x
+// 320 the same 28 either way, 16384 x 320 x 640 32 against 21). With the codes in LDS instead of registers, or rows of
+// up to 1024 that way, it was slower than through memory from 640 elements on (65536 x 640 x 640: 96 against 82).
 constexpr int kFusedRows = 128, kFusedCols = 128, kFusedStage = kFusedRows * kStageBytes, kFusedRing = 5;
 
 template <typename T, typename TO, int NK, bool ACT>

