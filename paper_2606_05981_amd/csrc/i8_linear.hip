@@ -31,7 +31,7 @@ template <bool ACT> __device__ __forceinline__ float finish(int acc, float s, fl
   return z;
 }
 
-// ---- up to 16 rows ------------------------------------------------------------------------------
+// ---- up to 32 rows ------------------------------------------------------------------------------
 //
 // Bound by the bytes of the weight, or by latency. A workgroup of 16 waves takes blocks of 16 weight rows in
 // turn; its waves share K, 128 bytes of each row at a time, straight from memory to the operands (the next
@@ -42,13 +42,14 @@ template <bool ACT> __device__ __forceinline__ float finish(int acc, float s, fl
 // ahead instead of one change nothing.
 // LDS: rows of codes 64 bytes further apart than they are long, so that an operand's 16 rows of 64 bytes
 // fill the banks.
-constexpr int kFewWaves = 16, kFewRows = 16, kFewThreads = 64 * kFewWaves, kFewLds = 96 * 1024;
+constexpr int kFewWaves = 16, kFewRows = 32, kFewThreads = 64 * kFewWaves, kFewLds = 95 * 1024;
 int few_lds(int m, int pitch) { return m * (pitch + 64); }
 
-template <typename T, typename TO, bool ACT>
+// MT: blocks of 16 rows of a.
+template <typename T, typename TO, bool ACT, int MT>
 __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
   constexpr int AHEAD = 2;                        // blocks of 128 bytes of K a wave and weight row, ahead
-  __shared__ i32x4 part[2][kFewWaves][64];
+  __shared__ i32x4 part[2][kFewWaves][MT][64];
   __shared__ uint32_t tops[kFewRows];
   __shared__ float sa[kFewRows];
   extern __shared__ u32x4 lds[];
@@ -79,9 +80,10 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
   } else {
     if (tid < kFewRows) tops[tid] = 0;
     __syncthreads();
-    // 1024, 512, .. 64 threads a row
-    const int per = kFewThreads >> (g.m > 8 ? 4 : g.m > 4 ? 3 : g.m > 2 ? 2 : g.m > 1 ? 1 : 0), r = tid / per, c0 = tid % per;
-    constexpr int KEPT = 4;
+    // 1024, 512, .. 64 threads a row; MT 2: 32
+    const int per = MT == 2 ? 32 : kFewThreads >> (g.m > 8 ? 4 : g.m > 4 ? 3 : g.m > 2 ? 2 : g.m > 1 ? 1 : 0);
+    const int r = tid / per, c0 = tid % per;
+    constexpr int KEPT = 4 * MT;
     RowChunks<T> row;
     Eight<T> y[KEPT];
     Top<T> top;
@@ -99,8 +101,8 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
       row.keep(z, c * 8);
       top.take(z);
     }
-    const uint32_t t = lanes_top<32>(top.bits());  // a wave is within a row
-    if (lane == 0) atomicMax(&tops[r], t);
+    const uint32_t t = lanes_top<MT == 2 ? 16 : 32>(top.bits());   // a wave, or half of one, is within a row
+    if (lane % (MT == 2 ? 32 : 64) == 0) atomicMax(&tops[r], t);
     __syncthreads();
     const Scale sc(tops[r]);
     if (r < g.m) {
@@ -119,34 +121,41 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
   }
   __syncthreads();
 
-  const char *ap = codes + min(lr, g.m - 1) * row_bytes + lk;
+  const char *ap[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) ap[t] = codes + min(16 * t + lr, g.m - 1) * row_bytes + lk;
   int buf = 0;
   for (int nb = blockIdx.x; nb < blocks; nb += gridDim.x, buf ^= 1) {
-    i32x4 acc{0, 0, 0, 0};
+    i32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = i32x4{0, 0, 0, 0};
+    auto add = [&](const i32x4 &x, const i32x4 &y, int k) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        mfma_i8(acc[t], x, *(const i32x4 *)(ap[t] + k));
+        mfma_i8(acc[t], y, *(const i32x4 *)(ap[t] + k + 64));
+      }
+    };
 #pragma unroll
     for (int b = 0; b < AHEAD; ++b) {
       const int k = (wave + b * kFewWaves) * 128;
-      if (k < g.pitch) {
-        mfma_i8(acc, w[2 * b], *(const i32x4 *)(ap + k));
-        mfma_i8(acc, w[2 * b + 1], *(const i32x4 *)(ap + k + 64));
-      }
+      if (k < g.pitch) add(w[2 * b], w[2 * b + 1], k);
     }
     if (g.pitch > AHEAD * kFewWaves * 128) {      // long rows: the rest
       const int8_t *bp = g.b + (int64_t)min(nb * 16 + lr, g.n - 1) * g.pitch + lk;
 #pragma unroll 2
-      for (int k = (wave + AHEAD * kFewWaves) * 128; k < g.pitch; k += kFewWaves * 128) {
-        mfma_i8(acc, *(const i32x4 *)(bp + k), *(const i32x4 *)(ap + k));
-        mfma_i8(acc, *(const i32x4 *)(bp + k + 64), *(const i32x4 *)(ap + k + 64));
-      }
+      for (int k = (wave + AHEAD * kFewWaves) * 128; k < g.pitch; k += kFewWaves * 128)
+        add(*(const i32x4 *)(bp + k), *(const i32x4 *)(bp + k + 64), k);
     }
-    part[buf][wave][lane] = acc;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) part[buf][wave][t][lane] = acc[t];
     if (nb + (int)gridDim.x < blocks) fetch(nb + gridDim.x);
     __syncthreads();
-    if (tid < 256) {                              // register e of lane l of every part: row l % 16, column 4 (l / 16) + e
-      const int l = tid >> 2, e = tid & 3, m = l & 15, n = nb * 16 + 4 * (l >> 4) + e;
+    if (tid < 256 * MT) {                         // register e of lane l of every part: row l % 16, column 4 (l / 16) + e
+      const int l = tid >> 2 & 63, e = tid & 3, m = (tid >> 8) * 16 + (l & 15), n = nb * 16 + 4 * (l >> 4) + e;
       int sum = 0;
 #pragma unroll
-      for (int v = 0; v < kFewWaves; ++v) sum += ((const int *)&part[buf][v][0])[tid];
+      for (int v = 0; v < kFewWaves; ++v) sum += ((const int *)&part[buf][v][0][0])[tid];
       if (m < g.m && n < g.n)
         ((TO *)g.out)[(int64_t)m * g.out_row + n] =
             from_f32<TO>(finish<ACT>(sum, sa[m], col_scale(g.sb[n]), g.bias ? to_f32(((const TO *)g.bias)[n]) : 0.f));
@@ -154,17 +163,25 @@ __global__ __launch_bounds__(kFewThreads) void k_i8_few(I8Args g) {
   }
 }
 
-template <typename T, typename TO, bool ACT> hipError_t run_few(const I8Args &g, hipStream_t s) {
-  const int bytes = few_lds(g.m, g.pitch), blocks = (g.n + 15) / 16;
-  auto kern = k_i8_few<T, TO, ACT>;
-  if (bytes > 16384) {                            // with the partial sums' 33 KB
-    static const hipError_t attr = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
-    if (attr != hipSuccess) return attr;
-  }
-  hipLaunchKernelGGL(kern, dim3(blocks < 256 ? blocks : 256), dim3(kFewThreads), bytes, s, g);
+template <typename T, typename TO, bool ACT, int MT> hipError_t launch_few(const I8Args &g, hipStream_t s) {
+  const int blocks = (g.n + 15) / 16;
+  auto kern = k_i8_few<T, TO, ACT, MT>;
+  static const hipError_t attr = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL(kern, dim3(blocks < 256 ? blocks : 256), dim3(kFewThreads), few_lds(g.m, g.pitch), s, g);
   return hipGetLastError();
 }
-bool takes_few(int m, int pitch) { return m <= kFewRows && few_lds(m, pitch) <= kFewLds; }
+template <typename T, typename TO, bool ACT> hipError_t run_few(const I8Args &g, hipStream_t s) {
+  return g.m <= 16 ? launch_few<T, TO, ACT, 1>(g, s) : launch_few<T, TO, ACT, 2>(g, s);
+}
+// 17 to 32 rows: where every workgroup has one block of columns, and rows that it quantises itself are short,
+// since all of them repeat that (us replayed / called, against tiles; 32 x 640 x 2048: 6.8 / 9.3, 7.5 / 13.9;
+// 32 x 2048 x 2048: 10.6 / 10.6, 10.7 / 13.9, of codes 4.8 against 6.1; 32 x 2048 x 8192: 13.6 / 13.5, 10.9 / 13.7;
+// 32 x 2944 x 2048: 16.2 / 15.9, 13.3 / 13.8, of codes 5.6 against 7.3).
+bool takes_few(int m, int pitch, int n, bool codes) {
+  if (m > kFewRows || few_lds(m, pitch) > kFewLds) return false;
+  return m <= 16 || (n <= 16 * 256 && (codes || pitch <= 2048));
+}
 
 // ---- many rows ----------------------------------------------------------------------------------
 //
@@ -603,12 +620,12 @@ template <typename T, typename TO, bool ACT> hipError_t run_fused(const I8Args &
   return hipGetLastError();
 }
 
-// How a product is done, by its sizes alone: up to 16 rows and many short rows in one launch from rows as they are,
+// How a product is done, by its sizes alone: few rows and many short rows in one launch from rows as they are,
 // others quantised by a launch of their own.
 enum Way { FEW, FUSED, TILES };
-Way way_of(int x_type, int m, int k, int pitch) {
+Way way_of(int x_type, int m, int n, int k, int pitch) {
   const bool whole = x_type == MTE_I8_CODES || k >= 8;   // (RowChunks)
-  if (whole && takes_few(m, pitch)) return FEW;
+  if (whole && takes_few(m, pitch, n, x_type == MTE_I8_CODES)) return FEW;
   return whole && x_type != MTE_I8_CODES && m >= 32768 && pitch <= 384 ? FUSED : TILES;
 }
 
@@ -624,13 +641,13 @@ template <typename TO, bool ACT> hipError_t run(const I8Args &g, Way way, int x_
 }  // namespace
 
 // Codes and scales of rows that the call quantises into memory.
-int64_t i8_workspace(int x_type, int m, int, int k) {
+int64_t i8_workspace(int x_type, int m, int n, int k) {
   const int64_t pitch = i8_pitch(k);
-  return x_type == MTE_I8_CODES || way_of(x_type, m, k, (int)pitch) != TILES ? 0 : m * pitch + (int64_t)m * 4;
+  return x_type == MTE_I8_CODES || way_of(x_type, m, n, k, (int)pitch) != TILES ? 0 : m * pitch + (int64_t)m * 4;
 }
 
 hipError_t launch_i8_linear(I8Args a, int x_type, int dtype, void *ws, hipStream_t s) {
-  const Way way = way_of(x_type, a.m, a.k, a.pitch);
+  const Way way = way_of(x_type, a.m, a.n, a.k, a.pitch);
   if (way == TILES && x_type != MTE_I8_CODES) {
     int8_t *codes = (int8_t *)ws;
     float *scales = (float *)(codes + (int64_t)a.m * a.pitch);

@@ -122,7 +122,7 @@ def i8_linear(x, weight: I8Rows, bias: Optional[torch.Tensor] = None, act: Optio
         y = w.new_empty((*lead, n), dtype=dtype) if out is None else out
         args = (src.data_ptr(), row, None if x_scales is None else x_scales.data_ptr(), x_type, m, k, w.data_ptr(),
                 w_scales.data_ptr(), n, None if bias is None else bias.data_ptr(), _ACT[act], y.data_ptr(), orow, _DTYPE[dtype])
-        _spaced(dev, "mte_i8_linear", x_scales is None and 16 < m < 32768, lambda: B.mte_i8_linear_workspace(x_type, m, k, n),
+        _spaced(dev, "mte_i8_linear", x_scales is None and 32 < m < 32768, lambda: B.mte_i8_linear_workspace(x_type, m, k, n),
                 lambda ws, nb: B.lib.mte_i8_linear(*args, ws, nb, st))
         return y
     return _on(dev, stream, (src, x_scales, w, w_scales, bias, out), call)

@@ -145,7 +145,7 @@ def _check_linear(got, x, w, bias, silu, dtype):
 LINEAR = [
     # m, k, n
     (1, 1, 1), (5, 7, 20), (16, 8, 5), (3, 9, 70), (40, 3, 9), (8200, 5, 40), (33000, 8, 40), (33000, 7, 9), (1, 2048, 2048), (1, 30000, 37), (1, 100000, 20), (2, 9000, 70), (4, 640, 5000), (7, 3000, 4200), (16, 5000, 33), (16, 6144, 40), (16, 8192, 40), (9, 8192, 9000), (2, 130, 17), (3, 128, 16), (15, 127, 33), (16, 320, 640), (17, 320, 40), (16, 2048, 1283),
-    (31, 640, 64), (33, 1001, 129), (64, 2048, 512), (65, 2048, 257), (96, 2048, 1024), (127, 513, 255), (128, 512, 256),
+    (17, 2048, 4096), (17, 2048, 4097), (32, 2048, 40), (20, 2900, 70), (24, 3100, 40), (32, 2944, 33), (32, 8, 1), (31, 640, 64), (33, 1001, 129), (64, 2048, 512), (65, 2048, 257), (96, 2048, 1024), (127, 513, 255), (128, 512, 256),
     (129, 129, 257), (200, 6144, 300), (255, 320, 640), (256, 384, 1283), (257, 4096, 1000), (777, 1001, 1283),
     (1030, 320, 640), (1536, 640, 1100), (2049, 300, 77), (300, 20000, 70),
     # many short rows
@@ -168,7 +168,7 @@ def test_linear(torch, P, m, k, n, dtype):
 
 
 @pytest.mark.parametrize("out_dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("m,k,n", [(1, 2048, 640), (40, 640, 130), (300, 1000, 515)])
+@pytest.mark.parametrize("m,k,n", [(1, 2048, 640), (30, 1500, 90), (32, 2944, 33), (40, 640, 130), (300, 1000, 515)])
 def test_linear_of_codes(torch, P, m, k, n, out_dtype):
     """Tokens quantised once for several layers, both result types; the largest sums (all codes -128 or 127)."""
     g = torch.Generator().manual_seed(7)
@@ -221,7 +221,7 @@ def test_linear_batch_invariant(torch, P):
     x, w = _randn(torch, 1, 33000, 320, std=2.0), _randn(torch, 2, 330, 320, std=0.05)
     weight, b = P.quantize_rows(w), _randn(torch, 3, 330)
     whole = P.i8_linear(x, weight, b, act="silu")
-    for a, e in ((0, 1), (3, 17), (5, 69), (100, 400), (7, 32900)):
+    for a, e in ((0, 1), (3, 17), (6, 30), (5, 69), (100, 400), (7, 32900)):
         assert torch.equal(P.i8_linear(x[a:e], weight, b, act="silu"), whole[a:e])
     assert torch.equal(P.i8_linear(P.quantize_rows(x), weight, b, act="silu"), whole)
 
