@@ -11,6 +11,10 @@ namespace mte {
 // arguments are at most 4 KB); more sequences take several launches.
 constexpr int kCondSeqs = 128;
 
+// Workgroups of a launch, of 512 threads or fewer: a launch counts its threads in 32 bits, and drops
+// those beyond without an error.
+constexpr int kMostGroups = 1 << 22;
+
 struct CondSeq {
   int q0, q_len;   // first packed query (or appended / read) row, rows
   int k0, k_len;   // first packed key row, key rows; the cache operators: row of the block table; attention

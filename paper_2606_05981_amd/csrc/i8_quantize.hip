@@ -101,15 +101,14 @@ __global__ __launch_bounds__(kThreads) void k_i8_tiny_rows(QuantArgs a) {
 }
 
 template <typename T> hipError_t run(const QuantArgs &a, hipStream_t s) {
-  // (a launch has under 2^32 threads: the kernels go on in strides of the grid)
-  constexpr int64_t kMostGroups = 1 << 22;
-  const dim3 grid((uint32_t)std::min(((int64_t)a.rows + 3) / 4, kMostGroups)), block(kThreads);
+  // (the kernels go on in strides of the grid)
+  const dim3 grid((uint32_t)std::min<int64_t>(((int64_t)a.rows + 3) / 4, kMostGroups)), block(kThreads);
   if (a.cols < 8) hipLaunchKernelGGL((k_i8_tiny_rows<T>), dim3((uint32_t)(((int64_t)a.rows + kThreads - 1) / kThreads)), block, 0, s, a);
   else if (a.pitch <= 512) hipLaunchKernelGGL((k_i8_rows<T, 1>), grid, block, 0, s, a);
   else if (a.pitch <= 1024) hipLaunchKernelGGL((k_i8_rows<T, 2>), grid, block, 0, s, a);
   else if (a.pitch <= 2048) hipLaunchKernelGGL((k_i8_rows<T, 4>), grid, block, 0, s, a);
   else if (a.pitch <= 4096) hipLaunchKernelGGL((k_i8_rows<T, 8>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_i8_long_rows<T>), dim3((uint32_t)std::min((int64_t)a.rows, kMostGroups)), block, 0, s, a);
+  else hipLaunchKernelGGL((k_i8_long_rows<T>), dim3((uint32_t)std::min(a.rows, kMostGroups)), block, 0, s, a);
   return hipGetLastError();
 }
 

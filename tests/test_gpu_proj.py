@@ -335,6 +335,24 @@ def test_rotary_in_place_and_strided(torch, P, inter, dtype):
     assert torch.equal(hq_major.transpose(0, 1), q) and torch.equal(hk_major.transpose(0, 1), k)
 
 
+@pytest.mark.parametrize("inter,heads", [(False, 3), (True, 6)])
+def test_rotary_more_workgroups_than_a_grid(torch, P, inter, heads):
+    """A token a workgroup, 2^24 of them and a few more: one token's queries and keys for all, turned by positions of
+    its own (the second axis's)."""
+    t, d = (1 << 24) + 5, 344
+    if torch.cuda.mem_get_info()[0] < t * heads * d * 2 + (4 << 30):
+        pytest.skip("needs the memory of a whole MI355X")
+    q, k = (_randn(torch, h, 1, h, d).expand(t, h, d) for h in (heads - 1, 1))
+    pos = torch.stack([torch.zeros(t, dtype=torch.int32, device="cuda"), torch.arange(t, dtype=torch.int32, device="cuda")])
+    freq, kw = _freq(P, 1), dict(interleaved=inter, sections=(0, 1))
+    got = P.rotary(q, pos, freq, k=k, **kw)
+    at = torch.tensor([0, 1, (1 << 22) - 1, 1 << 22, (1 << 23) + 3, t - 6, t - 5, t - 1], device="cuda")
+    for x, y in zip((q, k), got):
+        _check_rotary(y[at], x[:len(at)], pos[:, at], freq, "bf16", **kw)
+    del got, y
+    torch.cuda.empty_cache()
+
+
 def test_rotary_inverse_is_the_gradient(torch, P):
     """Turning back undoes a turn, and is the gradient: <R x, g> = <x, R^-1 g>, also against differences."""
     t, h, d, pairs = 12, 3, 40, 15
