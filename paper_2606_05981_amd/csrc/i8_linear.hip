@@ -4,6 +4,7 @@
 // rate of 16-bit floating point for the same bytes of operands. Codes are rows of a multiple of
 // 128 bytes, so that a K stage is 128 bytes of every row and there is no ragged end of K.
 // C^T = B A^T: a lane then holds four consecutive columns of one row of the result.
+#include <algorithm>
 #include <cmath>
 
 #include "gemm_kernel.h"
@@ -410,13 +411,7 @@ int pick_tile(int m, int n, int pitch) {
   return best;
 }
 
-template <typename TO, bool ACT> hipError_t run_many(I8Args g, hipStream_t s) {
-  const int id = pick_tile(g.m, g.n, g.pitch);
-  g.gm = (g.m + kTiles[id].bm - 1) / kTiles[id].bm;
-  g.gn = (g.n + kTiles[id].bn - 1) / kTiles[id].bn;
-  // an XCD's 32 tiles at a time as a block: about as many rows of a as of b
-  g.gh = 1;
-  while (g.gh < g.gm && g.gh * kTiles[id].bm < 6 * kTiles[id].bn) ++g.gh;
+template <typename TO, bool ACT> hipError_t run_tiles(const I8Args &g, int id, hipStream_t s) {
   switch (id) {
 #define I8_CASE(idv, bm, bn, wm, wn, p, occ, su, tu) \
   case idv: return run_tile<TO, ACT, bm, bn, wm, wn, p, occ>(g, s);
@@ -424,6 +419,31 @@ template <typename TO, bool ACT> hipError_t run_many(I8Args g, hipStream_t s) {
 #undef I8_CASE
   }
   return hipErrorInvalidValue;
+}
+template <typename TO, bool ACT> hipError_t run_many(const I8Args &all, hipStream_t s) {
+  const int id = pick_tile(all.m, all.n, all.pitch), bm = kTiles[id].bm, bn = kTiles[id].bn;
+  // in launches of kMostGroups tiles: columns, and rows of them
+  const int64_t cols = std::min<int64_t>((all.n + bn - 1) / bn, kMostGroups), rows = kMostGroups / cols;
+  for (int64_t n0 = 0; n0 < all.n; n0 += cols * bn)
+    for (int64_t m0 = 0; m0 < all.m; m0 += rows * bm) {
+      I8Args g = all;
+      g.m = (int)std::min(all.m - m0, rows * bm);
+      g.n = (int)std::min(all.n - n0, cols * bn);
+      g.a += m0 * g.pitch;
+      g.sa += m0;
+      g.b += n0 * g.pitch;
+      g.sb += n0;
+      if (g.bias) g.bias = (const TO *)g.bias + n0;
+      g.out = (TO *)g.out + m0 * g.out_row + n0;
+      g.gm = (g.m + bm - 1) / bm;
+      g.gn = (g.n + bn - 1) / bn;
+      // an XCD's 32 tiles at a time as a block: about as many rows of a as of b
+      g.gh = 1;
+      while (g.gh < g.gm && g.gh * bm < 6 * bn) ++g.gh;
+      const hipError_t e = run_tiles<TO, ACT>(g, id, s);
+      if (e != hipSuccess) return e;
+    }
+  return hipSuccess;
 }
 
 // ---- many short rows, quantised on the way ------------------------------------------------------

@@ -216,6 +216,36 @@ def test_linear_strides(torch, P, m, dtype):
         assert torch.equal(y.view(m, n), P.i8_linear(x, weight))
 
 
+def test_linear_more_tiles_than_a_grid(torch, P):
+    """More tiles of 64 rows than a launch takes workgroups for, 2^24; rows that overlap in memory, so that what is large
+    are the codes that the call makes."""
+    m, k = (1 << 30) + 70, 5
+    if torch.cuda.mem_get_info()[0] < m * 134 + (8 << 30):
+        pytest.skip("needs the memory of a whole MI355X")
+    x = _randn(torch, 1, m + k).as_strided((m, k), (1, 1))
+    weight, bias = P.quantize_rows(_randn(torch, 2, 1, k)), _randn(torch, 3, 1)
+    got = P.i8_linear(x, weight, bias)
+    for at in (0, (1 << 28) - 150, (1 << 29) - 150, m // 2, m - 300):
+        assert torch.equal(got[at:at + 300], P.i8_linear(x[at:at + 300], weight, bias)), at
+    del x, got
+    torch.cuda.empty_cache()
+
+
+def test_linear_more_tiles_across_than_a_launch(torch, P):
+    """The same of the weight's rows: 2^22 tiles of 64 columns a launch."""
+    m, k, n = 17, 5, (1 << 28) + 70
+    if torch.cuda.mem_get_info()[0] < n * (134 + 2 * m) + (8 << 30):
+        pytest.skip("needs the memory of a whole MI355X")
+    x, bias = _randn(torch, 1, m, k), _randn(torch, 3, 70).repeat(n // 70 + 1)[:n]
+    w = P.quantize_rows(_randn(torch, 2, n + k).as_strided((n, k), (1, 1)))
+    got = P.i8_linear(x, w, bias)
+    for at in (0, (1 << 27) - 150, (1 << 28) - 150, n - 300):
+        part = P.I8Rows(w.codes[at:at + 300], w.scales[at:at + 300], k)
+        assert torch.equal(got[:, at:at + 300], P.i8_linear(x, part, bias[at:at + 300].contiguous())), at
+    del w, bias, got, part
+    torch.cuda.empty_cache()
+
+
 def test_linear_batch_invariant(torch, P):
     """A row's result does not depend on the rows beside it, nor on the kernel that takes them: the sums are exact."""
     x, w = _randn(torch, 1, 33000, 320, std=2.0), _randn(torch, 2, 330, 320, std=0.05)
