@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_cross(CrossArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
   const int rw = wave % RW, kw = wave / RW;
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int klen = sq.k_len, rows = sq.q_len * a.rep;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_cross_stream(Cro
   extern __shared__ u32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int klen = sq.k_len, rows = sq.q_len * a.rep;
@@ -826,7 +826,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void k_kv8_tiles(
   __shared__ int again[4];                          // waves whose O holds NaN
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const int tile = un.tile, g = un.g, split = blockIdx.y;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int rows = sq.q_len * a.rep, t0 = (tile - sq.tile0) * 128, r0 = t0 + wave * 32, r = r0 + lrow;
@@ -935,7 +935,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2) void
   extern __shared__ u32x4 lds[];                    // [block][NK key + 2 ND value fragments][64 lanes]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int first = (tile - sq.tile0) * chunk;
@@ -1156,7 +1156,7 @@ template <int DP, bool WIDE> __device__ __forceinline__ int join_index() {
 // split: k0 = their first unit, k_len = its parts, tile0 = their first tile here.
 template <typename T, int DP, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_cross_join(CrossArgs a, int TR) {
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, un.tile)];
   const int rows = sq.q_len * a.rep, t = un.tile - sq.tile0, i = join_index<DP, WIDE>(), tiles = (rows + TR - 1) / TR;
   if (i >= TR || t * TR + i >= rows) return;
@@ -1168,7 +1168,7 @@ __global__ __launch_bounds__(kThreads) void k_cross_join(CrossArgs a, int TR) {
 // Grid: x = (tile, kv head), y = rows of the tile.
 template <typename T, int DP, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_kv8_tiles_join(Kv8AttnArgs a) {
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, un.tile)];
   const int rows = sq.q_len * a.rep, r0 = (un.tile - sq.tile0) * 128, i = join_index<DP, WIDE>();
   if (i >= 128 || r0 + i >= rows) return;
@@ -1182,7 +1182,7 @@ __global__ __launch_bounds__(kThreads) void k_kv8_tiles_join(Kv8AttnArgs a) {
 
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads) void k_kv8_rows_join(Kv8AttnArgs a, int target) {
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const CondSeq sq = a.seq[un.tile];
   const int i = blockIdx.y;
   if (i >= sq.q_len * a.rep) return;
@@ -1380,8 +1380,9 @@ static hipError_t run_cross(CrossArgs &a, const Plan &pl, hipStream_t s) {
     }
   }
   if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(units * a.hkv), dim3(kThreads), lds, s, a);
-  if ((e = hipGetLastError()) != hipSuccess || !pl.split) return e;
+  e = in_launches(a, (int64_t)units * a.hkv,
+                  [&](uint32_t n) { hipLaunchKernelGGL(kern, dim3(n), dim3(kThreads), lds, s, a); });
+  if (e != hipSuccess || !pl.split) return e;
   int n = 0, tiles = 0, most = 0;
   for (int i = 0; i < a.n_seq; ++i) {
     CondSeq q = a.seq[i];
@@ -1397,8 +1398,9 @@ static hipError_t run_cross(CrossArgs &a, const Plan &pl, hipStream_t s) {
   if (n == 0) return e;                             // none in this launch
   a.n_seq = n;
   auto join = most > kFewParts ? k_cross_join<T, DP, true> : k_cross_join<T, DP, false>;
-  hipLaunchKernelGGL(join, dim3(tiles * a.hkv, join_grid<DP>(most, a.ws_rows)), dim3(kThreads), 0, s, a, pl.TR);
-  return hipGetLastError();
+  const int across = join_grid<DP>(most, a.ws_rows);
+  return in_launches(a, (int64_t)tiles * a.hkv,
+                     [&](uint32_t n) { hipLaunchKernelGGL(join, dim3(n, across), dim3(kThreads), 0, s, a, pl.TR); });
 }
 
 hipError_t launch_cross(const AttnProblem &p, const void *k, const void *v, const uint8_t *mask, int64_t k_row,
@@ -1544,18 +1546,18 @@ int64_t kv8_workspace(const AttnProblem &p, int width) {
 }
 
 template <typename T, int D>
-static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, const Plan &pl, hipStream_t s) {
-  const dim3 grid(tiles * a.hkv, a.n_split);
+static hipError_t run_kv8(Kv8AttnArgs &a, int tiles, const Plan &pl, hipStream_t s) {
+  const int64_t groups = (int64_t)tiles * a.hkv;
   hipError_t e;
   if (pl.kind == Plan::RESIDENT) {
     constexpr bool B16 = sizeof(T) == 2;
     auto kern = pl.box ? (pl.nw == 4 ? k_kv8_res<T, D, 4, B16> : k_kv8_res<T, D, 8, B16>)
                        : (pl.nw == 4 ? k_kv8_res<T, D, 4, false> : k_kv8_res<T, D, 8, false>);
     if ((e = allow_lds(kern, pl.lds)) != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, grid, dim3(64 * pl.nw), pl.lds, s, a, pl.TR);
-    return hipGetLastError();
+    return in_launches(a, groups,
+                       [&](uint32_t n) { hipLaunchKernelGGL(kern, dim3(n), dim3(64 * pl.nw), pl.lds, s, a, pl.TR); });
   }
-  if (pl.kind == Plan::FEW) {                       // a tile is a chunk
+  if (pl.kind == Plan::FEW) {                       // a tile is a chunk: kCondSeqs of them at most
     const int target = std::max(pl.target, 1);
     const dim3 parts((tiles + (pl.target > 0 ? target : 0)) * a.hkv);
     hipLaunchKernelGGL((k_kv8_rows<T, D>), parts, dim3(kThreads), 3 * (2 + D / 2) * 64 * 4, s, a, target);
@@ -1563,11 +1565,13 @@ static hipError_t run_kv8(const Kv8AttnArgs &a, int tiles, const Plan &pl, hipSt
     hipLaunchKernelGGL((k_kv8_rows_join<T, D>), dim3(tiles * a.hkv, a.ws_rows), dim3(kThreads), 0, s, a, target);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((k_kv8_tiles<T, D>), grid, dim3(kThreads), 2 * 4 * (D / 32) * 64 * 16, s, a);
-  if ((e = hipGetLastError()) != hipSuccess || a.n_split == 1) return e;
+  e = in_launches(a, groups, [&](uint32_t n) {
+    hipLaunchKernelGGL((k_kv8_tiles<T, D>), dim3(n, a.n_split), dim3(kThreads), 2 * 4 * (D / 32) * 64 * 16, s, a);
+  });
+  if (e != hipSuccess || a.n_split == 1) return e;
   auto join = a.n_split > kFewParts ? k_kv8_tiles_join<T, D, true> : k_kv8_tiles_join<T, D, false>;
-  hipLaunchKernelGGL(join, dim3(tiles * a.hkv, join_grid<D>(a.n_split, a.ws_rows)), dim3(kThreads), 0, s, a);
-  return hipGetLastError();
+  const int across = join_grid<D>(a.n_split, a.ws_rows);
+  return in_launches(a, groups, [&](uint32_t n) { hipLaunchKernelGGL(join, dim3(n, across), dim3(kThreads), 0, s, a); });
 }
 
 hipError_t launch_kv8_attention(const AttnProblem &p, const Kv8View &c, int causal, hipStream_t s) {

@@ -69,6 +69,7 @@ inline AttnProblem problem(const mte_attn_shape &s, const int32_t *q_lens, int32
   p.c.ws_rows = 0;
   p.c.ws_ml = 0;
   p.c.big = 0;
+  p.c.first = 0;
   p.dtype = s.dtype;
   p.near_rows = s.k_row < (1 << 24) && s.v_row < (1 << 24);
   // 31 rows and rep heads: 2^29 + 2^30 elements; rep: what the tiles divide by in fp32 (exact below 2^22)

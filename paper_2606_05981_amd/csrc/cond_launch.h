@@ -33,7 +33,19 @@ struct AttnCommon {
   int n_seq, n_split, ws_rows;       // ws_rows: rows of a tile's partial result
   int64_t ws_ml;                     // float offset of the (m, l) pairs in ws
   int big;                           // out is more than the caches hold
+  int first;                         // workgroup of the call that the launch begins with (in_launches)
 };
+
+// A call of `groups` workgroups in launches of kMostGroups; launch(workgroups) with a.first set.
+template <typename A, typename F> hipError_t in_launches(A &a, int64_t groups, F launch) {
+  for (int64_t at = 0; at < groups; at += kMostGroups) {
+    a.first = (int)at;
+    launch((uint32_t)(groups - at < kMostGroups ? groups - at : kMostGroups));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 // How key ranges are cut: key tiles of a part, and of the shortest range that is cut.
 struct KeyCut { int per, from; };

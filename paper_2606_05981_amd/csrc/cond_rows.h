@@ -21,11 +21,11 @@ constexpr int kMaxParts = 512;                      // of a key range
 // The workgroup's tile and kv head, heads next to each other: the workgroups that run together then read
 // and write whole rows of q and out between them (head-major order: 4 to 10% slower).
 struct Unit { int tile, g; };
-__device__ __forceinline__ Unit unit_of(int hkv) {
-  const int flat = blockIdx.x;
+__device__ __forceinline__ Unit unit_of(const AttnCommon &a) {
+  const int flat = a.first + (int)blockIdx.x;
   Unit u;
-  u.tile = flat / hkv;
-  u.g = flat - u.tile * hkv;
+  u.tile = flat / a.hkv;
+  u.g = flat - u.tile * a.hkv;
   return u;
 }
 

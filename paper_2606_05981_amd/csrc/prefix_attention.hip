@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
   const int rw = wave % RW, kw = wave / RW;
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const Keys ks = keys_of(a, sq, KT);
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 4 : 3) void k_prefix_stream(Pr
   extern __shared__ u32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lrow = lane & 31, h = lane >> 5;
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const int tile = un.tile, g = un.g;
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const Keys ks = keys_of(a, sq, 32);
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(kThreads) void k_prefix_join(JoinArgs a) {
   constexpr int LPR = DP / 4, ROWS = kThreads / (LPR * TEAMS);
   __shared__ f32x4 sums[TEAMS > 1 ? kThreads : 1];
   __shared__ float2 tops[TEAMS > 1 ? kThreads / LPR : 1];
-  const Unit un = unit_of(a.hkv);
+  const Unit un = unit_of(a);
   const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, un.tile)];
   const int rows = sq.q_len * a.rep, tid = threadIdx.x, c = (tid % LPR) * 4, team = tid / LPR % TEAMS;
   const int i = blockIdx.y * ROWS + tid / (LPR * TEAMS), r = (un.tile - sq.tile0) * a.TR + i;
@@ -666,19 +666,17 @@ hipError_t run(PrefixArgs &a, const Plan &pl, bool copies, hipStream_t s) {
       }
     }
     if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3(units * a.hkv), dim3(kThreads), lds, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = in_launches(a, (int64_t)units * a.hkv,
+                    [&](uint32_t n) { hipLaunchKernelGGL(kern, dim3(n), dim3(kThreads), lds, s, a); });
+    if (e != hipSuccess) return e;
   }
   if (j.n_seq == 0) return hipSuccess;
   const int most = (int)std::min<int64_t>(pl.TR, pl.rows_at_once);
-  if (pl.most > 8) {
-    constexpr int TEAMS = kThreads / (DP / 4);
-    hipLaunchKernelGGL((k_prefix_join<T, DP, TEAMS>), dim3(join_tiles * a.hkv, most), dim3(kThreads), 0, s, j);
-  } else {
-    hipLaunchKernelGGL((k_prefix_join<T, DP, 1>), dim3(join_tiles * a.hkv, ceil_div(most, kThreads / (DP / 4))), dim3(kThreads),
-                       0, s, j);
-  }
-  return hipGetLastError();
+  const bool teams = pl.most > 8;
+  auto join = teams ? k_prefix_join<T, DP, kThreads / (DP / 4)> : k_prefix_join<T, DP, 1>;
+  const int across = teams ? most : ceil_div(most, kThreads / (DP / 4));
+  return in_launches(j, (int64_t)join_tiles * a.hkv,
+                     [&](uint32_t n) { hipLaunchKernelGGL(join, dim3(n, across), dim3(kThreads), 0, s, j); });
 }
 
 }  // namespace

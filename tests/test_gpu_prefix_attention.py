@@ -200,3 +200,34 @@ def test_large_scores(torch, C):
 def test_no_queries(torch, C):
     q, pk, pv, k, v = _make(torch, [0, 0], 5, [3, 0], 4, 2, 64, "bf16")
     assert C.prefix_attention(q, pk, pv, k, v, [0, 0], [3, 0]).shape == (0, 4, 64)
+
+
+# 257 tiles of 128 rows for each of 65535 heads: more workgroups than a launch takes. One token's queries for all.
+MANY, HEADS = [129] * 127 + [257], 65535
+
+
+@pytest.mark.parametrize("form", ["own", "cross", "cache"])
+def test_more_workgroups_than_a_grid(torch, C, form):
+    """Every sequence has one token, whose value is its result; the same of cross attention and of the 8-bit cache (a
+    token for all)."""
+    n, d = len(MANY), 64 if form == "cache" else 8
+    if torch.cuda.mem_get_info()[0] < sum(MANY) * HEADS * d * 2 + (4 << 30):
+        pytest.skip("needs the memory of a whole MI355X")
+    q = _randn(torch, 1, 1, HEADS, d).expand(sum(MANY), HEADS, d)
+    if form == "cache":
+        cache = C.kv8_cache(1, HEADS, d)
+        table, lens = torch.zeros((n, 21), dtype=torch.int32, device="cuda"), torch.ones(n, dtype=torch.int32, device="cuda")
+        k = _randn(torch, 2, 1, HEADS, d)
+        C.kv8_append(cache, table[:1], lens[:1], k, k, [1])
+        v = C.kv8_read(cache, table[:1], lens[:1], [1])[1].expand(n, HEADS, d)
+        got = C.kv8_attention(q, cache, table, lens, MANY)
+    else:
+        k, v = (_randn(torch, i, n, HEADS, d) for i in (2, 3))
+        got = C.cross_attention(q, k, v, MANY, [1] * n) if form == "cross" else \
+            C.prefix_attention(q, k[:0], k[:0], k, v, MANY, [1] * n, causal=False)
+    at = 0
+    for i, rows in enumerate(MANY):
+        assert bool((got[at:at + rows] == v[i]).all()), i
+        at += rows
+    del got
+    torch.cuda.empty_cache()
