@@ -78,6 +78,7 @@ struct Kv8RowsArgs {                 // append and read
   void *ko, *vo;                     // read: destinations
   int64_t k_row, k_head, v_row, v_head;
   int n_seq;
+  int first;                         // tile that the launch begins with (in_launches)
   CondSeq seq[kCondSeqs];
 };
 

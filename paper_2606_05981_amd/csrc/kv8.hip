@@ -107,9 +107,10 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Kv8RowsArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t sv[v_bytes(D)];
   __shared__ float smax[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, blockIdx.x)];
+  const int tile = a.first + (int)blockIdx.x;
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int g = blockIdx.y;
-  const Where w = block_of(a.c, sq, (int)blockIdx.x - sq.tile0, g);
+  const Where w = block_of(a.c, sq, tile - sq.tile0, g);
   // the whole workgroup: a sequence shorter than its new rows, or longer than its table, is not written
   if (w.start < 0 || w.kv > (int64_t)a.c.width * 32) return;
   const int sub = tid % (32 * PC), tok = sub / PC, pc = sub % PC;
@@ -216,9 +217,10 @@ __global__ __launch_bounds__(kThreads) void k_kv8_read(Kv8RowsArgs a) {
   constexpr int NT = D == 128 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) uint8_t sv[v_bytes(D)];
   const int tid = threadIdx.x;
-  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, blockIdx.x)];
+  const int tile = a.first + (int)blockIdx.x;
+  const CondSeq sq = a.seq[find_seq(a.seq, a.n_seq, tile)];
   const int g = blockIdx.y;
-  const Where w = block_of(a.c, sq, (int)blockIdx.x - sq.tile0, g);
+  const Where w = block_of(a.c, sq, tile - sq.tile0, g);
   uint8_t *kc = a.c.k_codes + w.at * (32 * D), *vc = a.c.v_codes + w.at * (32 * D);
   if (w.ok) {
     for (int i = tid; i < 32 * D / 16; i += kThreads)
@@ -268,8 +270,7 @@ hipError_t for_rows(Kv8RowsArgs &a, const int32_t *lens, int n, F launch) {
       row += lens[i];
     }
     if (tiles == 0) continue;
-    launch(dim3(tiles, a.c.hkv));
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = in_launches(a, tiles, [&](uint32_t n) { launch(dim3(n, a.c.hkv)); });
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

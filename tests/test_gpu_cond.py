@@ -577,6 +577,31 @@ def test_kv8_many_sequences(torch, C):
     _compare(got, *(np.concatenate([p[x] for p in parts]) for x in range(3)), 60, 64, "bf16", 8.0)
 
 
+def test_kv8_more_blocks_than_a_grid(torch, C):
+    """2^29 tokens appended and read at once, a workgroup a block: more than a launch takes. Tokens overlap in memory."""
+    t, d = (1 << 29) + 5, 64
+    nb = (t + 31) // 32
+    if torch.cuda.mem_get_info()[0] < t * 8 * 2 + nb * 64 * 64 + t * d * 4 + (6 << 30):
+        pytest.skip("needs the memory of a whole MI355X")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(8 * t + d, generator=g, device="cuda", dtype=torch.bfloat16).as_strided((t, 1, d), (8, d, 1))
+    cache = C.kv8_cache(nb, 1, d)
+    table = torch.arange(nb, dtype=torch.int32, device="cuda").view(1, nb)
+    lens = torch.tensor([t], dtype=torch.int32, device="cuda")
+    C.kv8_append(cache, table, lens, x, x, [t])
+    k, v = C.kv8_read(cache, table, lens, [t])
+    for at in (0, (1 << 22) - 2, nb // 2, nb - 3):
+        part = x[32 * at:32 * at + 96]
+        n = part.shape[0]
+        one, few = C.kv8_cache(3, 1, d), torch.tensor([n], dtype=torch.int32, device="cuda")
+        C.kv8_append(one, table[:, :3], few, part, part, [n])
+        assert all(bool((a[at:at + 3] == b).all()) for a, b in zip(cache, one)), at
+        for a, b in zip((k, v), C.kv8_read(one, table[:, :3], few, [n])):
+            assert torch.equal(a[32 * at:32 * at + n], b), at
+    del x, part, cache, k, v, a, b
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("ql,kl,width,hq,h", [(16, 40, None, 4, 2), (64, 64, None, 4, 2), (64, 64, 30, 4, 2),
                                               (300, 310, None, 32, 4), (300, 310, 40, 32, 4)])
