@@ -46,6 +46,7 @@ struct GnArgs : GroupNormArgs {
   int parts;           // of k_gn_stats: chunks x column parts
   int colparts;        // a bundle wider than a workgroup (then one group): its parts
   int same;            // a column lies inside one group
+  int first;           // workgroup of a row of the grid that the launch begins with (in_launches): k_gn_apply
 };
 
 template <typename T, int V> struct Vec {
@@ -309,8 +310,8 @@ __global__ __launch_bounds__(TH) void k_gn_apply(GnArgs a) {
   typedef Vec<T, V> vec;
   extern __shared__ float lds[];                    // [gb][2]
   const int tid = threadIdx.x;
-  const int chunk = (int)blockIdx.x / a.colparts;
-  const Place w = place_of<V, TH>(a, (int)blockIdx.x - chunk * a.colparts);
+  const int at = a.first + (int)blockIdx.x, chunk = at / a.colparts;
+  const Place w = place_of<V, TH>(a, at - chunk * a.colparts);
   const int px0 = chunk * a.apply, npx = w.on ? min(a.apply, a.pixels - px0) : 0;
   const T *x = (const T *)a.x + (int64_t)blockIdx.z * a.x_image + (int64_t)px0 * a.x_row + w.ch;
   T *y = (T *)a.y + (int64_t)blockIdx.z * a.y_image + (int64_t)px0 * a.y_row + w.ch;
@@ -454,7 +455,7 @@ template <typename K> hipError_t allow_lds(K kern, int bytes) {
 }
 
 template <typename T, int V>
-hipError_t run(const GnArgs &a, const GnPlan &p, int esize, hipStream_t s) {
+hipError_t run(GnArgs &a, const GnPlan &p, int esize, hipStream_t s) {
   const int sums = sums_bytes(p.gb, a.cpg, V, std::min(p.ncol, p.TH), p.ppi), bundles = a.groups / p.gb;
   hipError_t e;
   if (p.one) {
@@ -469,8 +470,9 @@ hipError_t run(const GnArgs &a, const GnPlan &p, int esize, hipStream_t s) {
   const int chunks = (int)(((int64_t)a.pixels + p.apply - 1) / p.apply);
   const bool past = (int64_t)a.n * a.pixels * a.channels * esize > (32 << 20);
   auto apply = past ? k_gn_apply<T, V, 256, true> : k_gn_apply<T, V, 256, false>;
-  hipLaunchKernelGGL(apply, dim3(chunks * p.colparts, bundles, a.n), dim3(256), p.gb * 8, s, a);
-  return hipGetLastError();
+  return in_launches(a, (int64_t)chunks * p.colparts, [&](uint32_t n) {
+    hipLaunchKernelGGL(apply, dim3(n, bundles, a.n), dim3(256), p.gb * 8, s, a);
+  });
 }
 
 }  // namespace
@@ -503,6 +505,7 @@ hipError_t launch_group_norm(const GroupNormArgs &g, int dtype, hipStream_t s) {
   a.parts = p.parts;
   a.colparts = p.colparts;
   a.same = p.gb == 1 || a.cpg % p.V == 0;
+  a.first = 0;
   if (dtype == MTE_BF16) {
     if (p.V == 8) return run<bf16, 8>(a, p, es, s);
     if (p.V == 4) return run<bf16, 4>(a, p, es, s);

@@ -775,3 +775,17 @@ def test_group_norm_large_mean(torch, C):
 def test_group_norm_empty(torch, C):
     assert C.group_norm(torch.empty((0, 4, 32), device="cuda"), 4).shape == (0, 4, 32)
     assert C.group_norm(torch.empty((2, 0, 32), device="cuda"), 4).shape == (2, 0, 32)
+
+
+def test_group_norm_more_workgroups_than_a_grid(torch, C):
+    """An image of more pixels than a launch has workgroups for (16 of 129 channels each), all of them one pixel."""
+    px, c = (1 << 28) + 37, 129
+    if torch.cuda.mem_get_info()[0] < px * c * 2 + (4 << 30):
+        pytest.skip("needs the memory of a whole MI355X")
+    x = _randn(torch, 75, 1, 1, c).expand(1, px, c)
+    got = C.group_norm(x, 1)
+    _check_norm(torch, got[:, :50].contiguous(), x[:, :50], 1, None, None, 1e-5, None, "bf16")
+    for at in range(0, px, 1 << 24):
+        assert bool((got[0, at:at + (1 << 24)] == got[0, 0]).all()), at
+    del got
+    torch.cuda.empty_cache()
