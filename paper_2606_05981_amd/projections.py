@@ -23,13 +23,13 @@ class I8Rows(NamedTuple):
     cols: int
 
 
-def _matrix(name: str, x):
-    """A [..., K] bf16 or fp32 GPU tensor as rows -> (the 2-d view, its row stride)."""
+def _matrix(name: str, x, most: int = B.MTE_I8_COLS):
+    """A [..., K] bf16 or fp32 GPU tensor, K up to `most`, as rows -> (the 2-d view, its row stride)."""
     if not isinstance(x, torch.Tensor) or x.dim() < 1 or not x.is_cuda or x.dtype not in _DTYPE:
         raise ValueError(f"{name}: expected a [..., channels] bf16 or fp32 tensor on the GPU")
     k = x.shape[-1]
-    if not 0 < k <= B.MTE_I8_COLS:
-        raise ValueError(f"{name}: expected 1 to {B.MTE_I8_COLS} channels, got {k}")
+    if not 0 < k <= most:
+        raise ValueError(f"{name}: expected 1 to {most} channels, got {k}")
     if x.dim() != 2:
         try:
             x = x.view(-1, k) if x.numel() else x.reshape(0, k)
@@ -114,7 +114,7 @@ def i8_linear(x, weight: I8Rows, bias: Optional[torch.Tensor] = None, act: Optio
     if out is not None:
         if not isinstance(out, torch.Tensor) or out.dtype != dtype or out.device != dev or tuple(out.shape) != (*lead, n):
             raise ValueError(f"out: expected a {dtype} tensor of shape {(*lead, n)} on {dev}")
-        flat, orow = _matrix("out", out)
+        flat, orow = _matrix("out", out, n)
         if flat.shape[0] > 1 and orow < n:
             raise ValueError("out: rows overlap")
 

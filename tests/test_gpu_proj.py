@@ -216,6 +216,20 @@ def test_linear_strides(torch, P, m, dtype):
         assert torch.equal(y.view(m, n), P.i8_linear(x, weight))
 
 
+@pytest.mark.parametrize("off,wide", [(0, 0), (8, 24), (3, 2)])
+def test_linear_result_wider_than_the_longest_rows(torch, P, off, wide):
+    """What bounds a row's channels (the sum) does not bound the weight's rows: a vocabulary's worth of them, into
+    a result of the caller's, whole and as a slice."""
+    m, k, n = 2, 64, 140000
+    x, weight = _randn(torch, 1, m, k), P.quantize_rows(_randn(torch, 2, n, k))
+    ref = P.i8_linear(x, weight)
+    buf = torch.full((m, off + n + wide), 7.0, dtype=x.dtype, device="cuda")
+    out = buf[:, off:off + n]
+    assert P.i8_linear(x, weight, out=out) is out
+    assert torch.equal(out, ref)
+    assert (buf[:, :off] == 7).all() and (buf[:, off + n:] == 7).all()
+
+
 def test_linear_more_tiles_than_a_grid(torch, P):
     """More tiles of 64 rows than a launch takes workgroups for, 2^24; rows that overlap in memory, so that what is large
     are the codes that the call makes."""
