@@ -165,8 +165,9 @@ def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Te
 
     q_lens / kv_lens: query rows and own tokens of each sequence (0 allowed); causal: query u of q_lens[i] sees
     own tokens up to kv_lens[i] - q_lens[i] + u (all of the prefix in any case); scale: default
-    1 / sqrt(d). A query that sees no token gets zeros. All but out (which may be q) may be strided over tokens and
-    heads. Streams of single queries over a long prefix read it once between them."""
+    1 / sqrt(d). A query that sees no token gets zeros. All may be strided over tokens and heads; out may be q, and
+    otherwise shares no memory with what the call reads. Streams of single queries over a long prefix read it once
+    between them."""
     hq, d, dtype, dev = _query(q)
     hkv = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
     sq = _rows("q", q, dtype, hq, d, dev)

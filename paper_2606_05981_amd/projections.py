@@ -43,6 +43,21 @@ def _matrix(name: str, x, most: int = B.MTE_I8_COLS):
     return x, row if x.shape[0] > 1 else 0
 
 
+def _meet(a, b) -> bool:
+    """Whether two pieces of memory, rows at one stride as (address, rows, bytes from row to row, bytes of a row),
+    share a byte. Rows that lie between the other's are apart; at two strides that do not tell, they are taken to meet."""
+    (p, m, s, w), (q, n, t, u) = ((x[0], 1, 0, (x[1] - 1) * x[2] + x[3]) if x[2] <= x[3] else x for x in (a, b))
+    if p + (m - 1) * s + w <= q or q + (n - 1) * t + u <= p:
+        return False
+    every = math.gcd(s if m > 1 else 0, t if n > 1 else 0)
+    at = (q - p) % every if every else 0
+    return at < w or at + u > every
+
+
+def _whole(t: torch.Tensor):
+    return t.data_ptr(), 1, 0, t.numel() * t.element_size()
+
+
 def _i8_rows(name: str, t, dev: torch.device):
     """Checks 8-bit rows -> (codes, scales, rows, cols)."""
     codes, scales, cols = t
@@ -84,7 +99,8 @@ def i8_linear(x, weight: I8Rows, bias: Optional[torch.Tensor] = None, act: Optio
 
     x: [..., K] bf16 or fp32, quantised within the call, or the I8Rows of M tokens; weight: I8Rows of
     N rows of K; bias: [N] of the result's dtype; act: None or "silu"; dtype of the result: bf16 or fp32, by
-    default x's (I8Rows: bf16). out: [M, N] or x's leading shape, rows at one stride."""
+    default x's (I8Rows: bf16). out: [M, N] or x's leading shape, rows at one stride; it shares no memory with what
+    the call reads (workgroups store rows while others read x)."""
     if act not in _ACT:
         raise ValueError(f"act: expected None or 'silu', got {act!r}")
     if isinstance(x, torch.Tensor):
@@ -117,6 +133,11 @@ def i8_linear(x, weight: I8Rows, bias: Optional[torch.Tensor] = None, act: Optio
         flat, orow = _matrix("out", out, n)
         if flat.shape[0] > 1 and orow < n:
             raise ValueError("out: rows overlap")
+        to, es = (out.data_ptr(), m, orow * out.element_size(), n * out.element_size()), src.element_size()
+        reads = [(src.data_ptr(), m, row * es, k * es)] if x_scales is None else [_whole(src), _whole(x_scales)]
+        reads += [_whole(t) for t in (w, w_scales, bias) if t is not None]
+        if m and any(_meet(to, r) for r in reads):
+            raise ValueError("out: expected memory that the call does not read")
 
     def call(st):
         y = w.new_empty((*lead, n), dtype=dtype) if out is None else out
@@ -171,7 +192,8 @@ def rotary(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, k: Opti
     positions: int32 [T], or [axes, T] (2 to 4 axes, such as the encoder's t, h, w) with sections, the pairs of
     each axis; freq: float64, device (``rotary_frequencies``); interleaved: pairs are neighbouring
     channels instead of the two halves; inverse: turns back (with the same factor, the gradient).
-    out: (q_out, k_out or None), which may be q and k themselves. q and k may be strided over tokens and heads."""
+    out: (q_out, k_out or None), which may be q and k themselves, and otherwise share no memory with what the call
+    reads, nor with each other. q and k may be strided over tokens and heads."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or not q.is_cuda or q.dtype not in _DTYPE:
         raise ValueError("q: expected a [tokens, heads, head_dim] bf16 or fp32 tensor on the GPU")
     t, hq, d = q.shape

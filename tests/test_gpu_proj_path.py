@@ -272,3 +272,26 @@ def test_wrappers_refuse(torch, C, P):
                 dict(out=q[:1].expand(7, 4, 64)), dict(q=_randn(torch, 7, 7, 3, 64)), dict(prefix_v=k.transpose(1, 2))):
         with pytest.raises((ValueError, MteError)):
             C.prefix_attention(**{**ok, **bad})
+
+
+def test_products_refuse_a_result_in_what_they_read(torch, P):
+    """A result in the memory of the rows (a square layer in place), of codes, weight or bias raises: workgroups store
+    while others read. Columns beside the rows, in one buffer, are taken."""
+    k = 128
+    for m in (5, 40):
+        x, w, bias = _randn(torch, 1, m, k), P.quantize_rows(_randn(torch, 2, k, k)), _randn(torch, 3, k)
+        ref = P.i8_linear(x, w, bias)
+        box = torch.zeros((m + 1, 2 * k), dtype=x.dtype, device="cuda")
+        rows, beside = box[:m, :k], box[:m, k:]
+        rows.copy_(x)
+        twice = torch.zeros((2 * m, k), dtype=torch.int8, device="cuda")        # codes in the first half
+        codes = P.I8Rows(twice[:m], P.quantize_rows(x).scales, k)
+        as_result = lambda t: t.view(-1).view(torch.bfloat16)[:m * k].view(m, k)
+        held = box.clone()
+        for src, out in ((x, x), (rows, rows), (rows, box[:m, 8:k + 8]), (rows, box[1:, :k]),
+                         (rows, box.view(-1)[k:(m + 1) * k].view(m, k)), (codes, as_result(twice)), (x, as_result(w.codes)),
+                         (x[:1], bias.view(1, k)), (x[:1], w.scales.view(torch.bfloat16)[:k].view(1, k))):
+            with pytest.raises(ValueError, match="out"):
+                P.i8_linear(src, w, bias, out=out)
+        assert torch.equal(box, held)
+        assert torch.equal(P.i8_linear(rows, w, bias, out=beside), ref) and torch.equal(rows, x)

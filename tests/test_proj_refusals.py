@@ -185,3 +185,23 @@ def test_rotary_frequencies_refuses(B, kw):
     from paper_2606_05981_amd import projections as J
     with pytest.raises(ValueError):
         J.rotary_frequencies(device="cpu", **kw)
+
+
+def test_rows_that_meet():
+    """Rows at strides against rows at strides, byte by byte: what shares one is found; what does not is told apart where
+    one of the two is a single run, or both have one stride."""
+    import itertools
+    from paper_2606_05981_amd import projections as J
+    cells = lambda x: {x[0] + r * x[2] + b for r in range(x[1]) for b in range(x[3])}
+    pieces = [(0, rows, step, width) for rows, step, width in ((1, 0, 5), (3, 4, 4), (3, 2, 5), (4, 0, 3), (3, 7, 3), (4, 12, 5), (2, 6, 1))]
+    told = 0
+    for a, b in itertools.product(pieces, pieces):
+        for at in range(60):
+            x, y = (20, *a[1:]), (at, *b[1:])
+            share = bool(cells(x) & cells(y))
+            runs = [p[1] == 1 or p[2] <= p[3] for p in (x, y)]
+            if share or any(runs) or x[2] == y[2]:
+                assert J._meet(x, y) == share, (x, y)
+                assert J._meet(y, x) == share, (x, y)
+                told += not share
+    assert told > 500
