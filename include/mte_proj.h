@@ -104,7 +104,8 @@ int mte_rotary(const mte_rotary_shape *shape, const void *q, const void *k, cons
  * prefix_len tokens that all of them share and then to its own kv_lens[i] tokens, in one softmax.
  * causal = 1: query u sees own tokens 0 .. kv_lens[i] - q_lens[i] + u only (the whole prefix in any
  * case). A query that sees nothing gets zeros. What tokens that a query does not see hold (infinities,
- * NaN) does not reach it.
+ * NaN) does not reach it. An infinite value of one that it sees is the result in its channel; where the weight is
+ * below 2^-100 of the heaviest key's, it may be NaN instead.
  *  shape:      heads, types and strides as in mte_cross_attention (k_*, v_*: of the own tokens).
  *  prefix_k/v: device, prefix_len rows at the strides pk_row, pk_head, pv_row, pv_head.
  *  k, v:       device, sum(kv_lens) rows back to back; q, out, workspace as in mte_cross_attention.

@@ -65,8 +65,9 @@ __device__ __forceinline__ Part part_in(const PrefixArgs &a, const CondSeq &sq, 
 
 // Infinities and NaN among the values of a tile whose rows see different keys: 0 times infinity in the matrix
 // product would reach the rows that do not see them. Such values become zeros on their way to LDS, and rows that
-// see them have them added after the last tile (add_wild; whatever its weight, an infinity stays one). In
-// the loop itself a second path to O would cost a second copy of it, and its registers.
+// see them have them added after the last tile and the waves' join (add_wild). An infinity stays one where fp32 holds
+// its weight; in a tile that all rows see, or a part of the list, whose weight beside the others' underflows, it is
+// zero times infinity. In the loop itself a second path to O would cost a second copy of it, and its registers.
 template <typename T> __device__ __forceinline__ bool tame(u32x4 &x) {
   bool wild = false;
 #pragma unroll
@@ -253,12 +254,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
       if (kt + 1 < span.hi) gload(kt + 1, 0);
     if (r0 < rows) compute(kt);                     // wave-uniform
   }
+  bool found = false;
   if (ks.cross) {
     __syncthreads();
-    if (kw == 0 && (wild[0] | wild[1] | wild[2] | wild[3])) {
-      const int from = max(max(span.lo - ks.np, 0) * KT, all_see / KT * KT), to = min((span.hi - ks.np) * KT, ks.klen);
-      add_wild<T, ND>(st.o, vg, a.v_row, a.d, from, to, mine, lane);
-    }
+    found = wild[0] | wild[1] | wild[2] | wild[3];
   }
   if constexpr (KW > 1) {
     __syncthreads();
@@ -266,6 +265,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_prefix(PrefixArgs a) {
     if (kw > 0) return;
   }
   if (r0 >= rows) return;
+  if (found) {                                      // (before the waves are joined, wave 0's weight would reach them)
+    const int from = max(max(span.lo - ks.np, 0) * KT, all_see / KT * KT), to = min((span.hi - ks.np) * KT, ks.klen);
+    add_wild<T, ND>(st.o, vg, a.v_row, a.d, from, to, mine, lane);
+  }
   if (span.used == 1 && !a.shared) store_rows<T, ND>(a, st, 1.f, live, tok, head, lane);
   else store_part<ND>(a, st, 1.f, live, a.unit0 + tile, g, 0, rw * 32 + lrow, lane);
 }

@@ -141,6 +141,23 @@ def test_wild_values_are_seen(torch, C):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_wild_values_beside_far_scores(torch, C, dtype):
+    """An infinite value of a heavy key, with scores of the other keys 300 below: 32 own keys and the prefix, which
+    another wave of the workgroup takes."""
+    ql, p, kl, h, d = [40], 20, [40], 2, 64
+    q, pk, pv, k, v = _make(torch, ql, p, kl, h, h, d, dtype)
+    one = torch.zeros_like(q)
+    one[..., 0] = 8.0                                                # a score is k[.., 0] (of 64: 8 / sqrt(64))
+    pk[..., 0], k[:32, :, 0], k[32:, :, 0] = -300.0, -300.0, 0.0
+    v[35, :, 7] = -math.inf
+    got = C.prefix_attention(one, pk, pv, k, v, ql, kl)
+    assert torch.isfinite(got[:35].float()).all()
+    assert (got[35:, :, 7] == -math.inf).all()
+    other = [c for c in range(d) if c != 7]
+    assert torch.isfinite(got[35:][..., other].float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("ql,p,kl", [([1] * 50, 800, [7] * 50), ([400], 100, [64])])
 def test_strides_out_and_in_place(torch, C, ql, p, kl, dtype):
     """Queries within fused rows, head-major keys, out in place of the queries; other channels and rows stay."""
