@@ -157,6 +157,68 @@ def test_wild_values_beside_far_scores(torch, C, dtype):
     assert torch.isfinite(got[35:][..., other].float()).all()
 
 
+# Every way through the keys whose own tokens hold infinities and NaN: q_lens, prefix, kv_lens, Hq, Hkv, d, far (rows of
+# the prefix too far apart for the copies of the streamed tiles)
+WAYS = [
+    ([2, 3] * 20, 1100, [64, 70] * 20, 8, 4, 64, False), ([2, 3] * 20, 1100, [64, 70] * 20, 4, 4, 120, False),   # shared
+    ([2, 5] * 20, 1500, [400, 1500] * 20, 8, 4, 128, False),          # shared, own ranges cut
+    ([1030], 320, [1030], 16, 8, 128, False),                         # tiles of 128 rows in one pass, cut
+    ([700, 900], 33, [700, 901], 12, 4, 40, False), ([1500, 129], 65, [1400, 129], 6, 6, 104, False),
+    ([1030, 64], 70, [40, 64], 8, 4, 64, False), ([1030, 64], 70, [40, 64], 8, 4, 64, True),                     # whole
+    ([2, 3] * 20, 1100, [64, 70] * 20, 8, 4, 64, True),
+    ([3], 5000, [600], 16, 8, 128, False), ([9, 4], 50, [9, 4], 4, 2, 72, False),                                # tiles of 32
+]
+
+
+def _wild(torch, C, case, dtype, key, value):
+    """Attention with `key` in channel 3 and `value` in channel 5 of two own tokens of each sequence, the last and one in
+    the middle -> result, oracle without them, the rows that see one."""
+    ql, p, kl, hq, hkv, d, far = case
+    q, pk, pv, k, v = _make(torch, ql, p, kl, hq, hkv, d, dtype)
+    full = O.prefix(*map(_f64, (q, pk, pv, k, v)), ql, kl, True)
+    at, row, bad = 0, 0, torch.zeros(q.shape[0], dtype=torch.bool)
+    for n, m in zip(ql, kl):
+        for j in (m - 1, max(m - 1 - n // 2, 0)):
+            if key is not None:
+                k[at + j, :, 3] = key
+            v[at + j, :, 5] = value
+            bad[row + max(j - (m - n), 0):row + n] = True
+        at, row = at + m, row + n
+    if far:
+        step = 1 << 24
+        box = torch.zeros(((p - 1) * step + hkv * d,), dtype=q.dtype, device="cuda").as_strided((p, hkv, d), (step, d, 1))
+        box.copy_(pk)
+        pk = box
+    got = C.prefix_attention(q, pk, pv, k, v, ql, kl)
+    assert bad.any() and not bad.all()
+    return got, full, bad
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", WAYS)
+def test_unseen_tokens_in_every_way(torch, C, case, dtype):
+    _say(f"unseen {case}, {dtype}")
+    for key, value in ((math.nan, math.inf), (math.inf, math.nan), (None, math.nan)):
+        got, full, bad = _wild(torch, C, case, dtype, key, value)
+        keep = ~bad
+        _compare(got[keep.cuda()], tuple(x[keep.numpy()] for x in full), case[1] + max(case[2]), case[5], dtype)
+        assert torch.isnan(got[bad.cuda()].float()).any(-1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", WAYS)
+def test_infinite_values_in_every_way(torch, C, case, dtype):
+    """An infinity of the rows that see it, in its channel alone; all else is what it is without."""
+    _say(f"infinite {case}, {dtype}")
+    for value in (math.inf, -math.inf):
+        got, full, bad = _wild(torch, C, case, dtype, None, value)
+        seen = got[bad.cuda()]
+        assert (seen[..., 5] == value).all()
+        got[..., 5][bad.cuda()] = 0.0
+        full[0][..., 5][bad.numpy()] = 0.0
+        _compare(got, full, case[1] + max(case[2]), case[5], dtype)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("ql,p,kl", [([1] * 50, 800, [7] * 50), ([400], 100, [64])])
 def test_strides_out_and_in_place(torch, C, ql, p, kl, dtype):
@@ -212,6 +274,24 @@ def test_large_scores(torch, C):
             best, gap = int(s.argmax()), float(s.topk(2).values.diff().abs())
             if gap > 1000 and float(s.max()) > float((pkd[:, g] @ qd[i, g]).max()) * 64.0 + 1000:
                 assert torch.equal(got[i, g], v[33 * i + best, g])
+
+
+def test_large_scores_are_decided(torch, C):
+    """As above with keys that make it so: the heaviest of every row and head leads by more than 1000, by turns an own
+    token and one of the prefix."""
+    ql, p, kl, h, d = [1] * 40, 900, [33] * 40, 4, 64
+    q, pk, pv, k, v = _make(torch, ql, p, kl, h, h, d, "bf16")
+    own = torch.arange(0, 40, 2)
+    k[33 * own + 5] = 16 * q[own]
+    pk[100 + own + 1] = 16 * q[own + 1]
+    got = C.prefix_attention(q, pk, pv, k, v, ql, kl, scale=64.0)
+    for i in range(40):
+        keys, values = torch.cat([pk, k[33 * i:33 * i + 33]]), torch.cat([pv, v[33 * i:33 * i + 33]])
+        for g in range(h):
+            s = (keys[:, g].double() @ q[i, g].double()) * 64.0
+            two = s.topk(2)
+            assert float(two.values[0] - two.values[1]) > 1000
+            assert torch.equal(got[i, g], values[two.indices[0], g])
 
 
 def test_no_queries(torch, C):

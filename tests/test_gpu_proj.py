@@ -182,6 +182,44 @@ def test_linear_of_codes(torch, P, m, k, n, out_dtype):
     _check_linear(got, (a[:, :k].double().numpy(), s.numpy()), (b[:, :k].double().numpy(), t.numpy()), None, False, out_dtype)
 
 
+@pytest.mark.parametrize("src,dst", [("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("m,k,n", [(3, 300, 70), (24, 500, 130), (30, 7, 9), (300, 1001, 130), (33000, 120, 70), (32900, 250, 130),
+                                   (33000, 300, 64)])
+def test_linear_of_two_types(torch, P, m, k, n, silu, src, dst):
+    """Rows of one type, bias and result of the other."""
+    x, w, b = _randn(torch, 1, m, k, std=2.0, dtype=src), _randn(torch, 2, n, k, std=1 / math.sqrt(k)), _randn(torch, 3, n, dtype=dst)
+    got = P.i8_linear(x, P.quantize_rows(w), b, act="silu" if silu else None, dtype=_dt(torch, dst))
+    assert got.dtype == _dt(torch, dst)
+    _check_linear(got, O.i8_rows(_f64(x)), O.i8_rows(_f64(w)), _f64(b), silu, dst)
+    bare = P.i8_linear(x, P.quantize_rows(w), act="silu" if silu else None, dtype=_dt(torch, dst))
+    _check_linear(bare, O.i8_rows(_f64(x)), O.i8_rows(_f64(w)), None, silu, dst)
+
+
+@pytest.mark.parametrize("dst", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", [(5, 640, 70), (30, 1500, 90), (40, 640, 130), (300, 1000, 515), (33000, 100, 70)])
+def test_linear_of_codes_with_bias(torch, P, m, k, n, dst):
+    """Ready codes, with bias and with SiLU: what the rows themselves give."""
+    x, w, b = _randn(torch, 1, m, k, std=2.0), _randn(torch, 2, n, k, std=1 / math.sqrt(k)), _randn(torch, 3, n, dtype=dst)
+    codes, weight = P.quantize_rows(x), P.quantize_rows(w)
+    for bias in (None, b):
+        for act in (None, "silu"):
+            got = P.i8_linear(codes, weight, bias, act=act, dtype=_dt(torch, dst))
+            _check_linear(got, O.i8_rows(_f64(x)), O.i8_rows(_f64(w)), None if bias is None else _f64(bias), act is not None, dst)
+            assert torch.equal(got, P.i8_linear(x, weight, bias, act=act, dtype=_dt(torch, dst)))
+
+
+@pytest.mark.parametrize("m", [1, 16, 17, 32])
+@pytest.mark.parametrize("k,n", [(2048, 12288), (6144, 2048)])
+def test_linear_feed_forward_steps(torch, P, m, k, n):
+    """The two widths of a feed-forward layer for a step's rows, of rows and of codes."""
+    x, w = _randn(torch, 1, m, k, std=2.0), _randn(torch, 2, n, k, std=1 / math.sqrt(k))
+    weight = P.quantize_rows(w)
+    got = P.i8_linear(x, weight)
+    _check_linear(got, O.i8_rows(_f64(x)), O.i8_rows(_f64(w)), None, False, "bf16")
+    assert torch.equal(P.i8_linear(P.quantize_rows(x), weight), got)
+
+
 def test_linear_longest_rows(torch, P):
     """131071 products of -128 and -128 still fit the sum."""
     k = 131071
