@@ -34,7 +34,8 @@ extern "C" {
 /* Rows in 8 bits. Row r of a matrix [rows, cols] is held as codes c (int8, -127 .. 127)
  * and one scale s (float): x ~ c s, with
  *   s = max(max |x| * (1/127), 2^-126), factor and product rounded to fp32 (max |x| / 127, give or take
- *       one unit in the last place),
+ *       one unit in the last place: the bits that torch's division by 127 has on this device, so that scales
+ *       and codes made there are those made here),
  *   c = x / s rounded to the nearest whole number, ties to the even one (the exact
  *       quotient, not its fp32 rounding).
  * A row that holds an infinity or NaN gets the scale NaN and codes of zero.

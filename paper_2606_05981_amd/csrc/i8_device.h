@@ -94,7 +94,9 @@ template <int STEP> __device__ __forceinline__ uint32_t lanes_top(uint32_t t) {
   return t;
 }
 
-// Codes are those of the exact quotient. x times the rounded 1 / s is off by 2^-16 at most, so that its nearest whole
+// s is top times the rounded 1 / 127, as torch divides by a number here: 4.7% of fp32 values and 6 of bf16's 128 mantissas
+// lie a unit in the last place from the rounded quotient, and beside a half their codes would differ.
+// Codes are those of the exact quotient x / s. x times the rounded 1 / s is off by 2^-16 at most, so that its nearest whole
 // number (the sum with 1.5 2^23 leaves it in the low bits) is the quotient's, unless it lies next to a half. There,
 // c may be off by one: r = x - c s is exact in one fma (a multiple of the finer ulp of x and s, and no more
 // than s), and c moves by one towards r where |r| is more than s / 2, or is s / 2 and c odd. 7 instructions an

@@ -38,7 +38,7 @@ template <bool ACT> __device__ __forceinline__ float finish(int acc, float s, fl
 // turn; its waves share K, 128 bytes of each row at a time, straight from memory to the operands (the next
 // block's loads are in flight meanwhile), and add up through LDS. The rows of a are few enough to lie in LDS
 // whole; every workgroup quantises them for itself, once, while its first weights arrive: a launch less than with
-// codes through memory (1 x 2048 x 2048: 8.4 us replayed, 14.2 called; so 5.3 and 8.7). 16 x 2048 x 12288: 10.7 us, 2.4
+// codes through memory (1 x 2048 x 2048: 8.4 us replayed, 14.2 called; so 5.1 and 9.7). 16 x 2048 x 12288: 10.7 us, 2.4
 // TB/s, of which launch, quantising and the last sums are about 5; 4 x 6144 x 12288: 20 us, 3.7 TB/s. Three blocks of weights
 // ahead instead of one change nothing.
 // LDS: rows of codes 64 bytes further apart than they are long, so that an operand's 16 rows of 64 bytes
@@ -176,9 +176,11 @@ template <typename T, typename TO, bool ACT> hipError_t run_few(const I8Args &g,
   return g.m <= 16 ? launch_few<T, TO, ACT, 1>(g, s) : launch_few<T, TO, ACT, 2>(g, s);
 }
 // 17 to 32 rows: where every workgroup has one block of columns, and rows that it quantises itself are short,
-// since all of them repeat that (us replayed / called, against tiles; 32 x 640 x 2048: 6.8 / 9.3, 7.5 / 13.9;
-// 32 x 2048 x 2048: 10.6 / 10.6, 10.7 / 13.9, of codes 4.8 against 6.1; 32 x 2048 x 8192: 13.6 / 13.5, 10.9 / 13.7;
-// 32 x 2944 x 2048: 16.2 / 15.9, 13.3 / 13.8, of codes 5.6 against 7.3).
+// since all of them repeat that. us replayed / called, against tiles: 17 x 640 x 2048 6.7 / 8.6, 7.4 / 14.4; 32 x 640 x
+// 2048 7.3 / 8.8, 7.7 / 14.5; 17 x 2048 x 4096 10.7 / 10.0, 10.8 / 14.4; of codes 32 x 2048 x 2048 5.3, 6.1. The line is drawn
+// for the call, which gains 3 to 6 everywhere within it; replayed, the longest rows lose near it: 32 x 2048 x 2048
+// 11.9 / 11.5, 11.1 / 14.4; 32 x 2048 x 4096 12.2 / 11.6, 11.1 / 14.5 (fp32 rows 11.7 against 9.8, the most). Beyond it
+// the call gains nothing: 32 x 2048 x 8192 13.6 / 13.5, 10.9 / 13.7; 32 x 2944 x 2048 16.2 / 15.9, 13.3 / 13.8.
 bool takes_few(int m, int pitch, int n, bool codes) {
   if (m > kFewRows || few_lds(m, pitch) > kFewLds) return false;
   return m <= 16 || (n <= 16 * 256 && (codes || pitch <= 2048));

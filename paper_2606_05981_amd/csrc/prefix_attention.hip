@@ -535,7 +535,7 @@ constexpr int kFill = 512;           // workgroups that fill the compute units w
 struct Plan {
   enum Kind { FEW, MANY } kind = FEW;
   int TR = 32, KT = 128;             // rows of a tile, keys of the tiles that ranges are cut in
-  bool shared = false, split = false;
+  bool shared = false;
   KeyCut p_cut{1, INT_MAX}, cut{1, INT_MAX};
   int p_tiles = 0, p_parts = 0;      // shared: row tiles of all rows, parts of the prefix
   int64_t units = 0;                 // with partial results, of the launch with the most; p_tiles * p_parts among them
@@ -607,7 +607,6 @@ Plan prefix_plan(const AttnProblem &p, int p_len, const int32_t *kv_lens) {
     if (p.q_lens[i] == 0) continue;
     const int used = list(i) == 0 ? 0 : parts_of(list(i), pl.cut);
     own = std::max(own, used);
-    pl.split |= used > 1;
     if (used > 1 || pl.shared) at += (int64_t)tiles_of((int64_t)p.q_lens[i] * rep, pl.TR) * used;
     top = std::max(top, at);
     if (++in == kCondSeqs) in = 0, at = 0;

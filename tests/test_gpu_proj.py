@@ -109,6 +109,18 @@ def test_quantize_borders(torch, P, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_are_those_that_torch_computes_here(torch, P, dtype):
+    """max |x| / 127 as torch has it on this device, bit for bit: rows of every bf16 mantissa, and of others in fp32. It is
+    not the rounded quotient of 64 bits, which differs for some of them."""
+    x = torch.cat([1 + torch.arange(128) / 128] + [torch.rand(4000, generator=torch.Generator().manual_seed(9)) + 2.0 ** e for e in (-20, 0, 9)])
+    x = x[:, None].mul(torch.tensor([0.25, -1.0, 0.5])).to(_dt(torch, dtype)).cuda()
+    rows, top = P.quantize_rows(x), x.float().abs().amax(1)
+    assert torch.equal(rows.scales, top / 127)
+    assert (rows.scales != (top.double() / 127).float()).any()
+    _check_rows(rows, x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m,k,wide,skip", [(5, 320, 3, 0), (5, 320, 8, 0), (4, 77, 0, 1), (6, 640, 1, 5), (3, 5000, 11, 3)])
 def test_quantize_strided(torch, P, m, k, wide, skip, dtype):
     """Rows of a wider buffer, at odd strides and addresses."""
